@@ -189,7 +189,7 @@ def prepare(case, seed):
 
 def _act(name, z):
     if name == "relu":
-        return torch.where(z > 0, z, torch.zeros_like(z))
+        return torch.where(z < 0, torch.zeros_like(z), z)
     if name == "gelu":
         return 0.5 * z * (1 + torch.erf(z * 0.5 ** 0.5))
     if name == "silu":
