@@ -588,6 +588,237 @@ sadmm_status sadmm_conv_bwd(const sadmm_plan* plan, const void* x, const void* d
 sadmm_status sadmm_gemm_bf16(const void* A, const void* B, float* C, long long M, long long N, long long K,
                              long long ldc, int accumulate, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Feed-forward operators.  Structured pruning of a language model takes hidden
+ * units out of its feed-forward blocks: a unit is a row (filter) of the block's
+ * first products and a column of its last one (the row and column pruning of
+ * Sec. 3 on plain matrices), and a pruned block is a smaller dense block of any
+ * width.  These calls run and retrain such a block:
+ *
+ *   sadmm_layernorm_fwd / _bwd   the norm before it
+ *   sadmm_gated_fwd / _bwd       act(x Wg^T + bg) * (x Wu^T + bu)
+ *   sadmm_linear_fwd / _bwd      act(x W^T + bias) + residual
+ *
+ * Conventions beyond those above:
+ *  - A matrix is row-major with a row stride `ld...` in elements, at least its
+ *    width and below 2^38; x, W, z, g, u, h, dh are bf16, vectors (bias, gamma,
+ *    beta, mean, rstd and their gradients) fp32, other types as said.  Pointers
+ *    stand on their elements' boundaries.  The products read matrices whose
+ *    base is 16-byte aligned and whose row stride is a multiple of 8 where they
+ *    lie; any other is first copied to the workspace, so a program that keeps
+ *    weights of an odd width does well to give their rows a padded stride.
+ *  - The workspace is device scratch, 256-byte aligned, of at least the
+ *    ..._workspace_size() of the same arguments (0: none needed, NULL allowed);
+ *    its contents need not be kept between calls.  The size functions return 0
+ *    for arguments that the call would refuse.
+ *  - `tokens` (`rows`) may be 0: nothing is read, the token matrices may be
+ *    NULL, and gradients summed over tokens are set to zero.  Up to
+ *    0x7fffff00 tokens and widths up to 2^28 (else SADMM_EUNSUPPORTED).
+ *  - Outputs must not overlap inputs or each other (equal pointers give
+ *    SADMM_EINVAL); the exceptions are y = residual in sadmm_linear_fwd, y = x
+ *    of the same type in sadmm_layernorm_fwd and dx = dres in
+ *    sadmm_layernorm_bwd, with the same row stride.  Rows of several matrices
+ *    may interleave in one buffer.
+ *  - Sums are taken in fp32, in an order that depends on the arguments' sizes
+ *    alone: the same call gives the same bits.  Infinities and NaN go through
+ *    the formulas; nothing outside a matrix's rows and columns reaches an
+ *    output.
+ */
+typedef enum {
+    SADMM_ACT_NONE = 0, /* z                                              */
+    SADMM_ACT_RELU = 1, /* max(z, 0), NaN kept; slope [z > 0]             */
+    SADMM_ACT_GELU = 2, /* z Phi(z), Phi the normal distribution (by erf) */
+    SADMM_ACT_SILU = 3  /* z / (1 + exp(-z))                              */
+} sadmm_act;
+
+/*
+ * Layer norm of each row: y = gamma (x - mean) rstd + beta with the row's mean
+ * and rstd = (var + eps)^(-1/2), var = avg (x - mean)^2.
+ *   x, y         [rows][cols] of type xdt, ydt (bf16 or fp32).
+ *   gamma, beta  [cols] or NULL (1, 0).
+ *   mean, rstd   [rows], each may be NULL: kept for the backward pass.
+ *   eps          >= 0, finite.
+ */
+typedef struct {
+    long long rows;
+    int cols;
+    const void* x;
+    long long ldx;
+    int xdt;
+    const float* gamma;
+    const float* beta;
+    float eps;
+    void* y;
+    long long ldy;
+    int ydt;
+    float* mean;
+    float* rstd;
+} sadmm_layernorm_fwd_args;
+sadmm_status sadmm_layernorm_fwd(const sadmm_layernorm_fwd_args* a, void* stream);
+
+/*
+ * Its backward pass.  With xhat = (x - mean) rstd and d = gamma dy:
+ *   dx     = rstd (d - avg d - xhat avg(d xhat)) + dres   [rows][cols] of type xdt
+ *   dgamma = sum over rows of dy xhat                     [cols]
+ *   dbeta  = sum over rows of dy                          [cols]
+ *   dy     [rows][cols] of type dydt; mean, rstd as the forward pass left them.
+ *   dres   [rows][cols] of type xdt or NULL: the gradient that reaches x along
+ *          the block's residual.
+ * Each output may be NULL (not all three).
+ */
+typedef struct {
+    long long rows;
+    int cols;
+    const void* x;
+    long long ldx;
+    int xdt;
+    const void* dy;
+    long long lddy;
+    int dydt;
+    const float* gamma;
+    const float* mean;
+    const float* rstd;
+    const void* dres;
+    long long lddres;
+    void* dx;
+    long long lddx;
+    float* dgamma;
+    float* dbeta;
+} sadmm_layernorm_bwd_args;
+size_t sadmm_layernorm_bwd_workspace_size(const sadmm_layernorm_bwd_args* a);
+sadmm_status sadmm_layernorm_bwd(const sadmm_layernorm_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * y = act(z) + residual, z = x W^T + bias.
+ *   x        [tokens][n_in];  w [n_out][n_in] (the plan's packed rows of
+ *            sadmm_pack for a 1x1 layer are such a matrix).
+ *   bias     [n_out] or NULL.
+ *   residual [tokens][n_out] of type ydt or NULL.
+ *   y        [tokens][n_out] of type ydt, rounded once.
+ *   z        [tokens][n_out] bf16 or NULL: kept for the backward pass.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_out;
+    const void* x;
+    long long ldx;
+    const void* w;
+    long long ldw;
+    const float* bias;
+    const void* residual;
+    long long ldr;
+    int act;
+    void* y;
+    long long ldy;
+    int ydt;
+    void* z;
+    long long ldz;
+} sadmm_linear_fwd_args;
+size_t sadmm_linear_fwd_workspace_size(const sadmm_linear_fwd_args* a);
+sadmm_status sadmm_linear_fwd(const sadmm_linear_fwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass, dz = dy act'(z):
+ *   dx = dz W    [tokens][n_in] of type dxdt
+ *   dw = dz^T x  [n_out][n_in] of type dwdt
+ *   db = sum over tokens of dz  [n_out]
+ * (The residual's gradient is dy.)  dy is [tokens][n_out] of type dydt; z is not
+ * read for SADMM_ACT_NONE.  Each output may be NULL (not all three); w is read
+ * for dx, x for dw.  dz is an operand of the tensor cores and rounded to bf16
+ * once for dx and dw (exact for a bf16 dy without an activation); db is summed
+ * before that rounding.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_out;
+    const void* dy;
+    long long lddy;
+    int dydt;
+    const void* x;
+    long long ldx;
+    const void* w;
+    long long ldw;
+    const void* z;
+    long long ldz;
+    int act;
+    void* dx;
+    long long lddx;
+    int dxdt;
+    void* dw;
+    long long lddw;
+    int dwdt;
+    float* db;
+} sadmm_linear_bwd_args;
+size_t sadmm_linear_bwd_workspace_size(const sadmm_linear_bwd_args* a);
+sadmm_status sadmm_linear_bwd(const sadmm_linear_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * h = act(g) * u, g = x Wg^T + bg, u = x Wu^T + bu, in one kernel.
+ *   x  [tokens][n_in];  wg, wu [n_hidden][n_in];  bg, bu [n_hidden] or NULL.
+ *   h  [tokens][n_hidden] bf16, rounded once.
+ *   g, u [tokens][n_hidden] bf16, each may be NULL: kept for the backward pass.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_hidden;
+    const void* x;
+    long long ldx;
+    const void* wg;
+    long long ldwg;
+    const void* wu;
+    long long ldwu;
+    const float* bg;
+    const float* bu;
+    int act;
+    void* h;
+    long long ldh;
+    void* g;
+    long long ldg;
+    void* u;
+    long long ldu;
+} sadmm_gated_fwd_args;
+size_t sadmm_gated_fwd_workspace_size(const sadmm_gated_fwd_args* a);
+sadmm_status sadmm_gated_fwd(const sadmm_gated_fwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass, dg = dh u act'(g), du = dh act(g):
+ *   dx  = dg Wg + du Wu   [tokens][n_in] of type dxdt
+ *   dwg = dg^T x, dwu = du^T x   [n_hidden][n_in] of type dwdt (both or neither)
+ *   dbg, dbu = sums over tokens of dg, du   [n_hidden]
+ * Each may be NULL (not all); wg and wu are read for dx, x for dwg and dwu.  dg
+ * and du are rounded to bf16 once for the products; dbg and dbu are summed
+ * before that.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_hidden;
+    const void* dh;
+    long long lddh;
+    const void* x;
+    long long ldx;
+    const void* wg;
+    long long ldwg;
+    const void* wu;
+    long long ldwu;
+    const void* g;
+    long long ldg;
+    const void* u;
+    long long ldu;
+    int act;
+    void* dx;
+    long long lddx;
+    int dxdt;
+    void* dwg;
+    long long lddwg;
+    void* dwu;
+    long long lddwu;
+    int dwdt;
+    float* dbg;
+    float* dbu;
+} sadmm_gated_bwd_args;
+size_t sadmm_gated_bwd_workspace_size(const sadmm_gated_bwd_args* a);
+sadmm_status sadmm_gated_bwd(const sadmm_gated_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
 /*
  * Failure-detection self-test; the paper has no counterpart.  Runs, in one
  * CTA on `stream`, the bounded mbarrier wait every pipelined kernel here uses,

@@ -6,5 +6,7 @@ include/sadmm.h); ``sadmm`` is its ctypes binding.
 from . import build
 from .sadmm import (  # noqa: F401
     SADMM_BF16, SADMM_FP32, SADMM_COL_NONE, SADMM_COL_SHAPE, SADMM_COL_CHANNEL,
+    SADMM_ACT_NONE, SADMM_ACT_RELU, SADMM_ACT_GELU, SADMM_ACT_SILU,
     SadmmError, PrunedConv, project_groups, load, make_desc,
+    layer_norm, layer_norm_backward, linear, linear_backward, gated, gated_backward,
 )

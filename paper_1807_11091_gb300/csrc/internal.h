@@ -162,6 +162,26 @@ sadmm_status launch_conv_slab(const sadmm_plan* plan, const Geometry& g, const v
 sadmm_status launch_conv_fwd(const sadmm_plan* plan, const Geometry& g, const void* x, const float* bias,
                              int relu, void* y, int ydt, int phase, cudaStream_t s);
 
+// ---- feed-forward products (linear.cu, tgemm.cu) ----
+// Scratch bytes and launches of checked arguments.
+size_t linear_fwd_bytes(const sadmm_linear_fwd_args& a);
+size_t linear_bwd_bytes(const sadmm_linear_bwd_args& a);
+size_t gated_fwd_bytes(const sadmm_gated_fwd_args& a);
+size_t gated_bwd_bytes(const sadmm_gated_bwd_args& a);
+sadmm_status launch_linear_fwd(const sadmm_linear_fwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_linear_bwd(const sadmm_linear_bwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_gated_fwd(const sadmm_gated_fwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_gated_bwd(const sadmm_gated_bwd_args& a, void* ws, cudaStream_t s);
+// out[c] (out2[c]) = the sum of part[0 .. parts-1][c] (part2), in a fixed order.
+// part2 NULL: one sum; out / out2 NULL: not written.
+sadmm_status launch_colsum(const float* part, const float* part2, float* out, float* out2, long long cols, int parts,
+                           cudaStream_t s);
+
+// ---- layer norm (norm.cu) ----
+size_t layernorm_bwd_bytes(const sadmm_layernorm_bwd_args& a);
+sadmm_status launch_layernorm_fwd(const sadmm_layernorm_fwd_args& a, cudaStream_t s);
+sadmm_status launch_layernorm_bwd(const sadmm_layernorm_bwd_args& a, void* ws, cudaStream_t s);
+
 // Tap-mask encoding of the gather table: 0 = one bit per tap (at most 31
 // taps), 1 = (kt,kh) row bits 0..15 and kw bits 16..30.  Bit 31 marks padding
 // columns and is never valid.
