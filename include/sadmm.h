@@ -619,8 +619,9 @@ sadmm_status sadmm_gemm_bf16(const void* A, const void* B, float* C, long long M
  *    of the same type in sadmm_layernorm_fwd and dx = dres in
  *    sadmm_layernorm_bwd, with the same row stride.  Rows of several matrices
  *    may interleave in one buffer.
- *  - Sums are taken in fp32, in an order that depends on the arguments' sizes
- *    alone: the same call gives the same bits.  Infinities and NaN go through
+ *  - Sums are taken in fp32, in an order that depends on the arguments' sizes,
+ *    types and alignment alone, not on which outputs are wanted: the same call
+ *    gives the same bits.  Infinities and NaN go through
  *    the formulas; nothing outside a matrix's rows and columns reaches an
  *    output.
  */

@@ -29,7 +29,7 @@ DEBUG_LIB = os.path.join(BUILD, "debug", "libsadmm.so")
 
 SOURCES = ["abi.cu", "project.cu", "pack.cu", "conv_fwd.cu", "conv_slab.cu", "admm.cu", "elements.cu", "gemm.cu",
            "bwd.cu", "bwd_slab.cu", "bwd_grid.cu", "conv_grid.cu", "sparse.cu", "abi_ffn.cu", "norm.cu", "linear.cu",
-           "tgemm.cu"]
+           "tgemm.cu", "tgemm_pair.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -99,6 +99,41 @@ def build(force: bool = False, verbose: bool = False, extra: List[str] | None = 
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, lib)
     return lib
+
+
+TORCH_LIB = os.path.join(BUILD, "torch_ffn.so")
+
+
+def build_torch_binding(force: bool = False) -> str:
+    """Compile csrc/torch_ffn.cpp, the feed-forward operators' binding, against the
+    torch of this interpreter (host code only).  Returns the module's path."""
+    import sysconfig
+
+    import torch
+    src = os.path.join(CSRC, "torch_ffn.cpp")
+    made_for = f"{sys.version} torch {torch.__version__}"
+    note = TORCH_LIB + ".for"
+    if not force and os.path.exists(TORCH_LIB) and os.path.exists(note) and open(note).read() == made_for:
+        t = os.path.getmtime(TORCH_LIB)
+        if all(os.path.getmtime(p) <= t for p in (src, os.path.join(INCLUDE, "sadmm.h"))):
+            return TORCH_LIB
+    os.makedirs(BUILD, exist_ok=True)
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    tmp = TORCH_LIB + f".tmp{os.getpid()}"
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-I", INCLUDE,
+           "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
+           "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(cuda, "include"), src, "-o", tmp, "-L", os.path.join(base, "lib"),
+           "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ldl"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on torch_ffn.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, TORCH_LIB)
+    with open(note, "w") as f:
+        f.write(made_for)
+    return TORCH_LIB
 
 
 if __name__ == "__main__":

@@ -420,7 +420,7 @@ sadmm_status launch_linear_fwd(const sadmm_linear_fwd_args& a, void* ws, cudaStr
     t.y = {a.y, a.ldy, a.ydt};
     t.residual = {const_cast<void*>(a.residual), a.ldr, a.ydt};
     t.z = {a.z, a.ldz, SADMM_BF16};
-    return launch_tgemm(t, s);
+    return launch_tgemm(&t, 1, s);
 }
 
 sadmm_status launch_linear_bwd(const sadmm_linear_bwd_args& a, void* ws, cudaStream_t s)
@@ -447,29 +447,23 @@ sadmm_status launch_linear_bwd(const sadmm_linear_bwd_args& a, void* ws, cudaStr
         d.act = a.act;
         SADMM_TRY(launch_dact(d, false, s));
     }
-    TgProblem t;
-    if (a.dx) {
-        SADMM_TRY(fill(p.w, a.w, a.n_out, a.n_in, a.ldw, s));
-        memset(&t, 0, sizeof(t));
-        t.mode = kTgSingle;
-        t.a[0] = kmajor(p.dz, a.tokens, a.n_out);
-        t.b[0] = across(p.w, a.n_in, a.n_out);
-        t.m = a.tokens;
-        t.n = a.n_in;
-        t.y = {a.dx, a.lddx, a.dxdt};
-        SADMM_TRY(launch_tgemm(t, s));
-    }
-    if (a.dw) {
-        SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
-        memset(&t, 0, sizeof(t));
-        t.mode = kTgSingle;
-        t.a[0] = across(p.dz, a.n_out, a.tokens);
-        t.b[0] = across(p.x, a.n_in, a.tokens);
-        t.m = a.n_out;
-        t.n = a.n_in;
-        t.y = {a.dw, a.lddw, a.dwdt};
-        SADMM_TRY(launch_tgemm(t, s));
-    }
+    if (a.dx) SADMM_TRY(fill(p.w, a.w, a.n_out, a.n_in, a.ldw, s));
+    if (a.dw) SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
+    TgProblem t[2];
+    memset(t, 0, sizeof(t));
+    t[0].mode = t[1].mode = kTgSingle;
+    t[0].a[0] = kmajor(p.dz, a.tokens, a.n_out);
+    t[0].b[0] = across(p.w, a.n_in, a.n_out);
+    t[0].m = a.tokens;
+    t[0].n = t[1].n = a.n_in;
+    t[0].y = {a.dx, a.lddx, a.dxdt};
+    t[0].skip = !a.dx;
+    t[1].a[0] = across(p.dz, a.n_out, a.tokens);
+    t[1].b[0] = across(p.x, a.n_in, a.tokens);
+    t[1].m = a.n_out;
+    t[1].y = {a.dw, a.lddw, a.dwdt};
+    t[1].skip = !a.dw;
+    SADMM_TRY(launch_tgemm(t, 2, s));
     if (a.db) SADMM_TRY(launch_colsum(p.part, nullptr, a.db, nullptr, a.n_out, (int)dact_chunks(a.tokens), s));
     return SADMM_OK;
 }
@@ -496,7 +490,7 @@ sadmm_status launch_gated_fwd(const sadmm_gated_fwd_args& a, void* ws, cudaStrea
     t.y = {a.h, a.ldh, SADMM_BF16};
     t.z = {a.g, a.ldg, SADMM_BF16};
     t.u = {a.u, a.ldu, SADMM_BF16};
-    return launch_tgemm(t, s);
+    return launch_tgemm(&t, 1, s);
 }
 
 sadmm_status launch_gated_bwd(const sadmm_gated_bwd_args& a, void* ws, cudaStream_t s)
@@ -526,34 +520,32 @@ sadmm_status launch_gated_bwd(const sadmm_gated_bwd_args& a, void* ws, cudaStrea
     d.cols = a.n_hidden;
     d.act = a.act;
     SADMM_TRY(launch_dact(d, true, s));
-    TgProblem t;
     if (a.dx) {
         SADMM_TRY(fill(p.wg, a.wg, a.n_hidden, a.n_in, a.ldwg, s));
         SADMM_TRY(fill(p.wu, a.wu, a.n_hidden, a.n_in, a.ldwu, s));
-        memset(&t, 0, sizeof(t));
-        t.mode = kTgSum;
-        t.a[0] = kmajor(p.dg, a.tokens, a.n_hidden);
-        t.a[1] = kmajor(p.du, a.tokens, a.n_hidden);
-        t.b[0] = across(p.wg, a.n_in, a.n_hidden);
-        t.b[1] = across(p.wu, a.n_in, a.n_hidden);
-        t.m = a.tokens;
-        t.n = a.n_in;
-        t.y = {a.dx, a.lddx, a.dxdt};
-        SADMM_TRY(launch_tgemm(t, s));
     }
-    if (a.dwg) {
-        SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
-        memset(&t, 0, sizeof(t));
-        t.mode = kTgPair;
-        t.a[0] = across(p.dg, a.n_hidden, a.tokens);
-        t.a[1] = across(p.du, a.n_hidden, a.tokens);
-        t.b[0] = across(p.x, a.n_in, a.tokens);
-        t.m = a.n_hidden;
-        t.n = a.n_in;
-        t.y = {a.dwg, a.lddwg, a.dwdt};
-        t.y2 = {a.dwu, a.lddwu, a.dwdt};
-        SADMM_TRY(launch_tgemm(t, s));
+    if (a.dwg) SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
+    TgProblem t[3];
+    memset(t, 0, sizeof(t));
+    t[0].mode = kTgSum;
+    t[0].a[0] = kmajor(p.dg, a.tokens, a.n_hidden);
+    t[0].a[1] = kmajor(p.du, a.tokens, a.n_hidden);
+    t[0].b[0] = across(p.wg, a.n_in, a.n_hidden);
+    t[0].b[1] = across(p.wu, a.n_in, a.n_hidden);
+    t[0].m = a.tokens;
+    t[0].n = a.n_in;
+    t[0].y = {a.dx, a.lddx, a.dxdt};
+    t[0].skip = !a.dx;
+    for (int i = 1; i < 3; ++i) {
+        t[i].mode = kTgSingle;
+        t[i].a[0] = across(i == 1 ? p.dg : p.du, a.n_hidden, a.tokens);
+        t[i].b[0] = across(p.x, a.n_in, a.tokens);
+        t[i].m = a.n_hidden;
+        t[i].n = a.n_in;
+        t[i].y = i == 1 ? TgMatrix{a.dwg, a.lddwg, a.dwdt} : TgMatrix{a.dwu, a.lddwu, a.dwdt};
+        t[i].skip = !a.dwg;
     }
+    SADMM_TRY(launch_tgemm(t, 3, s));
     if (p.part_g) SADMM_TRY(launch_colsum(p.part_g, p.part_u, a.dbg, a.dbu, a.n_hidden, (int)dact_chunks(a.tokens), s));
     return SADMM_OK;
 }

@@ -5,10 +5,13 @@
 //   d = gamma dy,  dx = rstd (d - avg(d) - xhat avg(d xhat)) [+ dres]
 //   dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy
 //
-// Bound by memory: a row is read once and kept in registers by the threads that
-// share it (a warp, or a block for long rows), in fp32; mean and variance are
+// Bound by memory.  A group of threads (a warp, or a block for long rows) takes
+// a row at a time and keeps it in registers in fp32; mean and variance are
 // taken one after the other from those registers, so the variance has no
-// cancellation.  The backward's threads own fixed columns, add up their shares
+// cancellation.  The group's next rows are on their way meanwhile: bulk copies
+// into a ring of rows in shared memory (the row's barrier of the reduction
+// frees a place), because the registers that would hold enough loads in flight
+// are not there.  The backward's threads own fixed columns, add up their shares
 // of dgamma and dbeta over the rows of their block in registers and leave one
 // partial sum per block, which a second kernel adds up in block order.  Rows
 // too long for registers are read again from cache instead.
@@ -93,30 +96,126 @@ SADMM_DEV void store_row(T* p, const Cols<VEC>& c, int k, const float (&v)[8])
     }
 }
 
-// Sums over the threads of a row: a warp, or the whole block (`slot` alternates
-// between calls so that one barrier a call is enough).
-SADMM_DEV float2 warp_sum(float2 v)
+// Sums over the threads of a row: a warp, or the whole block through shared
+// memory.  `slot` alternates between calls, so that one barrier a call is
+// enough.  Every thread adds the warps' sums up in the same order.
+SADMM_DEV float warp_sum(float v)
 {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+struct __align__(16) RowSums {
+    float v[2][2][32];  // [slot][which][warp]
+};
+
+template <bool BLOCK>
+SADMM_DEV float row_sum(float v, RowSums& red, int slot)
+{
+    v = warp_sum(v);
+    if (BLOCK) {
+        const int warp = threadIdx.x >> 5, n = blockDim.x >> 5;
+        if ((threadIdx.x & 31) == 0) red.v[slot][0][warp] = v;
+        __syncthreads();
+        v = 0.0f;
+        for (int w = 0; w < n; w += 4) {  // the places past the last warp hold zeros
+            const float4 q = *reinterpret_cast<const float4*>(&red.v[slot][0][w]);
+            v += (q.x + q.y) + (q.z + q.w);
+        }
     }
     return v;
 }
 
 template <bool BLOCK>
-SADMM_DEV float2 row_sum(float2 v, float2 (*red)[32], int slot)
+SADMM_DEV float2 row_sum2(float x, float y, RowSums& red, int slot)
 {
-    v = warp_sum(v);
+    x = warp_sum(x);
+    y = warp_sum(y);
     if (BLOCK) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockDim.x >> 5;
-        if (lane == 0) red[slot][warp] = v;
+        const int warp = threadIdx.x >> 5, n = blockDim.x >> 5;
+        if ((threadIdx.x & 31) == 0) {
+            red.v[slot][0][warp] = x;
+            red.v[slot][1][warp] = y;
+        }
         __syncthreads();
-        v = warp_sum(lane < n ? red[slot][lane] : make_float2(0.0f, 0.0f));
+        x = y = 0.0f;
+        for (int w = 0; w < n; w += 4) {
+            const float4 p = *reinterpret_cast<const float4*>(&red.v[slot][0][w]);
+            const float4 q = *reinterpret_cast<const float4*>(&red.v[slot][1][w]);
+            x += (p.x + p.y) + (p.z + p.w);
+            y += (q.x + q.y) + (q.z + q.w);
+        }
     }
-    return v;
+    return make_float2(x, y);
 }
+
+SADMM_DEV void clear(RowSums& red)
+{
+    for (int i = threadIdx.x; i < 128; i += blockDim.x) (&red.v[0][0][0])[i] = 0.0f;
+}
+
+// ------------------------------------------------------------------ ring --
+
+constexpr int kRingStages = 8;  // at most
+
+SADMM_DEV void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                     smem_u32(dst)),
+                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// Every copy has been waited for, unless a wait gave up: then some time for
+// those in flight to land before the block's shared memory is given back.
+SADMM_DEV void drain_after_failure(volatile int& abort_flag)
+{
+    if (!abort_flag) return;
+    const unsigned long long t0 = globaltimer();
+    while (globaltimer() - t0 < 10000000ull) {}
+}
+
+// What a bulk copy takes of row r: its whole eights (VEC; the ragged end is read
+// from global memory), or the 16-byte words that hold it.  Those of the first
+// and last row would reach past the matrix, so these rows are read directly.
+template <bool VEC, typename T>
+struct Part {
+    const T* p;
+    long long ld, rows;
+    int cols;
+    SADMM_DEV bool copied(long long r) const { return VEC || (r > 0 && r < rows - 1); }
+    SADMM_DEV const uint8_t* from(long long r) const
+    {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p + r * ld);
+        return reinterpret_cast<const uint8_t*>(VEC ? a : a & ~uintptr_t(15));
+    }
+    SADMM_DEV uint32_t bytes(long long r) const
+    {
+        if (VEC) return (uint32_t)(cols & ~7) * (uint32_t)sizeof(T);
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p + r * ld);
+        return (uint32_t)(((a + (uintptr_t)cols * sizeof(T) + 15) & ~uintptr_t(15)) - (a & ~uintptr_t(15)));
+    }
+    // Room for a copy of any row.
+    static __host__ __device__ int room(int cols) { return (cols * (int)sizeof(T) + 32 + 127) / 128 * 128; }
+    // The k-th eight of row r, from its copy at `s` (NULL: from global memory).
+    SADMM_DEV void load(const Cols<VEC>& c, const uint8_t* s, long long r, int k, float fill, float (&v)[8]) const
+    {
+        const T* g = p + r * ld;
+        if (VEC) {
+            if (s && c.whole(k))
+                load_vec(reinterpret_cast<const T*>(s) + c.at(k, 0), v);
+            else
+                load_row<VEC>(g, c, k, fill, v);
+        } else if (s) {
+            const T* q = reinterpret_cast<const T*>(s + (reinterpret_cast<uintptr_t>(g) & 15));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = c.at(k, j) < c.cols ? to_f32(q[c.at(k, j)]) : fill;
+        } else {
+            load_row<VEC>(g, c, k, fill, v);
+        }
+    }
+};
 
 struct FwdArgs {
     const void* x;
@@ -127,76 +226,141 @@ struct FwdArgs {
     float* rstd;
     long long rows, ldx, ldy;
     int cols;
+    int stages;  // rows of the ring (0: rows are read directly)
     float eps;
     float n;  // cols: sums are divided by it, so that a constant row's mean is that constant
+    int* status;
 };
 
-template <typename X, typename Y, bool VEC, bool BLOCK, int E>
-__global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_ln_fwd(const FwdArgs a)
+// CAP: threads of a block at most; 0: rows are taken by warps, eight a block.
+// Up to 16 columns a thread, gamma and beta stay in registers too.
+template <typename X, typename Y, bool VEC, int CAP, int E>
+__global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 256 || CAP == 0 ? 3 : 1) k_ln_fwd(const FwdArgs a)
 {
-    __shared__ float2 red[2][32];
+    constexpr bool BLOCK = CAP > 0, KEEP = E <= 2;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ RowSums red;
+    __shared__ uint64_t bars[BLOCK ? 1 : 8][kRingStages];
+    __shared__ volatile int abort_flag;
+    const int G = BLOCK ? blockDim.x : 32, R = BLOCK ? 1 : blockDim.x / 32;
+    const int group = BLOCK ? 0 : threadIdx.x >> 5;
+    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols};
+    const long long first = (long long)blockIdx.x * R + group, step = (long long)gridDim.x * R;
+    const Part<VEC, X> x = {static_cast<const X*>(a.x), a.ldx, a.rows, a.cols};
+    const int room = Part<VEC, X>::room(a.cols);
+    uint8_t* mine = ring + (size_t)group * a.stages * room;
+    uint64_t* bar = bars[group];
+    if (threadIdx.x == 0) abort_flag = 0;
+    if (c.t == 0) {
+        for (int s = 0; s < a.stages; ++s) mbar_init(&bar[s], 1);
+        fence_mbar_init();
+    }
+    clear(red);
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
-    const int G = BLOCK ? blockDim.x : 32, R = BLOCK ? 1 : blockDim.x / 32;
-    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols};
-    const long long r = (long long)blockIdx.x * R + (BLOCK ? 0 : threadIdx.x >> 5);
-    if (r >= a.rows) return;
-    const X* x = static_cast<const X*>(a.x) + r * a.ldx;
-    float v[E][8];
-    float2 s = make_float2(0.0f, 0.0f);
+    auto fetch = [&](long long r, int s) {  // by the group's first thread
+        if (r >= a.rows) return;
+        if (x.copied(r)) {
+            mbar_arrive_expect_tx(&bar[s], x.bytes(r));
+            bulk_load(mine + s * room, x.from(r), x.bytes(r), &bar[s]);
+        } else {
+            mbar_arrive(&bar[s]);
+        }
+    };
+    if (c.t == 0)
+        for (int s = 0; s < a.stages; ++s) fetch(first + s * step, s);
+    float g[KEEP ? E : 1][8], b[KEEP ? E : 1][8];
+    auto affine = [&](int k, float (&gk)[8], float (&bk)[8]) {
 #pragma unroll
-    for (int k = 0; k < E; ++k) {
-        load_row<VEC>(x, c, k, 0.0f, v[k]);
+        for (int j = 0; j < 8; ++j) gk[j] = 1.0f, bk[j] = 0.0f;
+        if (a.gamma) load_row<VEC>(a.gamma, c, k, 0.0f, gk);
+        if (a.beta) load_row<VEC>(a.beta, c, k, 0.0f, bk);
+    };
+    if (KEEP) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s.x += v[k][j];
+        for (int k = 0; k < E; ++k) affine(k, g[KEEP ? k : 0], b[KEEP ? k : 0]);
     }
-    const float mean = row_sum<BLOCK>(s, red, 0).x / a.n;
-    s = make_float2(0.0f, 0.0f);
+    int s = 0;
+    uint32_t phase = 0;
+    for (long long r = first; r < a.rows; r += step) {
+        const uint8_t* row = nullptr;
+        if (a.stages) {
+            mbar_wait(&bar[s], phase, &abort_flag, a.status);
+            if (x.copied(r)) row = mine + s * room;
+        }
+        float v[E][8];
+        float sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < E; ++k)
+        for (int k = 0; k < E; ++k) {
+            x.load(c, row, r, k, 0.0f, v[k]);
+            float t = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c.at(k, j) < a.cols) {
-                const float d = v[k][j] - mean;
-                s.x += d * d;
+            for (int j = 0; j < 8; ++j) t += v[k][j];
+            sum += t;
+        }
+        const float mean = row_sum<BLOCK>(sum, red, 0) / a.n;
+        if (a.stages) {  // the whole group has read its row
+            if (!BLOCK) __syncwarp();
+            if (c.t == 0) fetch(r + a.stages * step, s);
+            if (++s == a.stages) { s = 0; phase ^= 1u; }
+        }
+        sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            float t = 0.0f;
+            if (c.whole(k)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = v[k][j] - mean;
+                    t += d * d;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = c.at(k, j) < a.cols ? v[k][j] - mean : 0.0f;
+                    t += d * d;
+                }
             }
-    const float rstd = rsqrtf(row_sum<BLOCK>(s, red, 1).x / a.n + a.eps);
-    if (c.t == 0) {
-        if (a.mean) a.mean[r] = mean;
-        if (a.rstd) a.rstd[r] = rstd;
+            sum += t;
+        }
+        const float rstd = rsqrtf(row_sum<BLOCK>(sum, red, 1) / a.n + a.eps);
+        if (c.t == 0) {
+            if (a.mean) a.mean[r] = mean;
+            if (a.rstd) a.rstd[r] = rstd;
+        }
+        Y* y = static_cast<Y*>(a.y) + r * a.ldy;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            if (!KEEP) affine(k, g[0], b[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = (v[k][j] - mean) * rstd * g[KEEP ? k : 0][j] + b[KEEP ? k : 0][j];
+            store_row<VEC>(y, c, k, v[k]);
+        }
     }
-    Y* y = static_cast<Y*>(a.y) + r * a.ldy;
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-        float g[8], b[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = 1.0f, b[j] = 0.0f;
-        if (a.gamma) load_row<VEC>(a.gamma, c, k, 0.0f, g);
-        if (a.beta) load_row<VEC>(a.beta, c, k, 0.0f, b);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] = (v[k][j] - mean) * rstd * g[j] + b[j];
-        store_row<VEC>(y, c, k, v[k]);
-    }
+    drain_after_failure(abort_flag);
 }
 
 // Rows of any length: a block a row, read three times (from cache after the first).
 template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) k_ln_fwd_long(const FwdArgs a)
 {
-    __shared__ float2 red[2][32];
+    __shared__ RowSums red;
+    clear(red);
     pdl_wait();
     pdl_trigger();
+    __syncthreads();
     const long long r = blockIdx.x;
     const X* x = static_cast<const X*>(a.x) + r * a.ldx;
-    float2 s = make_float2(0.0f, 0.0f);
-    for (int c = threadIdx.x; c < a.cols; c += 1024) s.x += to_f32(x[c]);
-    const float mean = row_sum<true>(s, red, 0).x / a.n;
-    s = make_float2(0.0f, 0.0f);
+    float s = 0.0f;
+    for (int c = threadIdx.x; c < a.cols; c += 1024) s += to_f32(x[c]);
+    const float mean = row_sum<true>(s, red, 0) / a.n;
+    s = 0.0f;
     for (int c = threadIdx.x; c < a.cols; c += 1024) {
         const float d = to_f32(x[c]) - mean;
-        s.x += d * d;
+        s += d * d;
     }
-    const float rstd = rsqrtf(row_sum<true>(s, red, 1).x / a.n + a.eps);
+    const float rstd = rsqrtf(row_sum<true>(s, red, 1) / a.n + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[r] = mean;
         if (a.rstd) a.rstd[r] = rstd;
@@ -218,19 +382,54 @@ struct BwdArgs {
     float* part_b;
     long long rows, ldx, lddy, lddres, lddx;
     int cols;
-    float n;
+    int stages;
+    float inv_n;
+    int* status;
 };
 
-template <typename X, typename Y, bool VEC, bool BLOCK, int E>
-__global__ void __launch_bounds__(BLOCK ? 1024 / E : 256) k_ln_bwd(const BwdArgs a)
+template <typename X, typename Y, bool VEC, int CAP, int E>
+__global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(const BwdArgs a)
 {
-    __shared__ float2 red[2][32];
+    constexpr bool BLOCK = CAP > 0;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ RowSums red;
     __shared__ float comb[BLOCK ? 1 : 8][BLOCK ? 1 : 256];
+    __shared__ uint64_t bars[BLOCK ? 1 : 8][kRingStages];
+    __shared__ volatile int abort_flag;
+    const int G = BLOCK ? blockDim.x : 32, R = BLOCK ? 1 : blockDim.x / 32;
+    const int warp = threadIdx.x >> 5, group = BLOCK ? 0 : warp;
+    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols};
+    const long long first = (long long)blockIdx.x * R + group, step = (long long)gridDim.x * R;
+    const Part<VEC, X> x = {static_cast<const X*>(a.x), a.ldx, a.rows, a.cols};
+    const Part<VEC, Y> dy = {static_cast<const Y*>(a.dy), a.lddy, a.rows, a.cols};
+    const Part<VEC, X> dres = {static_cast<const X*>(a.dres), a.lddres, a.rows, a.cols};
+    const int room_x = Part<VEC, X>::room(a.cols), room_y = Part<VEC, Y>::room(a.cols);
+    const int room = room_x + room_y + (a.dres ? room_x : 0);
+    uint8_t* mine = ring + (size_t)group * a.stages * room;
+    uint64_t* bar = bars[group];
+    if (threadIdx.x == 0) abort_flag = 0;
+    if (c.t == 0) {
+        for (int s = 0; s < a.stages; ++s) mbar_init(&bar[s], 1);
+        fence_mbar_init();
+    }
+    clear(red);
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
-    const int G = BLOCK ? blockDim.x : 32, R = BLOCK ? 1 : blockDim.x / 32;
-    const int warp = threadIdx.x >> 5;
-    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols};
+    auto fetch = [&](long long r, int s) {  // by the group's first thread
+        if (r >= a.rows) return;
+        if (x.copied(r)) {
+            uint8_t* to = mine + s * room;
+            mbar_arrive_expect_tx(&bar[s], x.bytes(r) + dy.bytes(r) + (a.dres ? dres.bytes(r) : 0u));
+            bulk_load(to, x.from(r), x.bytes(r), &bar[s]);
+            bulk_load(to + room_x, dy.from(r), dy.bytes(r), &bar[s]);
+            if (a.dres) bulk_load(to + room_x + room_y, dres.from(r), dres.bytes(r), &bar[s]);
+        } else {
+            mbar_arrive(&bar[s]);
+        }
+    };
+    if (c.t == 0)
+        for (int s = 0; s < a.stages; ++s) fetch(first + s * step, s);
     float g[E][8], dg[E][8], db[E][8];
 #pragma unroll
     for (int k = 0; k < E; ++k) {
@@ -238,48 +437,60 @@ __global__ void __launch_bounds__(BLOCK ? 1024 / E : 256) k_ln_bwd(const BwdArgs
         for (int j = 0; j < 8; ++j) g[k][j] = 1.0f, dg[k][j] = db[k][j] = 0.0f;
         if (a.gamma) load_row<VEC>(a.gamma, c, k, 0.0f, g[k]);
     }
-    int slot = 0;
-    for (long long r = (long long)blockIdx.x * R + (BLOCK ? 0 : warp); r < a.rows; r += (long long)gridDim.x * R) {
-        const X* x = static_cast<const X*>(a.x) + r * a.ldx;
-        const Y* dy = static_cast<const Y*>(a.dy) + r * a.lddy;
-        const float mean = a.mean[r], rstd = a.rstd[r];
+    int slot = 0, s = 0, last = 0;
+    uint32_t phase = 0;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (first < a.rows) next_mean = a.mean[first], next_rstd = a.rstd[first];
+    for (long long r = first; r < a.rows; r += step) {
+        const float mean = next_mean, rstd = next_rstd;
+        if (r + step < a.rows) next_mean = a.mean[r + step], next_rstd = a.rstd[r + step];
+        const uint8_t* row = nullptr;
+        if (a.stages) {
+            mbar_wait(&bar[s], phase, &abort_flag, a.status);
+            if (x.copied(r)) row = mine + s * room;
+        }
         float xh[E][8], d[E][8];
-        float2 s = make_float2(0.0f, 0.0f);
+        float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            load_row<VEC>(x, c, k, mean, xh[k]);  // past the row's end: xhat = dy = 0
-            load_row<VEC>(dy, c, k, 0.0f, d[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < E; ++k)
+            x.load(c, row, r, k, mean, xh[k]);  // past the row's end: xhat = dy = 0
+            dy.load(c, row ? row + room_x : nullptr, r, k, 0.0f, d[k]);
+            float t1 = 0.0f, t2 = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 xh[k][j] = (xh[k][j] - mean) * rstd;
                 dg[k][j] += d[k][j] * xh[k][j];
                 db[k][j] += d[k][j];
                 d[k][j] *= g[k][j];
-                s.x += d[k][j];
-                s.y += d[k][j] * xh[k][j];
+                t1 += d[k][j];
+                t2 += d[k][j] * xh[k][j];
             }
-        if (!a.dx) continue;
-        s = row_sum<BLOCK>(s, red, slot);
-        slot ^= 1;
-        const float c1 = s.x / a.n, c2 = s.y / a.n;
-        X* dx = static_cast<X*>(a.dx) + r * a.lddx;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            float o[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = rstd * (d[k][j] - c1 - xh[k][j] * c2);
-            if (a.dres) {
-                float e[8];
-                load_row<VEC>(static_cast<const X*>(a.dres) + r * a.lddres, c, k, 0.0f, e);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] += e[j];
-            }
-            store_row<VEC>(dx, c, k, o);
+            s1 += t1;
+            s2 += t2;
         }
+        const float2 sum = row_sum2<BLOCK>(s1, s2, red, slot);
+        slot ^= 1;
+        // the whole group is done with the row before: its place takes the one `stages` rows on
+        if (a.stages && c.t == 0 && r != first) fetch(r + (a.stages - 1) * step, last);
+        if (a.dx) {
+            const float c1 = sum.x * a.inv_n, c2 = sum.y * a.inv_n;
+            X* dx = static_cast<X*>(a.dx) + r * a.lddx;
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                float e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] = 0.0f;
+                if (a.dres) dres.load(c, row ? row + room_x + room_y : nullptr, r, k, 0.0f, e);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] += rstd * (d[k][j] - c1 - xh[k][j] * c2);
+                store_row<VEC>(dx, c, k, e);
+            }
+        }
+        last = s;
+        if (++s == a.stages) { s = 0; phase ^= 1u; }
+        if (!BLOCK) __syncwarp();
     }
+    drain_after_failure(abort_flag);
     if (!a.part_g) return;
     float* pg = a.part_g + (long long)blockIdx.x * a.cols;
     float* pb = a.part_b + (long long)blockIdx.x * a.cols;
@@ -314,9 +525,11 @@ __global__ void __launch_bounds__(BLOCK ? 1024 / E : 256) k_ln_bwd(const BwdArgs
 template <typename X, typename Y>
 __global__ void __launch_bounds__(1024) k_ln_bwd_long(const BwdArgs a)
 {
-    __shared__ float2 red[2][32];
+    __shared__ RowSums red;
+    clear(red);
     pdl_wait();
     pdl_trigger();
+    __syncthreads();
     const long long r = blockIdx.x;
     const X* x = static_cast<const X*>(a.x) + r * a.ldx;
     const Y* dy = static_cast<const Y*>(a.dy) + r * a.lddy;
@@ -327,8 +540,8 @@ __global__ void __launch_bounds__(1024) k_ln_bwd_long(const BwdArgs a)
         s.x += d;
         s.y += d * (to_f32(x[c]) - mean) * rstd;
     }
-    s = row_sum<true>(s, red, 0);
-    const float c1 = s.x / a.n, c2 = s.y / a.n;
+    s = row_sum2<true>(s.x, s.y, red, 0);
+    const float c1 = s.x * a.inv_n, c2 = s.y * a.inv_n;
     const X* dres = a.dres ? static_cast<const X*>(a.dres) + r * a.lddres : nullptr;
     X* dx = static_cast<X*>(a.dx) + r * a.lddx;
     for (int c = threadIdx.x; c < a.cols; c += 1024) {
@@ -359,18 +572,34 @@ __global__ void __launch_bounds__(256) k_ln_cols_long(const BwdArgs a)
 
 // -------------------------------------------------------------------- host --
 
-constexpr int kWarpCols = 1024;       // a warp takes a row up to this length,
-constexpr int kFwdBlockCols = 32768;  // a block up to these (1024 threads x 32, 1024 x 8)
-constexpr int kBwdBlockCols = 8192;
+// A warp takes a row up to this length (16 elements a lane), a block up to
+// these: 512 threads of 16 (forward: 1024 of 32).
+constexpr int kWarpCols = 512;
+constexpr int kFwdBlockCols = 32768, kBwdBlockCols = 8192;
 
 // Threads of a block that share a row of `cols`, at e times 8 elements each.
 int block_threads(int cols, int e) { return (int)round_up((cols + 8 * e - 1) / (8 * e), 32); }
+
+// Blocks an SM holds: of eight warps with a row each, or of one row, where the
+// kernels' registers allow 768 threads (forward) and 512 (backward).
+int fwd_blocks_per_sm(int cols)
+{
+    if (cols <= kWarpCols) return 3;
+    const int threads = block_threads(cols, 2);
+    return threads > 256 ? 1 : 768 / threads < 8 ? 768 / threads : 8;
+}
+int bwd_blocks_per_sm(int cols)
+{
+    if (cols <= kWarpCols) return 2;
+    const int threads = block_threads(cols, 2);
+    return threads > 256 ? 1 : 512 / threads < 6 ? 512 / threads : 6;
+}
 
 // Blocks of the backward: each leaves a partial sum.
 int bwd_blocks(long long rows, int cols)
 {
     const int per = cols <= kWarpCols ? 8 : 1;
-    const long long want = (rows + per - 1) / per, most = 2ll * device_sm_count();
+    const long long want = (rows + per - 1) / per, most = (long long)bwd_blocks_per_sm(cols) * device_sm_count();
     return (int)(want < most ? want : most);
 }
 
@@ -379,52 +608,91 @@ bool rows16(const void* p, long long ld, int dt)
     return !p || ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (dt == SADMM_BF16 ? 2 : 4))) & 15) == 0;
 }
 
+constexpr int kMostRing = 212 * 1024;
+
+// Rows of the ring: what `blocks` CTAs an SM can hold, with one group or eight
+// (warps) a block, beside the kernels' static shared memory; none where a group
+// has one row, a row has no whole eight, or fewer than `least` fit.
+int ring_stages(long long rows, long long groups, int per_block, int blocks, int room, int cols, int least)
+{
+    if (rows <= groups || cols < 8) return 0;
+    int bytes = (224 / blocks - (per_block > 1 ? 10 : 3)) * 1024;
+    if (bytes > kMostRing) bytes = kMostRing;
+    int s = bytes / (room * per_block);
+    const long long most = (rows + groups - 1) / groups;
+    if (s > kRingStages) s = kRingStages;
+    if (s > most) s = (int)most;
+    return s < least ? 0 : s;
+}
+
+// Lets a kernel have the shared memory of its ring (once per device and kernel).
+template <typename K>
+bool allow_ring(K kern, bool (&done)[64])
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if (!done[dev])
+        done[dev] = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostRing) == cudaSuccess;
+    return done[dev];
+}
+
+template <typename X, typename Y, bool VEC, int CAP, int E>
+sadmm_status fwd_run(FwdArgs a, cudaStream_t s)
+{
+    static bool allowed[64];
+    auto kern = k_ln_fwd<X, Y, VEC, CAP, E>;
+    if (!allow_ring(kern, allowed)) return SADMM_ECUDA;
+    const int threads = CAP ? block_threads(a.cols, E) : 256, per = CAP ? 1 : 8;
+    const int blocks = fwd_blocks_per_sm(a.cols);
+    const long long want = (a.rows + per - 1) / per, most = (long long)blocks * device_sm_count();
+    const long long grid = want < most ? want : most;
+    const int room = Part<VEC, X>::room(a.cols);
+    a.stages = ring_stages(a.rows, grid * per, per, blocks, room, a.cols, 1);
+    return launch_pdl(kern, dim3((unsigned)grid), dim3(threads), (size_t)a.stages * room * per, s, a) == cudaSuccess
+               ? SADMM_OK
+               : SADMM_ECUDA;
+}
+
 template <typename X, typename Y, bool VEC>
 sadmm_status fwd(const FwdArgs& a, cudaStream_t s)
 {
-    cudaError_t e;
-    if (a.cols <= kWarpCols) {
-        const dim3 grid((unsigned)((a.rows + 7) / 8)), block(256);
-        if (a.cols <= 256)
-            e = launch_pdl(k_ln_fwd<X, Y, VEC, false, 1>, grid, block, 0, s, a);
-        else if (a.cols <= 512)
-            e = launch_pdl(k_ln_fwd<X, Y, VEC, false, 2>, grid, block, 0, s, a);
-        else
-            e = launch_pdl(k_ln_fwd<X, Y, VEC, false, 4>, grid, block, 0, s, a);
-    } else {
-        const dim3 grid((unsigned)a.rows);
-        if (a.cols <= 8192)
-            e = launch_pdl(k_ln_fwd<X, Y, VEC, true, 1>, grid, dim3(block_threads(a.cols, 1)), 0, s, a);
-        else if (a.cols <= 16384)
-            e = launch_pdl(k_ln_fwd<X, Y, VEC, true, 2>, grid, dim3(block_threads(a.cols, 2)), 0, s, a);
-        else if (a.cols <= kFwdBlockCols)
-            e = launch_pdl(k_ln_fwd<X, Y, VEC, true, 4>, grid, dim3(block_threads(a.cols, 4)), 0, s, a);
-        else
-            e = launch_pdl(k_ln_fwd_long<X, Y>, grid, dim3(1024), 0, s, a);
-    }
-    return e == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+    if (a.cols <= 256) return fwd_run<X, Y, VEC, 0, 1>(a, s);
+    if (a.cols <= kWarpCols) return fwd_run<X, Y, VEC, 0, 2>(a, s);
+    if (a.cols <= 4096) return fwd_run<X, Y, VEC, 256, 2>(a, s);
+    if (a.cols <= 8192) return fwd_run<X, Y, VEC, 512, 2>(a, s);
+    if (a.cols <= kFwdBlockCols) return fwd_run<X, Y, VEC, 1024, 4>(a, s);
+    return launch_pdl(k_ln_fwd_long<X, Y>, dim3((unsigned)a.rows), dim3(1024), 0, s, a) == cudaSuccess ? SADMM_OK
+                                                                                                        : SADMM_ECUDA;
+}
+
+template <typename X, typename Y, bool VEC, int CAP, int E>
+sadmm_status bwd_run(BwdArgs a, cudaStream_t s)
+{
+    static bool allowed[64];
+    auto kern = k_ln_bwd<X, Y, VEC, CAP, E>;
+    if (!allow_ring(kern, allowed)) return SADMM_ECUDA;
+    const int threads = CAP ? block_threads(a.cols, E) : 256, per = CAP ? 1 : 8;
+    const int grid = bwd_blocks(a.rows, a.cols);
+    const int room = Part<VEC, X>::room(a.cols) * (a.dres ? 2 : 1) + Part<VEC, Y>::room(a.cols);
+    a.stages = ring_stages(a.rows, (long long)grid * per, per, bwd_blocks_per_sm(a.cols), room, a.cols, 2);
+    return launch_pdl(kern, dim3((unsigned)grid), dim3(threads), (size_t)a.stages * room * per, s, a) == cudaSuccess
+               ? SADMM_OK
+               : SADMM_ECUDA;
 }
 
 template <typename X, typename Y, bool VEC>
 sadmm_status bwd(const BwdArgs& a, cudaStream_t s)
 {
-    cudaError_t e;
-    const dim3 grid((unsigned)bwd_blocks(a.rows, a.cols));
-    if (a.cols <= 256)
-        e = launch_pdl(k_ln_bwd<X, Y, VEC, false, 1>, grid, dim3(256), 0, s, a);
-    else if (a.cols <= 512)
-        e = launch_pdl(k_ln_bwd<X, Y, VEC, false, 2>, grid, dim3(256), 0, s, a);
-    else if (a.cols <= kWarpCols)
-        e = launch_pdl(k_ln_bwd<X, Y, VEC, false, 4>, grid, dim3(256), 0, s, a);
-    else if (a.cols <= kBwdBlockCols)
-        e = launch_pdl(k_ln_bwd<X, Y, VEC, true, 1>, grid, dim3(block_threads(a.cols, 1)), 0, s, a);
-    else {
-        e = cudaSuccess;
-        if (a.dx) e = launch_pdl(k_ln_bwd_long<X, Y>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
-        if (e == cudaSuccess && a.part_g)
-            e = launch_pdl(k_ln_cols_long<X, Y>, dim3((unsigned)((a.cols + 255) / 256), grid.x), dim3(256), 0, s, a);
-    }
-    return e == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+    if (a.cols <= 256) return bwd_run<X, Y, VEC, 0, 1>(a, s);
+    if (a.cols <= kWarpCols) return bwd_run<X, Y, VEC, 0, 2>(a, s);
+    if (a.cols <= 4096) return bwd_run<X, Y, VEC, 256, 2>(a, s);
+    if (a.cols <= kBwdBlockCols) return bwd_run<X, Y, VEC, 512, 2>(a, s);
+    cudaError_t err = cudaSuccess;
+    if (a.dx) err = launch_pdl(k_ln_bwd_long<X, Y>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+    if (err == cudaSuccess && a.part_g)
+        err = launch_pdl(k_ln_cols_long<X, Y>,
+                         dim3((unsigned)((a.cols + 255) / 256), (unsigned)bwd_blocks(a.rows, a.cols)), dim3(256), 0, s, a);
+    return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
 }
 
 }  // namespace
@@ -438,8 +706,8 @@ size_t layernorm_bwd_bytes(const sadmm_layernorm_bwd_args& a)
 sadmm_status launch_layernorm_fwd(const sadmm_layernorm_fwd_args& a, cudaStream_t s)
 {
     if (a.rows == 0) return SADMM_OK;
-    const FwdArgs f = {a.x, a.y, a.gamma, a.beta, a.mean, a.rstd, a.rows, a.ldx, a.ldy, a.cols, a.eps,
-                       (float)a.cols};
+    const FwdArgs f = {a.x, a.y, a.gamma, a.beta, a.mean, a.rstd, a.rows, a.ldx, a.ldy, a.cols, 0,
+                       a.eps, (float)a.cols, device_status_ptr()};
     const bool vec = rows16(a.x, a.ldx, a.xdt) && rows16(a.y, a.ldy, a.ydt) && rows16(a.gamma, 0, SADMM_FP32) &&
                      rows16(a.beta, 0, SADMM_FP32);
     if (a.xdt == SADMM_BF16) {
@@ -462,7 +730,7 @@ sadmm_status launch_layernorm_bwd(const sadmm_layernorm_bwd_args& a, void* ws, c
     float* pg = cols ? static_cast<float*>(ws) : nullptr;
     float* pb = cols ? pg + (size_t)blocks * (size_t)round_up(a.cols, 64) : nullptr;
     const BwdArgs b = {a.x, a.dy, a.dres, a.dx, a.gamma, a.mean, a.rstd, pg, pb, a.rows, a.ldx, a.lddy, a.lddres,
-                       a.lddx, a.cols, (float)a.cols};
+                       a.lddx, a.cols, 0, (float)(1.0 / a.cols), device_status_ptr()};
     const bool vec = rows16(a.x, a.ldx, a.xdt) && rows16(a.dy, a.lddy, a.dydt) && rows16(a.dres, a.lddres, a.xdt) &&
                      rows16(a.dx, a.lddx, a.xdt) && rows16(a.gamma, 0, SADMM_FP32);
     sadmm_status st;

@@ -16,280 +16,19 @@
 // tiles: the contraction is cut over the CTAs of a cluster, which leave their
 // sums in shared memory and add each other's up in rank order, so that results
 // do not depend on timing and no scratch memory is needed.
-#include <cuda.h>
-#include <cudaTypedefs.h>
-#include <string.h>
-
-#include "act.cuh"
-#include "common.cuh"
-#include "internal.h"
-#include "tgemm.cuh"
+#include "tgemm_dev.cuh"
 
 namespace sadmm {
-
-PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn();  // pack.cu
 
 namespace {
 
 constexpr int kThreads = 192;
-constexpr int kBox = 8192;        // one 64 x 64 bf16 box
-constexpr int kPTile = 2 * kBox;  // 128 rows x 64
 constexpr int kMaxStages = 8;
 constexpr int kMaxAccCols = 128;  // accumulator columns of a CTA (fp32 sums: 64 KB when cut over a cluster)
 
-// An output matrix as the epilogue stores it.  vec: 2 / 1 / 0 for rows on
-// 32-byte / 16-byte / other boundaries.
-struct Out {
-    void* p;
-    long long ld;
-    long long total;  // elements from p to the end of the last row
-    int bf16;
-    int vec;
-};
-
-struct TgArgs {
-    Out y, y2, res, z, u;
-    const float* bias;
-    const float* bias2;
-    long long m, n;        // output rows, columns
-    int act;
-    int mode;
-    int p_tiles;           // 128-row tiles of one product
-    int q_tiles;
-    int bn;                // rows of the Q side per tile (per half when gated)
-    int nk0, nk;           // 64-element contraction steps: of the first summand, of all
-    int splits, steps;     // CTAs per cluster, contraction steps of each
-    int stages;
-    int p_kmajor, q_kmajor;
-    uint32_t stage_bytes, q_off;
-    uint32_t acc_cols, tmem_cols;
-    uint32_t idesc;
-    int* status;
-};
-
-// ------------------------------------------------------------- device PTX --
-
-SADMM_DEV uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
-// Every thread of every CTA of the cluster calls it.
-SADMM_DEV void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-
-SADMM_DEV uint32_t map_rank(uint32_t saddr, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
-    return a;
-}
-
-SADMM_DEV float ld_cluster_f32(uint32_t a)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
-}
-
-// Waits for the 128 epilogue threads.
-SADMM_DEV void epi_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-
-// Shared-memory matrix descriptor of a row-contiguous (MN-major) operand held
-// as 64-row boxes of 64 contraction elements with the 128-byte swizzle: within
-// a box one contraction element is a 128-byte line of 64 rows, groups of 8
-// lines are 1024 bytes apart (stride offset), boxes of the next 64 rows follow
-// 8192 bytes on (leading offset).  16 contraction elements are 2048 bytes.
-SADMM_DEV uint64_t sdesc_mnmajor_sw128(uint32_t saddr)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(8192u >> 4) << 16;
-    d |= (uint64_t)(1024u >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-
-SADMM_DEV uint64_t sdesc(uint32_t saddr, int kmajor)
-{
-    return kmajor ? sdesc_kmajor_sw128(saddr) : sdesc_mnmajor_sw128(saddr);
-}
-
-// ---------------------------------------------------------------- epilogue --
-
-SADMM_DEV void st_v8(void* p, const uint32_t (&w)[8])
-{
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]),
-                 "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-}
-
-SADMM_DEV uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// v[0..15] to row r, columns c .. c+15 of o; columns at or past n are skipped.
-SADMM_DEV void store16(const Out& o, long long r, long long c, long long n, const float (&v)[16], int* status)
-{
-    const long long at = r * o.ld + c;
-    if (c + 16 <= n && o.vec && dbg_in(at, o.total, status) && dbg_in(at + 15, o.total, status)) {
-        if (o.bf16) {
-            __nv_bfloat16* p = static_cast<__nv_bfloat16*>(o.p) + at;
-            uint32_t w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-            if (o.vec == 2) {
-                st_v8(p, w);
-            } else {
-                reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            }
-        } else {
-            float* p = static_cast<float*>(o.p) + at;
-            if (o.vec == 2) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * h + j]);
-                    st_v8(p + 8 * h, w);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    reinterpret_cast<float4*>(p)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        if (c + j >= n || !dbg_in(at + j, o.total, status)) continue;
-        if (o.bf16)
-            static_cast<__nv_bfloat16*>(o.p)[at + j] = __float2bfloat16_rn(v[j]);
-        else
-            static_cast<float*>(o.p)[at + j] = v[j];
-    }
-}
-
-// v += row r, columns c .. c+15 of o.
-SADMM_DEV void add16(const Out& o, long long r, long long c, long long n, float (&v)[16], int* status)
-{
-    const long long at = r * o.ld + c;
-    if (c + 16 <= n && o.vec && dbg_in(at, o.total, status) && dbg_in(at + 15, o.total, status)) {
-        if (o.bf16) {
-            const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(o.p) + at);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 q = p[h];
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[8 * h + 2 * j] += __uint_as_float(w[j] << 16);
-                    v[8 * h + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
-                }
-            }
-        } else {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(o.p) + at);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 q = p[j];
-                v[4 * j] += q.x; v[4 * j + 1] += q.y; v[4 * j + 2] += q.z; v[4 * j + 3] += q.w;
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        if (c + j >= n || !dbg_in(at + j, o.total, status)) continue;
-        v[j] += o.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(o.p)[at + j])
-                       : static_cast<const float*>(o.p)[at + j];
-    }
-}
-
-SADMM_DEV void store1(const Out& o, long long r, long long c, float v, int* status)
-{
-    const long long at = r * o.ld + c;
-    if (!dbg_in(at, o.total, status)) return;
-    if (o.bf16)
-        static_cast<__nv_bfloat16*>(o.p)[at] = __float2bfloat16_rn(v);
-    else
-        static_cast<float*>(o.p)[at] = v;
-}
-
-SADMM_DEV float load1(const Out& o, long long r, long long c, int* status)
-{
-    const long long at = r * o.ld + c;
-    if (!dbg_in(at, o.total, status)) return 0.0f;
-    return o.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(o.p)[at]) : static_cast<const float*>(o.p)[at];
-}
-
-// Sixteen columns of one output row: sb / sb2 are the tile's biases in shared memory.
-template <bool GATED>
-SADMM_DEV void finish16(const TgArgs& a, const Out& y, long long r, long long c, float (&v)[16], float (&w)[16],
-                        const float* sb, const float* sb2)
-{
-#pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] += sb[j];
-    if (GATED) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] += sb2[j];
-        if (a.u.p) store16(a.u, r, c, a.n, w, a.status);
-    }
-    if (a.z.p) store16(a.z, r, c, a.n, v, a.status);
-    with_act(a.act, [&](auto tag) {
-        constexpr int A = decltype(tag)::value;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = act_f32<A>(v[j]);
-    });
-    if (GATED) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] *= w[j];
-    }
-    if (a.res.p) add16(a.res, r, c, a.n, v, a.status);
-    store16(y, r, c, a.n, v, a.status);
-}
-
-// One element.
-template <bool GATED>
-SADMM_DEV void finish1(const TgArgs& a, const Out& y, long long r, long long c, float v, float w, float b, float b2)
-{
-    v += b;
-    if (GATED) {
-        w += b2;
-        if (a.u.p) store1(a.u, r, c, w, a.status);
-    }
-    if (a.z.p) store1(a.z, r, c, v, a.status);
-    with_act(a.act, [&](auto tag) { v = act_f32<decltype(tag)::value>(v); });
-    if (GATED) v *= w;
-    if (a.res.p) v += load1(a.res, r, c, a.status);
-    store1(y, r, c, v, a.status);
-}
-
-// ------------------------------------------------------------------ kernel --
-
-// One operand's part of a stage: `rows` rows from row0, 64 contraction elements from k0.
-SADMM_DEV void load_part(uint8_t* dst, const CUtensorMap* map, uint64_t* bar, int kmajor, int rows, int row0, int k0)
-{
-    if (kmajor) {
-        tma_load_2d(dst, map, bar, k0, row0);
-    } else {
-        for (int j = 0; j * 64 < rows; ++j) tma_load_2d(dst + j * kBox, map, bar, row0 + 64 * j, k0);
-    }
-}
-
 template <bool SWAP, bool GATED>
-__global__ void __launch_bounds__(kThreads)
-    k_tgemm(const __grid_constant__ CUtensorMap p0, const __grid_constant__ CUtensorMap p1,
-            const __grid_constant__ CUtensorMap q0, const __grid_constant__ CUtensorMap q1,
-            const __grid_constant__ TgArgs a)
+__global__ void __launch_bounds__(kThreads, 2)
+    k_tgemm(const __grid_constant__ TgMaps maps, const __grid_constant__ TgArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -297,16 +36,16 @@ __global__ void __launch_bounds__(kThreads)
     __shared__ uint32_t tmem_holder;
     __shared__ volatile int abort_flag;
     __shared__ float s_bias[2 * kMaxAccCols];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;  // uniform
 
     const uint32_t rank = a.splits > 1 ? cluster_rank() : 0;
-    long long tile = blockIdx.x / a.splits;
-    const int pt = (int)(tile % a.p_tiles);
-    tile /= a.p_tiles;
-    const int qt = (int)(tile % a.q_tiles);
-    const int prob = (int)(tile / a.q_tiles);  // kTgPair: which product
+    int tile = (int)(blockIdx.x / (unsigned)a.splits), which = 0;
+    while (which + 1 < a.products && tile >= a.prod[which + 1].first) ++which;
+    const TgProduct& p = a.prod[which];
+    tile -= p.first;
+    const int qt = tile / p.p_tiles, pt = tile - qt * p.p_tiles;
     const int row0 = pt * 128, col0 = qt * a.bn;
-    const int k_begin = min((int)rank * a.steps, a.nk), k_end = min(k_begin + a.steps, a.nk);
+    const int k_begin = min((int)rank * p.steps, p.nk), k_end = min(k_begin + p.steps, p.nk);
     const int nk = k_end - k_begin;
 
     if (threadIdx.x == 0) {
@@ -332,7 +71,7 @@ __global__ void __launch_bounds__(kThreads)
 
     if (warp == 0) {
         if (lane == 0) {
-            const CUtensorMap* pa = (a.mode == kTgPair && prob) ? &p1 : &p0;
+            const CUtensorMap *p0 = &maps.map[p.pm], *q0 = &maps.map[p.qm];
             int issued = 0, s = 0;
             uint32_t phase = 0;
             for (int i = 0; i < nk; ++i) {
@@ -340,13 +79,13 @@ __global__ void __launch_bounds__(kThreads)
                 uint8_t* st = smem + (size_t)s * a.stage_bytes;
                 mbar_arrive_expect_tx(&full[s], a.stage_bytes);
                 int k = k_begin + i;
-                const bool second = a.mode == kTgSum && k >= a.nk0;
-                if (second) k -= a.nk0;
-                load_part(st, second ? &p1 : pa, &full[s], a.p_kmajor, 128, row0, k * 64);
-                if (GATED && SWAP) load_part(st + kPTile, &p1, &full[s], a.p_kmajor, 128, row0, k * 64);
+                const int second = k >= p.nk0;  // of a sum
+                if (second) k -= p.nk0;
+                load_part(st, p0 + second, &full[s], p.p_kmajor, 128, row0, k * 64);
+                if (GATED && SWAP) load_part(st + kPTile, p0 + 1, &full[s], p.p_kmajor, 128, row0, k * 64);
                 uint8_t* sq = st + a.q_off;
-                load_part(sq, second ? &q1 : &q0, &full[s], a.q_kmajor, a.bn, col0, k * 64);
-                if (GATED && !SWAP) load_part(sq + a.bn * 128, &q1, &full[s], a.q_kmajor, a.bn, col0, k * 64);
+                load_part(sq, q0 + second, &full[s], p.q_kmajor, a.bn, col0, k * 64);
+                if (GATED && !SWAP) load_part(sq + a.bn * 128, q0 + 1, &full[s], p.q_kmajor, a.bn, col0, k * 64);
                 ++issued;
                 if (++s == a.stages) { s = 0; phase ^= 1u; }
             }
@@ -359,7 +98,7 @@ __global__ void __launch_bounds__(kThreads)
         }
         __syncwarp();
     } else if (warp == 1) {
-        const uint32_t pstep = a.p_kmajor ? 2u : 128u, qstep = a.q_kmajor ? 2u : 128u;  // 16 elements, in 16 bytes
+        const uint32_t pstep = p.p_kmajor ? 2u : 128u, qstep = p.q_kmajor ? 2u : 128u;  // 16 elements, in 16 bytes
         bool ok = true;
         int s = 0;
         uint32_t phase = 0;
@@ -367,12 +106,12 @@ __global__ void __launch_bounds__(kThreads)
             if (!mbar_wait_warp(&full[s], phase, &abort_flag, a.status)) { ok = false; break; }
             tc_fence_after();
             const uint32_t st = smem_u32(smem + (size_t)s * a.stage_bytes);
-            const uint64_t pd = sdesc(st, a.p_kmajor), qd = sdesc(st + a.q_off, a.q_kmajor);
+            const uint64_t pd = sdesc(st, p.p_kmajor), qd = sdesc(st + a.q_off, p.q_kmajor);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                mma_bf16_ss_elect(tmem, pd + kk * pstep, qd + kk * qstep, a.idesc, (i | kk) != 0);
+                mma_bf16_ss_elect(tmem, pd + kk * pstep, qd + kk * qstep, p.idesc, (i | kk) != 0);
                 if (GATED && SWAP)
-                    mma_bf16_ss_elect(tmem + a.bn, pd + (kPTile >> 4) + kk * pstep, qd + kk * qstep, a.idesc,
+                    mma_bf16_ss_elect(tmem + a.bn, pd + (kPTile >> 4) + kk * pstep, qd + kk * qstep, p.idesc,
                                       (i | kk) != 0);
             }
             mma_commit_elect(&empty[s]);
@@ -398,8 +137,8 @@ __global__ void __launch_bounds__(kThreads)
         if (!SWAP) {
             for (int j = t; j < a.bn; j += 128) {
                 const long long c = col0 + j;
-                s_bias[j] = a.bias && c < a.n ? a.bias[c] : 0.0f;
-                if (GATED) s_bias[kMaxAccCols + j] = a.bias2 && c < a.n ? a.bias2[c] : 0.0f;
+                s_bias[j] = a.bias && c < p.n ? a.bias[c] : 0.0f;
+                if (GATED) s_bias[kMaxAccCols + j] = a.bias2 && c < p.n ? a.bias2[c] : 0.0f;
             }
             epi_sync();
         }
@@ -421,13 +160,12 @@ __global__ void __launch_bounds__(kThreads)
         cluster_sync();
     }
     if (warp >= 2 && ok) {
-        const Out& y = (a.mode == kTgPair && prob) ? a.y2 : a.y;
         const long long prow = (long long)row0 + trow;
         const uint32_t base = smem_u32(part) + 4u * (uint32_t)trow;
         if (SWAP) {
-            const float b = a.bias && prow < a.n ? a.bias[prow] : 0.0f;
-            const float b2 = GATED && a.bias2 && prow < a.n ? a.bias2[prow] : 0.0f;
-            const int cols = (int)min((long long)a.bn, a.m - col0);
+            const float b = a.bias && prow < p.n ? a.bias[prow] : 0.0f;
+            const float b2 = GATED && a.bias2 && prow < p.n ? a.bias2[prow] : 0.0f;
+            const int cols = (int)min((long long)a.bn, p.m - col0);
             if (a.splits > 1) {
                 for (int c = (int)rank; c < cols; c += a.splits) {
                     float v = 0.0f, w = 0.0f;
@@ -436,7 +174,7 @@ __global__ void __launch_bounds__(kThreads)
                         v += ld_cluster_f32(peer + (uint32_t)c * 512u);
                         if (GATED) w += ld_cluster_f32(peer + (uint32_t)(a.bn + c) * 512u);
                     }
-                    if (prow < a.n) finish1<GATED>(a, y, col0 + c, prow, v, w, b, b2);
+                    if (prow < p.n) finish1<GATED>(a, p, col0 + c, prow, v, w, b, b2);
                 }
             } else {
                 for (int c0 = 0; c0 < cols; c0 += 16) {
@@ -448,13 +186,13 @@ __global__ void __launch_bounds__(kThreads)
                     }
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (c0 + j < cols && prow < a.n)
-                            finish1<GATED>(a, y, col0 + c0 + j, prow, nk > 0 ? __uint_as_float(rv[j]) : 0.0f,
+                        if (c0 + j < cols && prow < p.n)
+                            finish1<GATED>(a, p, col0 + c0 + j, prow, nk > 0 ? __uint_as_float(rv[j]) : 0.0f,
                                            GATED && nk > 0 ? __uint_as_float(rw[j]) : 0.0f, b, b2);
                 }
             }
         } else {
-            const int cols = (int)min((long long)a.bn, a.n - col0);
+            const int cols = (int)min((long long)a.bn, p.n - col0);
             const int first = a.splits > 1 ? 16 * (int)rank : 0, step = 16 * a.splits;
             for (int c = first; c < cols; c += step) {
                 float v[16], w[16];
@@ -481,7 +219,7 @@ __global__ void __launch_bounds__(kThreads)
                         w[j] = GATED ? __uint_as_float(rw[j]) : 0.0f;
                     }
                 }
-                if (prow < a.m) finish16<GATED>(a, y, prow, col0 + c, v, w, s_bias + c, s_bias + kMaxAccCols + c);
+                if (prow < p.m) finish16<GATED>(a, p, prow, col0 + c, v, w, s_bias + c, s_bias + kMaxAccCols + c);
             }
         }
     }
@@ -496,42 +234,15 @@ __global__ void __launch_bounds__(kThreads)
 
 // -------------------------------------------------------------------- host --
 
-bool encode(CUtensorMap* map, const TgOperand& o, int rows_per_tile)
-{
-    PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode_fn();
-    if (!enc) return false;
-    memset(map, 0, sizeof(*map));
-    const cuuint64_t gdim[2] = {(cuuint64_t)(o.kmajor ? o.k : o.rows), (cuuint64_t)(o.kmajor ? o.rows : o.k)};
-    const cuuint64_t gstride[1] = {(cuuint64_t)o.ld * 2};
-    const cuuint32_t box[2] = {64u, o.kmajor ? (cuuint32_t)rows_per_tile : 64u};
-    const cuuint32_t estride[2] = {1u, 1u};
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(o.p), gdim, gstride, box, estride,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-Out make_out(const TgMatrix& m, long long rows, long long cols)
-{
-    Out o;
-    const long long es = m.dt == SADMM_BF16 ? 2 : 4;
-    o.p = m.p;
-    o.ld = m.ld;
-    o.total = (rows - 1) * m.ld + cols;
-    o.bf16 = m.dt == SADMM_BF16;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(m.p) | (uintptr_t)(m.ld * es);
-    o.vec = at % 32 == 0 ? 2 : at % 16 == 0 ? 1 : 0;
-    return o;
-}
-
 template <bool SWAP, bool GATED>
-sadmm_status run(const CUtensorMap (&map)[4], const TgArgs& a, size_t smem, long long ctas, cudaStream_t s)
+sadmm_status run(const TgMaps& maps, const TgArgs& a, size_t smem, cudaStream_t s)
 {
     static bool configured[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
     auto kern = k_tgemm<SWAP, GATED>;
     if (!configured[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess)
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 112 * 1024) != cudaSuccess)
             return SADMM_ECUDA;
         configured[dev] = true;
     }
@@ -543,84 +254,127 @@ sadmm_status run(const CUtensorMap (&map)[4], const TgArgs& a, size_t smem, long
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.gridDim = dim3((unsigned)a.tiles * (unsigned)a.splits);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = a.splits > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, map[0], map[1], map[2], map[3], a) == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+    return cudaLaunchKernelEx(&cfg, kern, maps, a) == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
 }
 
-}  // namespace
+// Weights on the 128-row side, tokens on the other: products of few rows.
+bool swapped(const TgProblem& t) { return t.m <= 64 && t.n > t.m; }
 
-sadmm_status launch_tgemm(const TgProblem& t, cudaStream_t s)
+// Rows of the Q side per tile (per half when gated).
+int tile_width(const TgProblem* t, int count)
 {
-    const bool gated = t.mode == kTgGated;
-    const bool swap = t.m <= 64 && t.b[0].rows > t.m && t.mode != kTgPair;
-    const TgOperand* P = swap ? t.b : t.a;
-    const TgOperand* Q = swap ? t.a : t.b;
-    const long long p_rows = swap ? t.n : t.m, q_rows = swap ? t.m : t.n;
-    TgArgs a;
-    memset(&a, 0, sizeof(a));
-    a.m = t.m;
-    a.n = t.n;
-    a.bias = t.bias;
-    a.bias2 = t.bias2;
-    a.act = t.act;
-    a.mode = t.mode;
-    a.y = make_out(t.y, t.m, t.n);
-    if (t.mode == kTgPair) a.y2 = make_out(t.y2, t.m, t.n);
-    if (t.residual.p) a.res = make_out(t.residual, t.m, t.n);
-    if (t.z.p) a.z = make_out(t.z, t.m, t.n);
-    if (t.u.p) a.u = make_out(t.u, t.m, t.n);
-    a.p_kmajor = P[0].kmajor;
-    a.q_kmajor = Q[0].kmajor;
-    const int sm = device_sm_count();
-    int bn = gated ? 64 : 128;
-    if (swap) {
-        bn = 16;
-        while (bn < q_rows) bn <<= 1;
+    if (!swapped(*t)) return t->mode == kTgGated ? 64 : 128;
+    long long most = 0;
+    bool boxes = false;
+    for (int i = 0; i < count; ++i) {
+        if (t[i].m > most) most = t[i].m;
+        boxes = boxes || !t[i].a[0].kmajor;
     }
-    if (!a.q_kmajor && bn < 64) bn = 64;  // whole 64-row boxes
-    a.bn = bn;
-    a.p_tiles = (int)((p_rows + 127) / 128);
-    a.q_tiles = (int)((q_rows + bn - 1) / bn);
-    const long long products = t.mode == kTgPair ? 2 : 1;
-    const long long tiles = (long long)a.p_tiles * a.q_tiles * products;
-    a.nk0 = (int)((P[0].k + 63) / 64);
-    a.nk = t.mode == kTgSum ? 2 * a.nk0 : a.nk0;
-    // few tiles: each contraction is cut over 2, 4 or 8 CTAs (of at least four steps each)
+    int bn = boxes ? 64 : 16;  // row-contiguous operands come in whole 64-row boxes
+    while (bn < most) bn <<= 1;
+    return bn;
+}
+
+// CTAs that each contraction is cut over.  Few tiles: 2, 4 or 8 (of at least
+// four steps each); and an fp32 output's anyway, so that no sum inside the
+// tensor cores passes 2048 elements where 8 CTAs are enough for that (over 8192
+// elements one sum was 1.0e-6 off, four added up in fp32 0.25e-6).
+int cuts(const TgProblem* t, int count)
+{
+    const int bn = tile_width(t, count), sm = device_sm_count();
+    long long tiles = 0, nk = 0, longest = 0;
+    for (int i = 0; i < count; ++i) {
+        const long long steps = steps_of(t[i]);
+        const bool swap = swapped(t[i]);
+        tiles += ((swap ? t[i].n : t[i].m) + 127) / 128 * (((swap ? t[i].m : t[i].n) + bn - 1) / bn);
+        if (steps > nk) nk = steps;
+        if (t[i].y.dt == SADMM_FP32 && steps > longest) longest = steps;
+    }
     int splits = 1;
-    while (splits < 8 && tiles * splits * 2 <= 2 * sm && a.nk >= 8 * splits) splits *= 2;
+    while (splits < 8 && ((tiles * splits * 2 <= 2 * sm && nk >= 8 * splits) || longest > 32 * splits)) splits *= 2;
+    return splits;
+}
+
+sadmm_status launch_tiles(const TgProblem* t, int count, int splits, cudaStream_t s)
+{
+    const bool gated = t->mode == kTgGated, swap = swapped(*t);
+    TgArgs a;
+    TgMaps maps;
+    fill_common(a, t, count);
+    const int bn = tile_width(t, count);
+    a.bn = bn;
+    long long tiles = 0;
+    int next = 0;
+    const int n_mma = gated && !swap ? 2 * bn : bn;
+    for (int i = 0; i < count; ++i) {
+        TgProduct& p = a.prod[i];
+        const long long p_rows = swap ? p.n : p.m, q_rows = swap ? p.m : p.n;
+        p.p_tiles = (int)((p_rows + 127) / 128);
+        p.q_tiles = (int)((q_rows + bn - 1) / bn);
+        p.first = (int)tiles;
+        tiles += (long long)p.p_tiles * p.q_tiles;
+        if (tiles > 0x0fffffffll) return SADMM_EUNSUPPORTED;
+        if (!encode_product(maps, next, p, t[i], swap, 128, bn, i ? &a.prod[i - 1] : nullptr, i ? &t[i - 1] : nullptr))
+            return SADMM_ECUDA;
+        p.idesc = idesc_bf16_f32(128, n_mma) | (p.p_kmajor ? 0u : 1u << 15) | (p.q_kmajor ? 0u : 1u << 16);
+    }
+    a.tiles = (int)tiles;
     a.splits = splits;
-    a.steps = (a.nk + splits - 1) / splits;
+    int steps = 1;
+    for (int i = 0; i < count; ++i) {
+        a.prod[i].steps = (a.prod[i].nk + splits - 1) / splits;
+        if (a.prod[i].steps > steps) steps = a.prod[i].steps;
+    }
     a.acc_cols = (uint32_t)(gated ? 2 * bn : bn);
     uint32_t cols = 32;
     while (cols < a.acc_cols) cols <<= 1;
     a.tmem_cols = cols;
     a.q_off = gated && swap ? 2 * kPTile : kPTile;
-    a.stage_bytes = a.q_off + (uint32_t)(gated && !swap ? 2 * bn : bn) * 128u;
+    a.stage_bytes = a.q_off + (uint32_t)n_mma * 128u;
     // two CTAs an SM: one's epilogue beside the other's products
     a.stages = (int)(108 * 1024 / a.stage_bytes);
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    if (a.stages > a.steps) a.stages = a.steps;
+    if (a.stages > steps) a.stages = steps;
     size_t smem = (size_t)a.stages * a.stage_bytes;
     if (splits > 1 && smem < (size_t)a.acc_cols * 512) smem = (size_t)a.acc_cols * 512;
     smem += 1024;
-    const int n_mma = gated && !swap ? 2 * bn : bn;
-    a.idesc = idesc_bf16_f32(128, n_mma) | (a.p_kmajor ? 0u : 1u << 15) | (a.q_kmajor ? 0u : 1u << 16);
-    a.status = device_status_ptr();
-    if (tiles * splits > 0x7fffffffll) return SADMM_EUNSUPPORTED;
-    alignas(64) CUtensorMap map[4];
-    const bool p_two = t.mode == kTgSum || t.mode == kTgPair || (gated && swap);
-    const bool q_two = t.mode == kTgSum || (gated && !swap);
-    if (!encode(&map[0], P[0], 128) || !encode(&map[1], P[p_two ? 1 : 0], 128) || !encode(&map[2], Q[0], bn) ||
-        !encode(&map[3], Q[q_two ? 1 : 0], bn))
-        return SADMM_ECUDA;
-    const long long ctas = tiles * splits;
-    if (gated) return swap ? run<true, true>(map, a, smem, ctas, s) : run<false, true>(map, a, smem, ctas, s);
-    return swap ? run<true, false>(map, a, smem, ctas, s) : run<false, false>(map, a, smem, ctas, s);
+    if (gated) return swap ? run<true, true>(maps, a, smem, s) : run<false, true>(maps, a, smem, s);
+    return swap ? run<true, false>(maps, a, smem, s) : run<false, false>(maps, a, smem, s);
+}
+
+}  // namespace
+
+sadmm_status launch_tgemm(const TgProblem* all, int count, cudaStream_t s)
+{
+    for (int i = 1; i < count; ++i) {
+        if (swapped(all[i]) == swapped(all[0])) continue;
+        for (int j = 0; j < count; ++j) {
+            const sadmm_status st = launch_tgemm(all + j, 1, s);
+            if (st != SADMM_OK) return st;
+        }
+        return SADMM_OK;
+    }
+    TgProblem t[kTgProducts];
+    int wanted = 0;
+    for (int i = 0; i < count; ++i)
+        if (!all[i].skip) t[wanted++] = all[i];
+    if (!wanted) return SADMM_OK;
+    if (!swapped(all[0])) {
+        const bool gated = all->mode == kTgGated;
+        const TgPairChoice c = choose_tgemm_pair(all, count);
+        long long work = 0;  // steps of 128-row tiles
+        for (int i = 0; i < count; ++i)
+            work += (all[i].m + 127) / 128 * ((all[i].n + (gated ? 63 : 127)) / (gated ? 64 : 128)) * steps_of(all[i]);
+        if (c.cycles < work * 560 / device_sm_count() + 6000)
+            return launch_tgemm_pair(t, wanted, choose_tgemm_pair(t, wanted).bn, s);
+    }
+    return launch_tiles(t, wanted, cuts(all, count), s);
 }
 
 }  // namespace sadmm

@@ -28,21 +28,21 @@ struct TgMatrix {
 };
 
 enum TgMode {
-    kTgSingle = 0,   // C = A0 B0^T
-    kTgSum = 1,      // C = A0 B0^T + A1 B1^T (one contraction of twice the length)
-    kTgPair = 2,     // y = A0 B0^T, y2 = A1 B0^T (two products in one launch)
-    kTgGated = 3,    // g = A0 B0^T + bias, u = A0 B1^T + bias2, y = act(g) * u
+    kTgSingle = 0,   // y = A0 B0^T, finished by the epilogue
+    kTgSum = 1,      // y = A0 B0^T + A1 B1^T (one contraction of twice the length)
+    kTgGated = 2,    // g = A0 B0^T + bias, u = A0 B1^T + bias2, y = act(g) * u
 };
 
 struct TgProblem {
     int mode;
+    bool skip;             // not wanted: weighed in the choice of tiles and cuts (so that the others' bits do not
+                           // depend on it), then left out; its pointers are not looked at
     TgOperand a[2], b[2];
     long long m, n;        // output rows and columns
     const float* bias;     // [n] or NULL
     const float* bias2;    // kTgGated: u's bias
     int act;               // sadmm_act
     TgMatrix y;
-    TgMatrix y2;           // kTgPair: the second product's output
     TgMatrix residual;     // p NULL: none; type of y
     TgMatrix z;            // bf16 pre-activation (kTgGated: g), p NULL: not kept
     TgMatrix u;            // kTgGated: u, p NULL: not kept
@@ -54,7 +54,19 @@ inline bool tg_aligned(const void* p, long long ld)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 7) == 0;
 }
 
-// Runs a checked problem (m, n >= 1; k >= 1).
-sadmm_status launch_tgemm(const TgProblem& t, cudaStream_t s);
+// Runs one to three checked problems (m, n, k >= 1).  Several are products
+// without epilogue (kTgSingle or kTgSum; bias, residual, z and u not given, no
+// activation); they share launches where they can.
+sadmm_status launch_tgemm(const TgProblem* t, int count, cudaStream_t s);
+
+// The same by CTA pairs (tgemm_pair.cu) with tiles of 256 x bn, bn a multiple
+// of 64 up to 256; choose_tgemm_pair gives the width it takes and an estimate
+// of its cycles.
+struct TgPairChoice {
+    int bn;
+    long long cycles;
+};
+TgPairChoice choose_tgemm_pair(const TgProblem* t, int count);
+sadmm_status launch_tgemm_pair(const TgProblem* t, int count, int bn, cudaStream_t s);
 
 }  // namespace sadmm

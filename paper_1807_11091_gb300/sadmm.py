@@ -11,6 +11,7 @@ call raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -752,250 +753,66 @@ def pack_batch(convs, stream=None) -> None:
 # Tensors are [tokens][width] (or any leading shape that views as that) with a
 # contiguous last dimension; row strides are free.  What a call allocates for an
 # output of odd width are rows on 32-byte boundaries, so that the next call
-# reads them where they lie: such an output is a view of a wider buffer.
+# reads them where they lie: such an output is a view of a wider buffer.  A bad
+# argument raises TypeError or ValueError here, or SadmmError from the library.
+# The checks, outputs and scratch are those of csrc/torch_ffn.cpp, because on a
+# few tokens they are what a call costs.
 
-def _rows(t, name: str, cols: int = -1):
-    """(pointer, row stride, rows, columns) of t as a matrix.  The stride of a
-    single row is free and taken as its width's next multiple of 8."""
-    n = t.shape[-1]
-    if t.dim() != 2:
-        if t.dim() < 1:
-            raise TypeError(f"{name} needs a last dimension")
-        t = t.unsqueeze(0) if t.dim() == 1 else t.view(-1, n)
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    s0, s1 = t.stride()
-    if s1 != 1 and n > 1:
-        raise TypeError(f"{name}'s last dimension must be contiguous")
-    if cols >= 0 and n != cols:
-        raise ValueError(f"{name} is {n} wide, not {cols}")
-    rows = t.shape[0]
-    return t.data_ptr(), (s0 if rows > 1 else (n + 7) // 8 * 8), rows, n
+_ffn_module = None
 
 
-def _bf16_rows(t, name: str, rows: int = -1, cols: int = -1):
-    if t.dtype != _torch().bfloat16:
-        raise TypeError(f"{name} must be bf16, got {t.dtype}")
-    m = _rows(t, name, cols)
-    if rows >= 0 and m[2] != rows:
-        raise ValueError(f"{name} has {m[2]} rows, not {rows}")
-    return m
+def _ffn():
+    """The native binding of the functions below, built on first use."""
+    global _ffn_module
+    if _ffn_module is None:
+        load()
+        _torch()  # its libraries, which the binding links against
+        path = _build.build_torch_binding()
+        spec = importlib.util.spec_from_file_location("torch_ffn", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(library_path(), SadmmError)
+        _ffn_module = module
+    return _ffn_module
 
 
-def _typed_rows(t, name: str, rows: int, cols: int):
-    m = _rows(t, name, cols)
-    if rows >= 0 and m[2] != rows:
-        raise ValueError(f"{name} has {m[2]} rows, not {rows}")
-    return m + (_dt(t.dtype, name),)
-
-
-def _dt(dtype, name: str) -> int:
-    torch = _torch()
-    if dtype == torch.bfloat16:
-        return SADMM_BF16
-    if dtype == torch.float32:
-        return SADMM_FP32
-    raise TypeError(f"{name} must be bf16 or fp32, got {dtype}")
-
-
-def _vector(t, n: int, name: str) -> Optional[int]:
-    """The pointer of an fp32 vector of n elements, or None."""
-    if t is None:
-        return None
-    if t.dtype != _torch().float32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        raise TypeError(f"{name} must be a contiguous fp32 CUDA tensor of {n} elements")
-    return t.data_ptr()
-
-
-def _new_rows(rows: int, cols: int, dtype, device):
-    """An uninitialised [rows][cols] whose rows start on 32-byte boundaries."""
-    torch = _torch()
-    step = 16 if dtype == torch.bfloat16 else 8
-    if cols % step == 0:
-        return torch.empty((rows, cols), dtype=dtype, device=device)
-    return torch.empty((rows, (cols + step - 1) // step * step), dtype=dtype, device=device)[:, :cols]
-
-
-def _like_rows(w, dtype):
-    """An uninitialised matrix of w's shape and row stride."""
-    torch = _torch()
-    rows, cols = w.shape
-    ld = max(w.stride(0), cols) if rows > 1 else cols
-    if ld == cols:
-        return torch.empty((rows, cols), dtype=dtype, device=w.device)
-    return torch.empty((rows, ld), dtype=dtype, device=w.device)[:, :cols]
-
-
-def _shaped(t, like):
-    """t ([tokens][n]) with the leading dimensions of `like`."""
-    if like.dim() == 2:
-        return t
-    return t[0] if like.dim() == 1 else t.unflatten(0, like.shape[:-1])
-
-
-def _run_with_scratch(call, size, a, device, stream, where: str, keep=()):
-    """call(a, workspace, bytes, stream) with a workspace of size(a) bytes.  On a
-    stream other than torch's current one the workspace and the outputs in
-    `keep` are marked as used there, so that their memory is not handed out
-    before the kernels are done."""
-    torch = _torch()
-    nbytes = size(ctypes.byref(a)) if size is not None else 0
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    _check(call(ctypes.byref(a), _ptr(ws), nbytes, _stream(stream)), where)
-    _used_on(stream, (ws,) + tuple(keep))
-
-
-def _used_on(stream, tensors) -> None:
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-
-
-def _apart(*matrices) -> bool:
-    """Whether a product would copy one of these (pointer, stride, ...) first."""
-    bits = 0
-    for m in matrices:
-        bits |= m[0] | (m[1] << 1)
-    return (bits & 15) != 0
+def _handle(stream):
+    return None if stream is None else int(stream.cuda_stream)
 
 
 def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out_dtype=None, stats: bool = False, out=None, stream=None):
     """Runs sadmm_layernorm_fwd over the last dimension: y, or (y, mean, rstd) with `stats`."""
-    torch = _torch()
-    px, ldx, rows, cols = _rows(x, "x")
-    xdt = _dt(x.dtype, "x")
-    y = out if out is not None else _new_rows(rows, cols, out_dtype or x.dtype, x.device)
-    py, ldy, _, _, ydt = _typed_rows(y, "out", rows, cols)
-    mean = rstd = None
-    if stats:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
-    a = LayerNormFwdArgs(rows, cols, px, ldx, xdt, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, py,
-                         ldy, ydt, _ptr(mean), _ptr(rstd))
-    _check(load().sadmm_layernorm_fwd(ctypes.byref(a), _stream(stream)), "sadmm_layernorm_fwd")
-    _used_on(stream, (y, mean, rstd))
-    if out is None:
-        y = _shaped(y, x)
-    return (y, mean, rstd) if stats else y
+    return (_ffn_module or _ffn()).layer_norm(x, gamma, beta, eps, out_dtype, stats, out, _handle(stream))
 
 
 def layer_norm_backward(dy, x, mean, rstd, gamma=None, dres=None, want_dx: bool = True, want_dgamma: bool = True,
                         want_dbeta: bool = True, stream=None):
     """Runs sadmm_layernorm_bwd: (dx, dgamma, dbeta), None where not wanted.  dres
     (of x's type) is the gradient along the block's residual, added to dx."""
-    torch = _torch()
-    px, ldx, rows, cols = _rows(x, "x")
-    pdy, lddy, _, _, dydt = _typed_rows(dy, "dy", rows, cols)
-    xdt = _dt(x.dtype, "x")
-    pr, ldr = None, 0
-    if dres is not None:
-        pr, ldr, _, _, rdt = _typed_rows(dres, "dres", rows, cols)
-        if rdt != xdt:
-            raise TypeError("dres must be of x's type")
-    dx, pdx, lddx = None, None, 0
-    if want_dx:
-        dx = _new_rows(rows, cols, x.dtype, x.device)
-        pdx, lddx = dx.data_ptr(), (dx.stride(0) if rows > 1 else (cols + 7) // 8 * 8)
-    dgamma = torch.empty(cols, dtype=torch.float32, device=x.device) if want_dgamma else None
-    dbeta = torch.empty(cols, dtype=torch.float32, device=x.device) if want_dbeta else None
-    a = LayerNormBwdArgs(rows, cols, px, ldx, xdt, pdy, lddy, dydt, _vector(gamma, cols, "gamma"),
-                         _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), pr, ldr, pdx, lddx, _ptr(dgamma),
-                         _ptr(dbeta))
-    lib = load()
-    _run_with_scratch(lib.sadmm_layernorm_bwd, lib.sadmm_layernorm_bwd_workspace_size, a, x.device, stream,
-                      "sadmm_layernorm_bwd", (dx, dgamma, dbeta))
-    return (_shaped(dx, x) if want_dx else None), dgamma, dbeta
+    return (_ffn_module or _ffn()).layer_norm_backward(dy, x, mean, rstd, gamma, dres, want_dx, want_dgamma, want_dbeta,
+                                                       _handle(stream))
 
 
 def linear(x, W, bias=None, residual=None, act: int = SADMM_ACT_NONE, out_dtype=None, save: bool = False, out=None,
            stream=None):
     """Runs sadmm_linear_fwd: act(x W^T + bias) + residual, or that and the
-    pre-activation z (bf16) with `save`."""
-    torch = _torch()
-    mx = _bf16_rows(x, "x")
-    px, ldx, tokens, n_in = mx
-    mw = _bf16_rows(W, "W", cols=n_in)
-    pw, ldw, n_out, _ = mw
-    if out is not None:
-        y = out
-    else:
-        y = _new_rows(tokens, n_out, out_dtype or (residual.dtype if residual is not None else x.dtype), x.device)
-    py, ldy, _, _, ydt = _typed_rows(y, "out", tokens, n_out)
-    pr, ldr = None, 0
-    if residual is not None:
-        pr, ldr, _, _, rdt = _typed_rows(residual, "residual", tokens, n_out)
-        if rdt != ydt:
-            raise TypeError("the residual must be of the output's type")
-    z, pz, ldz = None, None, 0
-    if save:
-        z = _new_rows(tokens, n_out, torch.bfloat16, x.device)
-        pz, ldz = _rows(z, "z")[:2]
-    a = LinearFwdArgs(tokens, n_in, n_out, px, ldx, pw, ldw, _vector(bias, n_out, "bias"), pr, ldr, act, py, ldy, ydt,
-                      pz, ldz)
-    lib = load()
-    _run_with_scratch(lib.sadmm_linear_fwd, lib.sadmm_linear_fwd_workspace_size if _apart(mx, mw) else None, a,
-                      x.device, stream, "sadmm_linear_fwd", (y, z))
-    if out is None:
-        y = _shaped(y, x)
-    return (y, _shaped(z, x)) if save else y
+    pre-activation z (bf16) with `save`.  The output's type is out_dtype, the
+    residual's, or bf16."""
+    return (_ffn_module or _ffn()).linear(x, W, bias, residual, act, out_dtype, save, out, _handle(stream))
 
 
 def linear_backward(dy, x, W, z=None, act: int = SADMM_ACT_NONE, want_dx: bool = True, want_dw: bool = True,
                     want_db: bool = True, dx_dtype=None, dw_dtype=None, stream=None):
     """Runs sadmm_linear_bwd: (dx, dW, db), None where not wanted.  dx and dW are
     bf16 unless dx_dtype / dw_dtype say fp32; dW has W's row stride."""
-    torch = _torch()
-    pdy, lddy, tokens, n_out = _rows(dy, "dy")
-    dydt = _dt(dy.dtype, "dy")
-    px, ldx, _, n_in = _bf16_rows(x, "x", tokens)
-    pw, ldw, _, _ = _bf16_rows(W, "W", n_out, n_in)
-    pz, ldz = None, 0
-    if act != SADMM_ACT_NONE:
-        if z is None:
-            raise TypeError("the gradient of an activation needs z")
-        pz, ldz = _bf16_rows(z, "z", tokens, n_out)[:2]
-    dx, mdx = None, (None, 0, 0, 0, SADMM_BF16)
-    if want_dx:
-        dx = _new_rows(tokens, n_in, dx_dtype or torch.bfloat16, x.device)
-        mdx = _typed_rows(dx, "dx", tokens, n_in)
-    dw, mdw = None, (None, 0, 0, 0, SADMM_BF16)
-    if want_dw:
-        dw = _like_rows(W, dw_dtype or torch.bfloat16)
-        mdw = _typed_rows(dw, "dW", n_out, n_in)
-    db = torch.empty(n_out, dtype=torch.float32, device=x.device) if want_db else None
-    a = LinearBwdArgs(tokens, n_in, n_out, pdy, lddy, dydt, px, ldx, pw, ldw, pz, ldz, act, mdx[0], mdx[1], mdx[4],
-                      mdw[0], mdw[1], mdw[4], _ptr(db))
-    lib = load()
-    _run_with_scratch(lib.sadmm_linear_bwd, lib.sadmm_linear_bwd_workspace_size, a, x.device, stream,
-                      "sadmm_linear_bwd", (dx, dw, db))
-    return (_shaped(dx, x) if want_dx else None), dw, db
+    return (_ffn_module or _ffn()).linear_backward(dy, x, W, z, act, want_dx, want_dw, want_db, dx_dtype, dw_dtype,
+                                                   _handle(stream))
 
 
 def gated(x, Wg, Wu, bg=None, bu=None, act: int = SADMM_ACT_SILU, save: bool = False, out=None, stream=None):
     """Runs sadmm_gated_fwd: h = act(x Wg^T + bg) * (x Wu^T + bu) in bf16, or (h, g,
     u) with `save`, g and u the two products with their biases."""
-    torch = _torch()
-    mx = _bf16_rows(x, "x")
-    px, ldx, tokens, n_in = mx
-    mg = _bf16_rows(Wg, "Wg", cols=n_in)
-    n = mg[2]
-    mu = _bf16_rows(Wu, "Wu", n, n_in)
-    h = out if out is not None else _new_rows(tokens, n, torch.bfloat16, x.device)
-    ph, ldh = _bf16_rows(h, "out", tokens, n)[:2]
-    g = u = pg = pu = None
-    ldg = ldu = 0
-    if save:
-        g, u = _new_rows(tokens, n, torch.bfloat16, x.device), _new_rows(tokens, n, torch.bfloat16, x.device)
-        pg, ldg = _rows(g, "g")[:2]
-        pu, ldu = _rows(u, "u")[:2]
-    a = GatedFwdArgs(tokens, n_in, n, px, ldx, mg[0], mg[1], mu[0], mu[1], _vector(bg, n, "bg"), _vector(bu, n, "bu"),
-                     act, ph, ldh, pg, ldg, pu, ldu)
-    lib = load()
-    _run_with_scratch(lib.sadmm_gated_fwd, lib.sadmm_gated_fwd_workspace_size if _apart(mx, mg, mu) else None, a,
-                      x.device, stream, "sadmm_gated_fwd", (h, g, u))
-    if out is None:
-        h = _shaped(h, x)
-    return (h, _shaped(g, x), _shaped(u, x)) if save else h
+    return (_ffn_module or _ffn()).gated(x, Wg, Wu, bg, bu, act, save, out, _handle(stream))
 
 
 def gated_backward(dh, x, Wg, Wu, g, u, act: int = SADMM_ACT_SILU, want_dx: bool = True, want_dw: bool = True,
@@ -1003,29 +820,8 @@ def gated_backward(dh, x, Wg, Wu, g, u, act: int = SADMM_ACT_SILU, want_dx: bool
     """Runs sadmm_gated_bwd: (dx, dWg, dWu, dbg, dbu), None where not wanted.  dx and
     the weights' gradients are bf16 unless dx_dtype / dw_dtype say fp32; the
     latter have their weights' row strides."""
-    torch = _torch()
-    pdh, lddh, tokens, n = _bf16_rows(dh, "dh")
-    px, ldx, _, n_in = _bf16_rows(x, "x", tokens)
-    mwg, mwu = _bf16_rows(Wg, "Wg", n, n_in), _bf16_rows(Wu, "Wu", n, n_in)
-    mg, mu = _bf16_rows(g, "g", tokens, n), _bf16_rows(u, "u", tokens, n)
-    dx, mdx = None, (None, 0, 0, 0, SADMM_BF16)
-    if want_dx:
-        dx = _new_rows(tokens, n_in, dx_dtype or torch.bfloat16, x.device)
-        mdx = _typed_rows(dx, "dx", tokens, n_in)
-    dwg = dwu = None
-    mdg = mdu = (None, 0, 0, 0, SADMM_BF16)
-    if want_dw:
-        dwg, dwu = _like_rows(Wg, dw_dtype or torch.bfloat16), _like_rows(Wu, dw_dtype or torch.bfloat16)
-        mdg, mdu = _typed_rows(dwg, "dWg", n, n_in), _typed_rows(dwu, "dWu", n, n_in)
-    dbg = dbu = None
-    if want_db:
-        dbg, dbu = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
-    a = GatedBwdArgs(tokens, n_in, n, pdh, lddh, px, ldx, mwg[0], mwg[1], mwu[0], mwu[1], mg[0], mg[1], mu[0], mu[1],
-                     act, mdx[0], mdx[1], mdx[4], mdg[0], mdg[1], mdu[0], mdu[1], mdg[4], _ptr(dbg), _ptr(dbu))
-    lib = load()
-    _run_with_scratch(lib.sadmm_gated_bwd, lib.sadmm_gated_bwd_workspace_size, a, x.device, stream, "sadmm_gated_bwd",
-                      (dx, dwg, dwu, dbg, dbu))
-    return (_shaped(dx, x) if want_dx else None), dwg, dwu, dbg, dbu
+    return (_ffn_module or _ffn()).gated_backward(dh, x, Wg, Wu, g, u, act, want_dx, want_dw, want_db, dx_dtype,
+                                                  dw_dtype, _handle(stream))
 
 
 def device_status(stream=None) -> int:
