@@ -29,7 +29,7 @@ DEBUG_LIB = os.path.join(BUILD, "debug", "libsadmm.so")
 
 SOURCES = ["abi.cu", "project.cu", "pack.cu", "conv_fwd.cu", "conv_slab.cu", "admm.cu", "elements.cu", "gemm.cu",
            "bwd.cu", "bwd_slab.cu", "bwd_grid.cu", "conv_grid.cu", "sparse.cu", "abi_ffn.cu", "norm.cu", "linear.cu",
-           "tgemm.cu", "tgemm_pair.cu"]
+           "tgemm.cu", "tgemm_pair.cu", "few.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -64,6 +64,9 @@ SADMM_DEV int atom_add_acq_rel_gpu(int* p, int v)
 // completed and its memory is visible, so it comes before the first read of
 // anything an earlier kernel wrote.  pdl_trigger() lets the next kernel of the
 // stream be scheduled once every CTA of this one has issued it (or exited).
+// A kernel launched in clusters does not trigger: clusters of the next kernel
+// that were let in early, and waited, took the places of this one's that had
+// not started yet, and both stood still.
 // A kernel's completion means that of every kernel before it: each one waits,
 // at its start or (k_grid_conv's late_wait) at its end.
 SADMM_DEV void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -113,6 +116,65 @@ SADMM_DEV uint32_t tap_mask(int it0, int ih0, int iw0, int KT, int KH, int KW, i
     for (int kt = t_lo; kt < t_hi; ++kt)
         for (int kh = h_lo; kh < h_hi; ++kh) m |= cm << ((kt * KH + kh) * KW);
     return m;
+}
+
+// ----------------------------------------------------------------- cluster --
+
+SADMM_DEV uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+// Every thread of every CTA of the cluster calls it.  The warp's lanes come
+// together first: lanes that ran ahead of a branch into the barrier's wait keep
+// the others of their warp from ever arriving.
+SADMM_DEV void cluster_sync()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+SADMM_DEV uint32_t map_rank(uint32_t saddr, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
+    return a;
+}
+
+// N neighbouring floats of any CTA of the cluster (a from map_rank), or of this one.
+template <int N>
+SADMM_DEV void ld_cluster(uint32_t a, float (&v)[N])
+{
+    static_assert(N == 2 || N == 4, "8 or 16 bytes");
+    if constexpr (N == 4)
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                     : "r"(a)
+                     : "memory");
+    else
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(a) : "memory");
+}
+
+template <int N>
+SADMM_DEV void ld_own(uint32_t a, float (&v)[N])
+{
+    static_assert(N == 2 || N == 4, "8 or 16 bytes");
+    if constexpr (N == 4)
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                     : "r"(a)
+                     : "memory");
+    else
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(a) : "memory");
+}
+
+SADMM_DEV float ld_cluster_f32(uint32_t a)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
 }
 
 SADMM_DEV void raise_status(int* status, int code)
@@ -241,6 +303,14 @@ SADMM_DEV void tma_load_4d(void* dst, const void* tmap, uint64_t* bar, int c0, i
         " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
         "l"(tmap), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
+}
+
+// The box on its way into L2 only.  L2 is where every write of this GPU lands, so
+// this may run ahead of the kernel that writes the box.
+SADMM_DEV void tma_prefetch_2d(const void* tmap, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(tmap), "r"(c0), "r"(c1)
+                 : "memory");
 }
 
 SADMM_DEV void tma_prefetch_desc(const void* tmap)

@@ -172,10 +172,12 @@ sadmm_status launch_linear_fwd(const sadmm_linear_fwd_args& a, void* ws, cudaStr
 sadmm_status launch_linear_bwd(const sadmm_linear_bwd_args& a, void* ws, cudaStream_t s);
 sadmm_status launch_gated_fwd(const sadmm_gated_fwd_args& a, void* ws, cudaStream_t s);
 sadmm_status launch_gated_bwd(const sadmm_gated_bwd_args& a, void* ws, cudaStream_t s);
-// out[c] (out2[c]) = the sum of part[0 .. parts-1][c] (part2), in a fixed order.
-// part2 NULL: one sum; out / out2 NULL: not written.
-sadmm_status launch_colsum(const float* part, const float* part2, float* out, float* out2, long long cols, int parts,
-                           cudaStream_t s);
+
+// ---- feed-forward products of a few tokens (few.cu) ----
+bool few_linear(const sadmm_linear_fwd_args& a);  // whether they run there
+bool few_gated(const sadmm_gated_fwd_args& a);
+sadmm_status launch_few_linear(const sadmm_linear_fwd_args& a, cudaStream_t s);
+sadmm_status launch_few_gated(const sadmm_gated_fwd_args& a, cudaStream_t s);
 
 // ---- layer norm (norm.cu) ----
 size_t layernorm_bwd_bytes(const sadmm_layernorm_bwd_args& a);

@@ -3,9 +3,8 @@
 // h = act(x Wg^T + bg) * (x Wu^T + bu), with their backward passes.  The
 // products run in tgemm.cu; here are the passes around them:
 //   k_dact     dz = dy act'(z), or dg and du of the gated pair, rounded to bf16
-//              once for the tensor cores, and the bias gradients' partial sums
-//              (fp32, taken before that rounding)
-//   k_colsum   those partial sums added up in row-chunk order
+//              once for the tensor cores, and the bias gradients (fp32 sums,
+//              taken before that rounding)
 //   k_realign  a matrix whose rows do not start on 16-byte boundaries, copied
 //              to rows that do, which is what the tensor-memory accelerator reads
 #include <string.h>
@@ -22,59 +21,64 @@ using bf16 = __nv_bfloat16;
 
 // --------------------------------------------------------------- k_realign --
 
-// A thread writes 8 elements (16 bytes) of a row.  Inside a row they come from
-// the two aligned 16-byte words that hold them; at the row's ends one by one.
-__global__ void __launch_bounds__(256) k_realign(const bf16* __restrict__ src, long long ld, bf16* __restrict__ dst,
-                                                 long long ldd, long long rows, long long cols)
+struct Copies {
+    const bf16* src[3];
+    bf16* dst[3];
+    long long ld[3], ldd[3], rows[3];
+    int cols[3];
+};
+
+// Matrix blockIdx.y, a warp a row's 1024 elements (segment blockIdx.z), a lane 8
+// elements (16 bytes) at a time, all in flight together.  Inside
+// a row they come from the two aligned 16-byte words that hold them (funnel
+// shifts), at the row's ends one by one.
+__global__ void __launch_bounds__(256) k_realign(const Copies a)
 {
     pdl_wait();
     pdl_trigger();
-    const long long per = ldd >> 3, n = rows * per;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        const long long r = i / per, c = (i - r * per) * 8;
-        const bf16* p = src + r * ld + c;
-        const int off = (int)((reinterpret_cast<uintptr_t>(p) & 15) >> 1);  // elements past a 16-byte boundary
-        __align__(16) uint16_t e[8];
-        if (c >= off && c + 16 <= cols) {
-            const uint4* w = reinterpret_cast<const uint4*>(p - off);
-            const uint4 lo = __ldg(w), hi = off ? __ldg(w + 1) : lo;
-            const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const int m = blockIdx.y, lane = threadIdx.x & 31;
+    const int cols = a.cols[m], words = (int)(a.ldd[m] >> 3);
+    const long long step = (long long)gridDim.x * 8;
+    for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < a.rows[m]; r += step) {
+        const bf16* row = a.src[m] + r * a.ld[m];
+        uint4* to = reinterpret_cast<uint4*>(a.dst[m] + r * a.ldd[m]);
+        // elements of the row's first 16-byte word that lie before the row
+        const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) >> 1);
+        const uint4* from = reinterpret_cast<const uint4*>(row - off);
+        const int sh = (off & 1) * 16, w0 = off >> 1;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t a = 0, b = 0;  // words (off / 2) + j and the next
+        for (int k = 0; k < 4; ++k) {
+            const int i = (blockIdx.z * 4 + k) * 32 + lane;
+            if (i >= words) break;
+            const int c = i * 8;
+            uint4 o;
+            if (c >= off && c + 16 <= cols) {
+                const uint4 lo = __ldg(from + i), hi = __ldg(from + i + 1);
+                // words w0 .. w0 + 4 of the eight (w0 is the row's: the same for the warp)
+                uint32_t v0, v1, v2, v3, v4;
+                if (w0 == 0) v0 = lo.x, v1 = lo.y, v2 = lo.z, v3 = lo.w, v4 = hi.x;
+                else if (w0 == 1) v0 = lo.y, v1 = lo.z, v2 = lo.w, v3 = hi.x, v4 = hi.y;
+                else if (w0 == 2) v0 = lo.z, v1 = lo.w, v2 = hi.x, v3 = hi.y, v4 = hi.z;
+                else v0 = lo.w, v1 = hi.x, v2 = hi.y, v3 = hi.z, v4 = hi.w;
+                o = make_uint4(__funnelshift_r(v0, v1, sh), __funnelshift_r(v1, v2, sh), __funnelshift_r(v2, v3, sh),
+                               __funnelshift_r(v3, v4, sh));
+            } else {
+                uint32_t e[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (k == (off >> 1) + j) a = v[k];
-                    if (k == (off >> 1) + j + 1) b = v[k];
-                }
-                const uint32_t u = (off & 1) ? __funnelshift_r(a, b, 16) : a;
-                e[2 * j] = (uint16_t)(u & 0xffffu);
-                e[2 * j + 1] = (uint16_t)(u >> 16);
+                for (int j = 0; j < 8; ++j)
+                    e[j] = c + j < cols ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + j) : 0u;
+                o = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                e[j] = c + j < cols ? __ldg(reinterpret_cast<const unsigned short*>(p) + j) : (uint16_t)0;
+            to[i] = o;
         }
-        *reinterpret_cast<uint4*>(dst + r * ldd + c) = *reinterpret_cast<const uint4*>(e);
     }
-}
-
-sadmm_status realign(const void* src, long long ld, void* dst, long long ldd, long long rows, long long cols,
-                     cudaStream_t s)
-{
-    const long long n = rows * (ldd >> 3);
-    const long long blocks = (n + 255) / 256, most = (long long)device_sm_count() * 16;
-    return launch_pdl(k_realign, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s,
-                      static_cast<const bf16*>(src), ld, static_cast<bf16*>(dst), ldd, rows, cols) == cudaSuccess
-               ? SADMM_OK
-               : SADMM_ECUDA;
 }
 
 // ------------------------------------------------------------------ k_dact --
 
-constexpr int kStrip = 256;  // columns of a CTA: 32 lanes x 8
-constexpr int kWarps = 8;    // rows at a time
+constexpr int kStrip = 64;        // columns of a CTA
+constexpr int kDactThreads = 256;
+constexpr int kDactCluster = 8;   // CTAs that share a strip's column sums
 
 struct DactArgs {
     const void* dy;            // dy (dz = dy act'(z)) or dh, bf16 or fp32
@@ -82,166 +86,215 @@ struct DactArgs {
     const bf16* u;             // gated
     bf16* dz;                  // dz or dg; NULL: not written
     bf16* du;                  // gated
-    float* part;               // [chunks][cols] partial column sums (gated: dg's, then du's at part_u); NULL: none
-    float* part_u;
+    float* db;                 // column sums of dz (dg); NULL: none
+    float* dbu;                // of du
     long long lddy, ldz, ldu, ldd;
     long long rows, cols, chunk;
     int act;
-    int dy_fp32;
+    int cluster;               // CTAs of a strip, in one cluster where sums are wanted
+    int sums;
 };
 
-// Eight consecutive elements; those at or past `left` read as zero.
-SADMM_DEV void load8(const bf16* p, bool whole, long long left, float (&v)[8])
-{
-    if (whole) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[2 * j] = __uint_as_float(w[j] << 16);
-            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < left ? __bfloat162float(p[j]) : 0.0f;
-    }
-}
+// N consecutive elements, as they lie in memory.
+template <typename T, int N>
+struct Raw {
+    T e[N];
+};
 
-SADMM_DEV void load8(const float* p, bool whole, long long left, float (&v)[8])
+// Eight neighbours by 16-byte loads; one element otherwise.
+SADMM_DEV void load_raw(const bf16* p, Raw<bf16, 8>& r)
 {
-    if (whole) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < left ? p[j] : 0.0f;
-    }
+    *reinterpret_cast<uint4*>(r.e) = *reinterpret_cast<const uint4*>(p);
 }
-
-// Eight consecutive elements of a row of the (aligned, padded) scratch copy.
-SADMM_DEV void store8(bf16* p, const float (&v)[8])
+SADMM_DEV void load_raw(const float* p, Raw<float, 8>& r)
 {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<float4*>(r.e)[0] = reinterpret_cast<const float4*>(p)[0];
+    reinterpret_cast<float4*>(r.e)[1] = reinterpret_cast<const float4*>(p)[1];
 }
-
-// A CTA takes a strip of 256 columns and a chunk of rows, a warp a row at a
-// time, a lane 8 columns.  VEC: every matrix read starts its rows on 16-byte
-// boundaries.  The scratch copies always do, and end their rows with zeros up
-// to a multiple of 8 columns.
-template <bool GATED, bool VEC>
-__global__ void __launch_bounds__(kWarps * 32) k_dact(const DactArgs a)
+template <typename T>
+SADMM_DEV void load_raw(const T*, Raw<T, 2>&)  // (not called: two columns are loaded one by one)
 {
+}
+SADMM_DEV float f32(bf16 v) { return __bfloat162float(v); }
+SADMM_DEV float f32(float v) { return v; }
+
+// A CTA takes a strip of 64 columns and a chunk of rows.  VEC: every matrix read
+// starts its rows on 16-byte boundaries; a thread takes 8 neighbouring columns
+// (where all are inside) of every 32nd row, else columns 32 apart of every 8th,
+// so that a warp's loads are neighbours either way.  Several rows' loads are in
+// flight before the first is used (bound by memory).  The scratch copies start
+// rows on 16-byte boundaries, with zeros up to a multiple of 8 columns.  Column
+// sums: over a thread's rows in order, then the CTA's threads, then the
+// cluster's CTAs in rank order.
+template <bool GATED, bool VEC, typename DY>
+__global__ void __launch_bounds__(kDactThreads, GATED ? 3 : VEC ? 4 : 2) k_dact(const DactArgs a)
+{
+    constexpr int N = VEC ? 8 : 2;              // columns of a thread
+    constexpr int L = VEC ? 32 : 8;             // rows at a time
+    __shared__ float red[GATED ? 2 : 1][L][kStrip + 1];
+    __shared__ float csum[2][kStrip];
     pdl_wait();
-    pdl_trigger();
-    __shared__ float red[kWarps][kStrip];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long c = (long long)blockIdx.x * kStrip + lane * 8;
-    const long long r0 = (long long)blockIdx.y * a.chunk, r1 = min(r0 + a.chunk, a.rows);
-    const long long left = a.cols - c;
-    const bool whole = VEC && left >= 8;
-    float s[8], su[8];
+    if (!a.sums) pdl_trigger();  // (clusters do not: see common.cuh)
+    const int rank = (int)(blockIdx.x % (unsigned)a.cluster);
+    const long long c0 = (long long)(blockIdx.x / (unsigned)a.cluster) * kStrip;
+    const int cl = VEC ? threadIdx.x & 7 : threadIdx.x & 31, rl = VEC ? threadIdx.x >> 3 : threadIdx.x >> 5;
+    auto col = [&](int j) { return VEC ? cl * 8 + j : cl + 32 * j; };  // of the strip
+    const long long left = a.cols - c0;
+    const long long padded = ((a.cols + 7) & ~7ll) - c0;  // columns of the copies
+    const long long r0 = (long long)rank * a.chunk, r1 = min(r0 + a.chunk, a.rows);
+    const bool whole = VEC && cl * 8 + 8 <= left;
+    const DY* dy = static_cast<const DY*>(a.dy) + c0;
+    const bf16 *zp = a.z + c0, *up = a.u + c0;
+    float s[N], su[N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = su[j] = 0.0f;
-    if (left > 0) {
-        with_act(a.z ? a.act : SADMM_ACT_NONE, [&](auto tag) {
-            constexpr int A = decltype(tag)::value;
-#pragma unroll 2
-            for (long long r = r0 + warp; r < r1; r += kWarps) {
-                float d[8], z[8], u[8];
-                if (a.dy_fp32)
-                    load8(static_cast<const float*>(a.dy) + r * a.lddy + c, whole, left, d);
-                else
-                    load8(static_cast<const bf16*>(a.dy) + r * a.lddy + c, whole, left, d);
-                if (A != SADMM_ACT_NONE || GATED) load8(a.z + r * a.ldz + c, whole, left, z);
-                if (GATED) load8(a.u + r * a.ldu + c, whole, left, u);
+    for (int j = 0; j < N; ++j) s[j] = su[j] = 0.0f;
+
+    with_act(a.z ? a.act : SADMM_ACT_NONE, [&](auto tag) {
+        constexpr int A = decltype(tag)::value;
+        constexpr bool Z = GATED || A != SADMM_ACT_NONE;
+        constexpr int U = VEC ? (Z ? 2 : 4) : 8;  // turns whose loads are in flight together
+        // one row's values: sums them up and writes the copies
+        auto row = [&](long long r, const Raw<DY, N>& rd, const Raw<bf16, N>& rz, const Raw<bf16, N>& ru) {
+            float d[N], e[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                d[j] = f32(rd.e[j]);
+                float act = 0.0f, slope = 1.0f;
+                if (Z) act_slope_f32<A>(f32(rz.e[j]), act, slope);
                 if (GATED) {
-                    float du[8];
+                    e[j] = d[j] * act;
+                    d[j] = d[j] * f32(ru.e[j]) * slope;
+                    su[j] += e[j];
+                } else if (A != SADMM_ACT_NONE) {
+                    d[j] *= slope;
+                }
+                s[j] += d[j];
+            }
+            if (VEC) {
+                if (a.dz && cl * 8 < left) {
+                    __align__(16) Raw<bf16, 8> o;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        du[j] = d[j] * act_f32<A>(z[j]);
-                        d[j] = d[j] * u[j] * dact_f32<A>(z[j]);
-                        s[j] += d[j];
-                        su[j] += du[j];
-                    }
-                    store8(a.du + r * a.ldd + c, du);
-                    store8(a.dz + r * a.ldd + c, d);
-                } else {
+                    for (int j = 0; j < N; ++j) o.e[j] = __float2bfloat16_rn(d[j]);
+                    *reinterpret_cast<uint4*>(a.dz + r * a.ldd + c0 + cl * 8) = *reinterpret_cast<const uint4*>(o.e);
+                    if (GATED) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        if (A != SADMM_ACT_NONE) d[j] *= dact_f32<A>(z[j]);
-                        s[j] += d[j];
+                        for (int j = 0; j < N; ++j) o.e[j] = __float2bfloat16_rn(e[j]);
+                        *reinterpret_cast<uint4*>(a.du + r * a.ldd + c0 + cl * 8) = *reinterpret_cast<const uint4*>(o.e);
                     }
-                    if (a.dz) store8(a.dz + r * a.ldd + c, d);
+                }
+            } else if (a.dz) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (col(j) < padded) {
+                        a.dz[r * a.ldd + c0 + col(j)] = __float2bfloat16_rn(d[j]);
+                        if (GATED) a.du[r * a.ldd + c0 + col(j)] = __float2bfloat16_rn(e[j]);
+                    }
+            }
+        };
+        auto load = [&](auto inside, long long r, Raw<DY, N>& rd, Raw<bf16, N>& rz, Raw<bf16, N>& ru) {
+            if constexpr (decltype(inside)::value) {
+                load_raw(dy + r * a.lddy + cl * 8, rd);
+                if (Z) load_raw(zp + r * a.ldz + cl * 8, rz);
+                if (GATED) load_raw(up + r * a.ldu + cl * 8, ru);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const bool in = col(j) < left;  // past the end: zeros
+                    rd.e[j] = in ? dy[r * a.lddy + col(j)] : DY(0.0f);
+                    if (Z) rz.e[j] = in ? zp[r * a.ldz + col(j)] : bf16(0.0f);
+                    if (GATED) ru.e[j] = in ? up[r * a.ldu + col(j)] : bf16(0.0f);
                 }
             }
-        });
+        };
+        // (the choice outside the loop: inside it the loads of several rows would not be in flight together)
+        auto rows = [&](auto inside) {
+            long long r = r0 + rl;
+            for (; r + (U - 1) * L < r1; r += U * L) {
+                __align__(16) Raw<DY, N> rd[U];
+                __align__(16) Raw<bf16, N> rz[U], ru[U];
+#pragma unroll
+                for (int i = 0; i < U; ++i) load(inside, r + i * L, rd[i], rz[i], ru[i]);
+#pragma unroll
+                for (int i = 0; i < U; ++i) row(r + i * L, rd[i], rz[i], ru[i]);
+            }
+            for (; r < r1; r += L) {
+                __align__(16) Raw<DY, N> rd;
+                __align__(16) Raw<bf16, N> rz, ru;
+                load(inside, r, rd, rz, ru);
+                row(r, rd, rz, ru);
+            }
+        };
+        if constexpr (VEC) {
+            if (whole)
+                rows(ActTag<1>());
+            else if (cl * 8 < left)
+                rows(ActTag<0>());
+        } else {
+            rows(ActTag<0>());
+        }
+    });
+    if (!a.sums) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        red[0][rl][col(j)] = s[j];
+        if (GATED) red[GATED ? 1 : 0][rl][col(j)] = su[j];
     }
-    if (!a.part) return;
-#pragma unroll
-    for (int half = 0; half < (GATED ? 2 : 1); ++half) {
-        if (half) __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) red[warp][j * 32 + lane] = half ? su[j] : s[j];
-        __syncthreads();
-        // thread t adds up column 8 (t % 32) + t / 32 of the strip
-        float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += red[w][threadIdx.x];
-        const long long col = (long long)blockIdx.x * kStrip + lane * 8 + warp;
-        if (col < a.cols) (half ? a.part_u : a.part)[(long long)blockIdx.y * a.cols + col] = v;
-    }
-}
-
-// db[c] = the sum of part[0 .. chunks-1][c], eight groups of chunks at a time.
-// blockIdx.y selects the second sum of the gated pair.
-__global__ void __launch_bounds__(256) k_colsum(const float* __restrict__ part, const float* __restrict__ part2,
-                                                float* __restrict__ out, float* __restrict__ out2, long long cols,
-                                                int chunks)
-{
-    pdl_wait();
-    pdl_trigger();
-    __shared__ float red[8][32];
-    const float* p = blockIdx.y ? part2 : part;
-    float* o = blockIdx.y ? out2 : out;
-    const int g = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long c = (long long)blockIdx.x * 32 + lane;
-    float v = 0.0f;
-    if (c < cols)
-        for (int k = g; k < chunks; k += 8) v += p[k * cols + c];
-    red[g][lane] = v;
     __syncthreads();
-    if (g == 0 && c < cols && o) {
-        for (int k = 1; k < 8; ++k) v += red[k][lane];
-        o[c] = v;
+    if (threadIdx.x < (GATED ? 2 : 1) * kStrip) {
+        const int which = threadIdx.x / kStrip, c = threadIdx.x % kStrip;
+        float v = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < L; ++i) v += red[which][i][c];
+        csum[which][c] = v;
     }
+    cluster_sync();
+    const int share = kStrip / a.cluster;  // columns that this CTA finishes
+    if ((int)threadIdx.x < (GATED ? 2 : 1) * share) {
+        const int which = threadIdx.x / share, c = rank * share + threadIdx.x % share;
+        float v = 0.0f;
+        for (int i = 0; i < a.cluster; ++i) v += ld_cluster_f32(map_rank(smem_u32(&csum[which][c]), (uint32_t)i));
+        float* out = which ? a.dbu : a.db;
+        if (out && c < left) out[c0 + c] = v;
+    }
+    cluster_sync();  // the others have read this CTA's sums
 }
 
-// Rows of a chunk: enough CTAs to fill the device, at most 128 partial sums a column.
-long long dact_chunk(long long rows)
+template <bool GATED, bool VEC, typename DY>
+sadmm_status run_dact(const DactArgs& a, cudaStream_t s)
 {
-    long long c = (rows + 127) / 128;
-    if (c < 64) c = 64;
-    return round_up(c, kWarps);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.cols + kStrip - 1) / kStrip) * (unsigned)a.cluster);
+    cfg.blockDim = dim3(kDactThreads);
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.sums ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_dact<GATED, VEC, DY>, a) == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
 }
-long long dact_chunks(long long rows) { return (rows + dact_chunk(rows) - 1) / dact_chunk(rows); }
 
-sadmm_status launch_dact(DactArgs a, bool gated, cudaStream_t s)
+sadmm_status launch_dact(DactArgs a, bool gated, bool fp32, cudaStream_t s)
 {
-    a.chunk = dact_chunk(a.rows);
-    const dim3 grid((unsigned)((a.cols + kStrip - 1) / kStrip), (unsigned)dact_chunks(a.rows));
-    bool vec = (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0 && a.lddy % (a.dy_fp32 ? 4 : 8) == 0;
+    a.sums = a.db || a.dbu;
+    // with sums at most a cluster's CTAs share a strip's rows, of at least 32 each; without, chunks of 128
+    if (a.sums) {
+        a.cluster = 1;
+        while (a.cluster < kDactCluster && a.rows > 32ll * a.cluster) a.cluster *= 2;
+    } else {
+        a.cluster = (int)((a.rows + 127) / 128 < 4096 ? (a.rows + 127) / 128 : 4096);
+    }
+    a.chunk = (a.rows + a.cluster - 1) / a.cluster;
+    bool vec = (reinterpret_cast<uintptr_t>(a.dy) & 15) == 0 && a.lddy % (fp32 ? 4 : 8) == 0;
     if (a.z) vec = vec && tg_aligned(a.z, a.ldz);
     if (a.u) vec = vec && tg_aligned(a.u, a.ldu);
-    auto k = gated ? (vec ? k_dact<true, true> : k_dact<true, false>)
-                   : (vec ? k_dact<false, true> : k_dact<false, false>);
-    return launch_pdl(k, grid, dim3(kWarps * 32), 0, s, a) == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+    if (gated) return vec ? run_dact<true, true, bf16>(a, s) : run_dact<true, false, bf16>(a, s);
+    if (fp32) return vec ? run_dact<false, true, float>(a, s) : run_dact<false, false, float>(a, s);
+    return vec ? run_dact<false, true, bf16>(a, s) : run_dact<false, false, bf16>(a, s);
 }
 
 // ------------------------------------------------------------------- parts --
@@ -274,12 +327,35 @@ Source place(Scratch& w, const void* p, long long rows, long long cols, long lon
     }
     return o;
 }
-sadmm_status fill(Source& o, const void* p, long long rows, long long cols, long long ld, cudaStream_t s)
-{
-    if (tg_aligned(p, ld)) return SADMM_OK;
-    o.p = o.copy;
-    return realign(p, ld, o.copy, o.ld, rows, cols, s);
-}
+// The copies that a call's sources need, in one launch.
+struct Filler {
+    Copies c;
+    int n = 0;
+    long long rows = 0, widest = 0;
+    void add(Source& o, const void* p, long long rows_, long long cols, long long ld)
+    {
+        if (tg_aligned(p, ld)) return;
+        o.p = o.copy;
+        c.src[n] = static_cast<const bf16*>(p);
+        c.dst[n] = static_cast<bf16*>(o.copy);
+        c.ld[n] = ld;
+        c.ldd[n] = o.ld;
+        c.rows[n] = rows_;
+        c.cols[n] = (int)cols;
+        if (rows_ > rows) rows = rows_;
+        if (o.ld > widest) widest = o.ld;
+        ++n;
+    }
+    sadmm_status run(cudaStream_t s) const
+    {
+        if (!n) return SADMM_OK;
+        const long long blocks = (rows + 7) / 8, most = 8ll * device_sm_count();
+        const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)n, (unsigned)((widest + 1023) / 1024));
+        return launch_pdl(k_realign, grid, dim3(256), 0, s, c) == cudaSuccess
+                   ? SADMM_OK
+                   : SADMM_ECUDA;
+    }
+};
 
 TgOperand kmajor(const Source& o, long long rows, long long k) { return {o.p, rows, k, o.ld, true}; }
 TgOperand across(const Source& o, long long rows, long long k) { return {o.p, rows, k, o.ld, false}; }
@@ -298,13 +374,13 @@ struct LinearFwdPlan {
 };
 LinearFwdPlan plan_linear_fwd(const sadmm_linear_fwd_args& a, Scratch& w)
 {
+    if (few_linear(a)) return {};
     return {place(w, a.x, a.tokens, a.n_in, a.ldx), place(w, a.w, a.n_out, a.n_in, a.ldw)};
 }
 
 struct LinearBwdPlan {
     Source x, w, dz;
     bool own_dz;  // dz is formed in scratch (an activation, fp32 or unaligned dy)
-    float* part;
 };
 LinearBwdPlan plan_linear_bwd(const sadmm_linear_bwd_args& a, Scratch& w)
 {
@@ -318,7 +394,6 @@ LinearBwdPlan plan_linear_bwd(const sadmm_linear_bwd_args& a, Scratch& w)
         p.dz.ld = round_up(a.n_out, 8);
         p.dz.p = p.dz.copy = w.take((size_t)a.tokens * (size_t)p.dz.ld * 2);
     }
-    if (a.db) p.part = static_cast<float*>(w.take((size_t)dact_chunks(a.tokens) * (size_t)a.n_out * 4));
     return p;
 }
 
@@ -327,13 +402,13 @@ struct GatedFwdPlan {
 };
 GatedFwdPlan plan_gated_fwd(const sadmm_gated_fwd_args& a, Scratch& w)
 {
+    if (few_gated(a)) return {};
     return {place(w, a.x, a.tokens, a.n_in, a.ldx), place(w, a.wg, a.n_hidden, a.n_in, a.ldwg),
             place(w, a.wu, a.n_hidden, a.n_in, a.ldwu)};
 }
 
 struct GatedBwdPlan {
     Source x, wg, wu, dg, du;
-    float *part_g, *part_u;
 };
 GatedBwdPlan plan_gated_bwd(const sadmm_gated_bwd_args& a, Scratch& w)
 {
@@ -348,24 +423,10 @@ GatedBwdPlan plan_gated_bwd(const sadmm_gated_bwd_args& a, Scratch& w)
     p.dg.ld = p.du.ld = ld;
     p.dg.p = p.dg.copy = w.take((size_t)a.tokens * (size_t)ld * 2);
     p.du.p = p.du.copy = w.take((size_t)a.tokens * (size_t)ld * 2);
-    if (a.dbg || a.dbu) {
-        const size_t bytes = (size_t)dact_chunks(a.tokens) * (size_t)a.n_hidden * 4;
-        p.part_g = static_cast<float*>(w.take(bytes));
-        p.part_u = static_cast<float*>(w.take(bytes));
-    }
     return p;
 }
 
 }  // namespace
-
-sadmm_status launch_colsum(const float* part, const float* part2, float* out, float* out2, long long cols, int parts,
-                           cudaStream_t s)
-{
-    const dim3 grid((unsigned)((cols + 31) / 32), part2 ? 2u : 1u);
-    return launch_pdl(k_colsum, grid, dim3(256), 0, s, part, part2, out, out2, cols, parts) == cudaSuccess
-               ? SADMM_OK
-               : SADMM_ECUDA;
-}
 
 #define SADMM_TRY(call)                          \
     do {                                         \
@@ -404,10 +465,13 @@ size_t gated_bwd_bytes(const sadmm_gated_bwd_args& a)
 sadmm_status launch_linear_fwd(const sadmm_linear_fwd_args& a, void* ws, cudaStream_t s)
 {
     if (a.tokens == 0) return SADMM_OK;
+    if (few_linear(a)) return launch_few_linear(a, s);
     Scratch w = {static_cast<char*>(ws), 0};
     LinearFwdPlan p = plan_linear_fwd(a, w);
-    SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
-    SADMM_TRY(fill(p.w, a.w, a.n_out, a.n_in, a.ldw, s));
+    Filler f;
+    f.add(p.x, a.x, a.tokens, a.n_in, a.ldx);
+    f.add(p.w, a.w, a.n_out, a.n_in, a.ldw);
+    SADMM_TRY(f.run(s));
     TgProblem t;
     memset(&t, 0, sizeof(t));
     t.mode = kTgSingle;
@@ -436,19 +500,20 @@ sadmm_status launch_linear_bwd(const sadmm_linear_bwd_args& a, void* ws, cudaStr
         memset(&d, 0, sizeof(d));
         d.dy = a.dy;
         d.lddy = a.lddy;
-        d.dy_fp32 = a.dydt == SADMM_FP32;
         d.z = a.act == SADMM_ACT_NONE ? nullptr : static_cast<const bf16*>(a.z);
         d.ldz = a.ldz;
         d.dz = static_cast<bf16*>(p.dz.copy);
         d.ldd = p.dz.ld;
-        d.part = p.part;
+        d.db = a.db;
         d.rows = a.tokens;
         d.cols = a.n_out;
         d.act = a.act;
-        SADMM_TRY(launch_dact(d, false, s));
+        SADMM_TRY(launch_dact(d, false, a.dydt == SADMM_FP32, s));
     }
-    if (a.dx) SADMM_TRY(fill(p.w, a.w, a.n_out, a.n_in, a.ldw, s));
-    if (a.dw) SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
+    Filler f;
+    if (a.dx) f.add(p.w, a.w, a.n_out, a.n_in, a.ldw);
+    if (a.dw) f.add(p.x, a.x, a.tokens, a.n_in, a.ldx);
+    SADMM_TRY(f.run(s));
     TgProblem t[2];
     memset(t, 0, sizeof(t));
     t[0].mode = t[1].mode = kTgSingle;
@@ -464,18 +529,20 @@ sadmm_status launch_linear_bwd(const sadmm_linear_bwd_args& a, void* ws, cudaStr
     t[1].y = {a.dw, a.lddw, a.dwdt};
     t[1].skip = !a.dw;
     SADMM_TRY(launch_tgemm(t, 2, s));
-    if (a.db) SADMM_TRY(launch_colsum(p.part, nullptr, a.db, nullptr, a.n_out, (int)dact_chunks(a.tokens), s));
     return SADMM_OK;
 }
 
 sadmm_status launch_gated_fwd(const sadmm_gated_fwd_args& a, void* ws, cudaStream_t s)
 {
     if (a.tokens == 0) return SADMM_OK;
+    if (few_gated(a)) return launch_few_gated(a, s);
     Scratch w = {static_cast<char*>(ws), 0};
     GatedFwdPlan p = plan_gated_fwd(a, w);
-    SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
-    SADMM_TRY(fill(p.wg, a.wg, a.n_hidden, a.n_in, a.ldwg, s));
-    SADMM_TRY(fill(p.wu, a.wu, a.n_hidden, a.n_in, a.ldwu, s));
+    Filler f;
+    f.add(p.x, a.x, a.tokens, a.n_in, a.ldx);
+    f.add(p.wg, a.wg, a.n_hidden, a.n_in, a.ldwg);
+    f.add(p.wu, a.wu, a.n_hidden, a.n_in, a.ldwu);
+    SADMM_TRY(f.run(s));
     TgProblem t;
     memset(&t, 0, sizeof(t));
     t.mode = kTgGated;
@@ -514,17 +581,19 @@ sadmm_status launch_gated_bwd(const sadmm_gated_bwd_args& a, void* ws, cudaStrea
     d.dz = static_cast<bf16*>(p.dg.copy);
     d.du = static_cast<bf16*>(p.du.copy);
     d.ldd = p.dg.ld;
-    d.part = p.part_g;
-    d.part_u = p.part_u;
+    d.db = a.dbg;
+    d.dbu = a.dbu;
     d.rows = a.tokens;
     d.cols = a.n_hidden;
     d.act = a.act;
-    SADMM_TRY(launch_dact(d, true, s));
+    SADMM_TRY(launch_dact(d, true, false, s));
+    Filler f;
     if (a.dx) {
-        SADMM_TRY(fill(p.wg, a.wg, a.n_hidden, a.n_in, a.ldwg, s));
-        SADMM_TRY(fill(p.wu, a.wu, a.n_hidden, a.n_in, a.ldwu, s));
+        f.add(p.wg, a.wg, a.n_hidden, a.n_in, a.ldwg);
+        f.add(p.wu, a.wu, a.n_hidden, a.n_in, a.ldwu);
     }
-    if (a.dwg) SADMM_TRY(fill(p.x, a.x, a.tokens, a.n_in, a.ldx, s));
+    if (a.dwg) f.add(p.x, a.x, a.tokens, a.n_in, a.ldx);
+    SADMM_TRY(f.run(s));
     TgProblem t[3];
     memset(t, 0, sizeof(t));
     t[0].mode = kTgSum;
@@ -546,7 +615,6 @@ sadmm_status launch_gated_bwd(const sadmm_gated_bwd_args& a, void* ws, cudaStrea
         t[i].skip = !a.dwg;
     }
     SADMM_TRY(launch_tgemm(t, 3, s));
-    if (p.part_g) SADMM_TRY(launch_colsum(p.part_g, p.part_u, a.dbg, a.dbu, a.n_hidden, (int)dact_chunks(a.tokens), s));
     return SADMM_OK;
 }
 

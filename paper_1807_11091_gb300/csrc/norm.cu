@@ -13,7 +13,7 @@
 // frees a place), because the registers that would hold enough loads in flight
 // are not there.  The backward's threads own fixed columns, add up their shares
 // of dgamma and dbeta over the rows of their block in registers and leave one
-// partial sum per block, which a second kernel adds up in block order.  Rows
+// partial sum per block, which a second kernel adds up in a fixed order.  Rows
 // too long for registers are read again from cache instead.
 #include <string.h>
 
@@ -62,6 +62,34 @@ SADMM_DEV void store_vec(float* p, const float (&v)[8])
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// Two fp32 values in a 64-bit register, for the paired instructions.
+SADMM_DEV unsigned long long pair(float lo, float hi)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+SADMM_DEV float low(unsigned long long v) { return __uint_as_float((uint32_t)v); }
+SADMM_DEV float high(unsigned long long v) { return __uint_as_float((uint32_t)(v >> 32)); }
+SADMM_DEV unsigned long long add2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+SADMM_DEV unsigned long long mul2(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+SADMM_DEV unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // A row over G threads, E times 8 elements each.  VEC: the matrices' rows start
 // on 16-byte boundaries and thread t's k-th eight are the neighbours from
 // column (k G + t) 8; otherwise element j of them is column (8 k + j) G + t, so
@@ -69,6 +97,8 @@ SADMM_DEV void store_vec(float* p, const float (&v)[8])
 template <bool VEC>
 struct Cols {
     int g, t, cols;
+    // Whether element (k, j) is inside the row.
+    SADMM_DEV bool in(int k, int j) const { return at(k, j) < cols; }
     SADMM_DEV int at(int k, int j) const { return VEC ? (k * g + t) * 8 + j : (8 * k + j) * g + t; }
     SADMM_DEV bool whole(int k) const { return VEC && at(k, 0) + 8 <= cols; }
 };
@@ -388,7 +418,7 @@ struct BwdArgs {
 };
 
 template <typename X, typename Y, bool VEC, int CAP, int E>
-__global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(const BwdArgs a)
+__global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 1 ? 3 : 2) k_ln_bwd(const BwdArgs a)
 {
     constexpr bool BLOCK = CAP > 0;
     extern __shared__ __align__(128) uint8_t ring[];
@@ -430,12 +460,15 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(
     };
     if (c.t == 0)
         for (int s = 0; s < a.stages; ++s) fetch(first + s * step, s);
-    float g[E][8], dg[E][8], db[E][8];
+    unsigned long long g[E][4], dg[E][4], db[E][4];
 #pragma unroll
     for (int k = 0; k < E; ++k) {
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[k][j] = 1.0f, dg[k][j] = db[k][j] = 0.0f;
-        if (a.gamma) load_row<VEC>(a.gamma, c, k, 0.0f, g[k]);
+        for (int j = 0; j < 8; ++j) v[j] = 1.0f;
+        if (a.gamma) load_row<VEC>(a.gamma, c, k, 0.0f, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) g[k][j] = pair(v[2 * j], v[2 * j + 1]), dg[k][j] = db[k][j] = 0;
     }
     int slot = 0, s = 0, last = 0;
     uint32_t phase = 0;
@@ -449,31 +482,33 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(
             mbar_wait(&bar[s], phase, &abort_flag, a.status);
             if (x.copied(r)) row = mine + s * room;
         }
-        float xh[E][8], d[E][8];
-        float s1 = 0.0f, s2 = 0.0f;
+        // pairs of neighbouring elements (f32x2): half the instructions
+        unsigned long long xh[E][4], d[E][4], t1 = 0, t2 = 0;
+        const unsigned long long minus = pair(-mean, -mean), scale = pair(rstd, rstd);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            x.load(c, row, r, k, mean, xh[k]);  // past the row's end: xhat = dy = 0
-            dy.load(c, row ? row + room_x : nullptr, r, k, 0.0f, d[k]);
-            float t1 = 0.0f, t2 = 0.0f;
+            float xv[8], dv[8];
+            x.load(c, row, r, k, mean, xv);  // past the row's end: xhat = dy = 0
+            dy.load(c, row ? row + room_x : nullptr, r, k, 0.0f, dv);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                xh[k][j] = (xh[k][j] - mean) * rstd;
-                dg[k][j] += d[k][j] * xh[k][j];
-                db[k][j] += d[k][j];
-                d[k][j] *= g[k][j];
-                t1 += d[k][j];
-                t2 += d[k][j] * xh[k][j];
+            for (int j = 0; j < 4; ++j) {
+                xh[k][j] = mul2(add2(pair(xv[2 * j], xv[2 * j + 1]), minus), scale);
+                const unsigned long long v = pair(dv[2 * j], dv[2 * j + 1]);
+                dg[k][j] = fma2(v, xh[k][j], dg[k][j]);
+                db[k][j] = add2(db[k][j], v);
+                d[k][j] = mul2(v, g[k][j]);
+                t1 = add2(t1, d[k][j]);
+                t2 = fma2(d[k][j], xh[k][j], t2);
             }
-            s1 += t1;
-            s2 += t2;
         }
+        const float s1 = low(t1) + high(t1), s2 = low(t2) + high(t2);
         const float2 sum = row_sum2<BLOCK>(s1, s2, red, slot);
         slot ^= 1;
         // the whole group is done with the row before: its place takes the one `stages` rows on
         if (a.stages && c.t == 0 && r != first) fetch(r + (a.stages - 1) * step, last);
         if (a.dx) {
             const float c1 = sum.x * a.inv_n, c2 = sum.y * a.inv_n;
+            const unsigned long long m1 = pair(-c1, -c1), m2 = pair(-c2, -c2);
             X* dx = static_cast<X*>(a.dx) + r * a.lddx;
 #pragma unroll
             for (int k = 0; k < E; ++k) {
@@ -482,7 +517,12 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(
                 for (int j = 0; j < 8; ++j) e[j] = 0.0f;
                 if (a.dres) dres.load(c, row ? row + room_x + room_y : nullptr, r, k, 0.0f, e);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] += rstd * (d[k][j] - c1 - xh[k][j] * c2);
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned long long v =
+                        fma2(fma2(xh[k][j], m2, add2(d[k][j], m1)), scale, pair(e[2 * j], e[2 * j + 1]));
+                    e[2 * j] = low(v);
+                    e[2 * j + 1] = high(v);
+                }
                 store_row<VEC>(dx, c, k, e);
             }
         }
@@ -500,8 +540,8 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (c.at(k, j) < a.cols) {
-                    pg[c.at(k, j)] = dg[k][j];
-                    pb[c.at(k, j)] = db[k][j];
+                    pg[c.at(k, j)] = (j & 1) ? high(dg[k][j / 2]) : low(dg[k][j / 2]);
+                    pb[c.at(k, j)] = (j & 1) ? high(db[k][j / 2]) : low(db[k][j / 2]);
                 }
     } else {
         // the warps' sums added up in warp order, thread (j, lane) for element j of lane's eight
@@ -511,7 +551,10 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : 2) k_ln_bwd(
             for (int half = 0; half < 2; ++half) {
                 __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) comb[BLOCK ? 0 : warp][BLOCK ? 0 : j * 32 + c.t] = half ? db[k][j] : dg[k][j];
+                for (int j = 0; j < 8; ++j) {
+                    const unsigned long long v = half ? db[k][j / 2] : dg[k][j / 2];
+                    comb[BLOCK ? 0 : warp][BLOCK ? 0 : j * 32 + c.t] = (j & 1) ? high(v) : low(v);
+                }
                 __syncthreads();
                 float v = 0.0f;
                 for (int w = 0; w < R; ++w) v += comb[BLOCK ? 0 : w][BLOCK ? 0 : threadIdx.x];
@@ -570,12 +613,39 @@ __global__ void __launch_bounds__(256) k_ln_cols_long(const BwdArgs a)
     a.part_b[(long long)blockIdx.y * a.cols + c] = b;
 }
 
+// out[c] = the sum of part[0 .. parts-1][c], 32 groups of parts at a time, then
+// the groups in order.  blockIdx.y: dgamma or dbeta.
+__global__ void __launch_bounds__(1024) k_ln_sums(const float* __restrict__ part_g, const float* __restrict__ part_b,
+                                                  float* __restrict__ dgamma, float* __restrict__ dbeta, int cols,
+                                                  int parts)
+{
+    pdl_wait();
+    pdl_trigger();
+    __shared__ float red[32][33];
+    const float* p = blockIdx.y ? part_b : part_g;
+    float* o = blockIdx.y ? dbeta : dgamma;
+    if (!o) return;
+    const int g = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * 32 + lane;
+    float v = 0.0f;
+    if (c < cols) {
+#pragma unroll 16
+        for (int k = g; k < parts; k += 32) v += p[(size_t)k * cols + c];
+    }
+    red[g][lane] = v;
+    __syncthreads();
+    // warp g adds up column g of the 32
+    v = warp_sum(red[lane][g]);
+    if (lane == 0 && blockIdx.x * 32 + g < cols) o[blockIdx.x * 32 + g] = v;
+}
+
 // -------------------------------------------------------------------- host --
 
 // A warp takes a row up to this length (16 elements a lane), a block up to
 // these: 512 threads of 16 (forward: 1024 of 32).
 constexpr int kWarpCols = 512;
 constexpr int kFwdBlockCols = 32768, kBwdBlockCols = 8192;
+constexpr int kBwdShortCols = 2048;  // backward: up to here 8 elements a thread
 
 // Threads of a block that share a row of `cols`, at e times 8 elements each.
 int block_threads(int cols, int e) { return (int)round_up((cols + 8 * e - 1) / (8 * e), 32); }
@@ -591,8 +661,9 @@ int fwd_blocks_per_sm(int cols)
 int bwd_blocks_per_sm(int cols)
 {
     if (cols <= kWarpCols) return 2;
+    if (cols <= kBwdShortCols) return 768 / block_threads(cols, 1) < 4 ? 768 / block_threads(cols, 1) : 4;
     const int threads = block_threads(cols, 2);
-    return threads > 256 ? 1 : 512 / threads < 6 ? 512 / threads : 6;
+    return threads > 256 ? 1 : 512 / threads < 4 ? 512 / threads : 4;
 }
 
 // Blocks of the backward: each leaves a partial sum.
@@ -685,6 +756,7 @@ sadmm_status bwd(const BwdArgs& a, cudaStream_t s)
 {
     if (a.cols <= 256) return bwd_run<X, Y, VEC, 0, 1>(a, s);
     if (a.cols <= kWarpCols) return bwd_run<X, Y, VEC, 0, 2>(a, s);
+    if (a.cols <= kBwdShortCols) return bwd_run<X, Y, VEC, 256, 1>(a, s);
     if (a.cols <= 4096) return bwd_run<X, Y, VEC, 256, 2>(a, s);
     if (a.cols <= kBwdBlockCols) return bwd_run<X, Y, VEC, 512, 2>(a, s);
     cudaError_t err = cudaSuccess;
@@ -745,7 +817,10 @@ sadmm_status launch_layernorm_bwd(const sadmm_layernorm_bwd_args& a, void* ws, c
         st = vec ? bwd<float, float, true>(b, s) : bwd<float, float, false>(b, s);
     }
     if (st != SADMM_OK || !cols) return st;
-    return launch_colsum(pg, pb, a.dgamma, a.dbeta, a.cols, blocks, s);
+    return launch_pdl(k_ln_sums, dim3((unsigned)((a.cols + 31) / 32), 2), dim3(1024), 0, s, pg, pb, a.dgamma, a.dbeta,
+                      a.cols, blocks) == cudaSuccess
+               ? SADMM_OK
+               : SADMM_ECUDA;
 }
 
 }  // namespace sadmm

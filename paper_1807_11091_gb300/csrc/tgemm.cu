@@ -4,27 +4,29 @@
 // adds the residual in registers, so that nothing but the operator's own
 // outputs is written.
 //
-// One CTA per 128 x bn tile, six warps:
+// One CTA per 128 x bn tile, eight warps:
 //   warp 0      TMA producer: boxes of 64 contraction elements (K-major
 //               operand: 64 x rows; row-contiguous operand: 64 rows x 64) with
 //               the 128-byte swizzle
 //   warp 1      TMEM allocator and issuer of tcgen05.mma (M 128, N bn, K 16)
-//   warps 2-5   epilogue: tcgen05.ld, one lane per tile row
+//   warps 2-5   tcgen05.ld of the sums, one lane per tile row; then all eight
+//               warps finish the output's rows
 // The tile's 128 rows are the product's rows ("plain"), or, where there are few
 // of those, its columns ("swapped": weights on the 128-row side, tokens on the
-// bn side, so that a handful of tokens costs a handful of MMA columns).  Few
-// tiles: the contraction is cut over the CTAs of a cluster, which leave their
-// sums in shared memory and add each other's up in rank order, so that results
-// do not depend on timing and no scratch memory is needed.
+// bn side, so that a handful of tokens costs a handful of MMA columns).  Where
+// tiles are few or uneven the contraction is cut over the CTAs of a cluster,
+// which leave their sums in shared memory and add each other's up in rank
+// order, so that results do not depend on timing and no scratch memory is
+// needed.
 #include "tgemm_dev.cuh"
 
 namespace sadmm {
-
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kThreads = 256;
 constexpr int kMaxStages = 8;
-constexpr int kMaxAccCols = 128;  // accumulator columns of a CTA (fp32 sums: 64 KB when cut over a cluster)
+constexpr int kPrefetchSteps = 32;
+constexpr int kSwapStride = 132;  // floats of a staged row of 128, so that neither way in or out has bank conflicts
 
 template <bool SWAP, bool GATED>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -35,7 +37,6 @@ __global__ void __launch_bounds__(kThreads, 2)
     __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full, drain;
     __shared__ uint32_t tmem_holder;
     __shared__ volatile int abort_flag;
-    __shared__ float s_bias[2 * kMaxAccCols];
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;  // uniform
 
     const uint32_t rank = a.splits > 1 ? cluster_rank() : 0;
@@ -62,8 +63,25 @@ __global__ void __launch_bounds__(kThreads, 2)
         tmem_alloc(&tmem_holder, a.tmem_cols);
         tmem_relinquish();
     }
-    pdl_wait();  // nothing above reads global memory
-    pdl_trigger();
+    if (SWAP && warp == 0 && lane == 0) {
+        // the weights are what a few tokens wait for: on their way to L2 while the kernel before still runs
+        for (int i = 0; i < nk && i < kPrefetchSteps; ++i) {
+            int k = k_begin + i;
+            const int second = k >= p.nk0;
+            if (second) k -= p.nk0;
+            for (int half = 0; half < (GATED ? 2 : 1); ++half) {
+                const CUtensorMap* map = &maps.map[p.pm + second + half];
+                if (p.p_kmajor) {
+                    tma_prefetch_2d(map, k * 64, row0);
+                } else {
+                    tma_prefetch_2d(map, row0, k * 64);
+                    tma_prefetch_2d(map, row0 + 64, k * 64);
+                }
+            }
+        }
+    }
+    pdl_wait();  // nothing above reads what an earlier kernel may write
+    if (a.splits == 1) pdl_trigger();  // (clusters do not: see common.cuh)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -126,101 +144,98 @@ __global__ void __launch_bounds__(kThreads, 2)
         __syncwarp();
     }
 
-    // ---- epilogue: TMEM lane = tile row
-    const int q = warp & 3;
-    const int trow = q * 32 + lane;
-    const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
-    float* part = reinterpret_cast<float*>(smem);  // [accumulator column][128 rows], when the contraction is cut
-    bool ok = false;
-    if (warp >= 2) {
-        const int t = threadIdx.x - 64;
-        if (!SWAP) {
-            for (int j = t; j < a.bn; j += 128) {
-                const long long c = col0 + j;
-                s_bias[j] = a.bias && c < p.n ? a.bias[c] : 0.0f;
-                if (GATED) s_bias[kMaxAccCols + j] = a.bias2 && c < p.n ? a.bias2[c] : 0.0f;
-            }
-            epi_sync();
-        }
-        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full, 0, &abort_flag, a.status));
+    // ---- epilogue: the sums to shared memory as rows of the output, then every warp of the cluster's CTAs takes
+    // rows of them in turn, a lane N neighbouring columns, so that loads and stores are neighbours whatever the
+    // output's alignment
+    constexpr int N = !SWAP && GATED ? 2 : 4;
+    float* part = reinterpret_cast<float*>(smem);
+    const int live = (int)min((long long)(SWAP ? a.bn : 128), p.m - (SWAP ? col0 : row0));  // rows
+    const uint32_t stride = SWAP ? kSwapStride : a.acc_cols + 4;                             // floats of a staged row
+    const uint32_t u_off = SWAP ? (uint32_t)a.bn * kSwapStride : (uint32_t)a.bn;             // gated: from g to u
+    if (warp >= 2 && warp < 6 && __all_sync(0xffffffffu, mbar_wait(&acc_full, 0, &abort_flag, a.status))) {
+        const int q = warp & 3, trow = q * 32 + lane;
+        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
         tc_fence_after();
-    }
-    if (a.splits > 1) {
-        if (warp >= 2 && ok) {
-            for (uint32_t c = 0; c < a.acc_cols; c += 16) {
-                uint32_t r[16];
-                if (nk > 0) {
-                    tmem_ld_32x32b_x16(taddr + c, r);
-                    tmem_ld_wait();
-                }
+        for (uint32_t c = 0; c < a.acc_cols; c += 16) {
+            if (SWAP && (int)(c >= (uint32_t)a.bn ? c - a.bn : c) >= live) continue;
+            uint32_t r[16];
+            if (nk > 0) {
+                tmem_ld_32x32b_x16(taddr + c, r);
+                tmem_ld_wait();
+            } else {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) part[(c + j) * 128 + trow] = nk > 0 ? __uint_as_float(r[j]) : 0.0f;
+                for (int j = 0; j < 16; ++j) r[j] = 0;
+            }
+            if (SWAP) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) part[(c + j) * kSwapStride + trow] = __uint_as_float(r[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; j += 4)
+                    *reinterpret_cast<uint4*>(part + trow * stride + c + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
             }
         }
-        cluster_sync();
     }
-    if (warp >= 2 && ok) {
-        const long long prow = (long long)row0 + trow;
-        const uint32_t base = smem_u32(part) + 4u * (uint32_t)trow;
-        if (SWAP) {
-            const float b = a.bias && prow < p.n ? a.bias[prow] : 0.0f;
-            const float b2 = GATED && a.bias2 && prow < p.n ? a.bias2[prow] : 0.0f;
-            const int cols = (int)min((long long)a.bn, p.m - col0);
-            if (a.splits > 1) {
-                for (int c = (int)rank; c < cols; c += a.splits) {
-                    float v = 0.0f, w = 0.0f;
-                    for (int s = 0; s < a.splits; ++s) {
-                        const uint32_t peer = map_rank(base, (uint32_t)s);
-                        v += ld_cluster_f32(peer + (uint32_t)c * 512u);
-                        if (GATED) w += ld_cluster_f32(peer + (uint32_t)(a.bn + c) * 512u);
-                    }
-                    if (prow < p.n) finish1<GATED>(a, p, col0 + c, prow, v, w, b, b2);
-                }
-            } else {
-                for (int c0 = 0; c0 < cols; c0 += 16) {
-                    uint32_t rv[16], rw[16];
-                    if (nk > 0) {
-                        tmem_ld_32x32b_x16(taddr + c0, rv);
-                        if (GATED) tmem_ld_32x32b_x16(taddr + a.bn + c0, rw);
-                        tmem_ld_wait();
-                    }
+    if (a.splits > 1)
+        cluster_sync();
+    else
+        __syncthreads();
+    if (!abort_flag) {
+        const long long col = (SWAP ? row0 : col0) + lane * N;
+        const int first_row = SWAP ? col0 : row0;
+        float b[N], b2[N];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c0 + j < cols && prow < p.n)
-                            finish1<GATED>(a, p, col0 + c0 + j, prow, nk > 0 ? __uint_as_float(rv[j]) : 0.0f,
-                                           GATED && nk > 0 ? __uint_as_float(rw[j]) : 0.0f, b, b2);
+        for (int j = 0; j < N; ++j) {
+            b[j] = a.bias && col + j < p.n ? a.bias[col + j] : 0.0f;
+            b2[j] = GATED && a.bias2 && col + j < p.n ? a.bias2[col + j] : 0.0f;
+        }
+        const uint32_t base = smem_u32(part) + 4u * (uint32_t)(lane * N);
+        auto rows = [&](auto cut) {
+            constexpr int S = decltype(cut)::value;
+            constexpr int kStep = S * (kThreads / 32);
+            auto load = [&](int i, float (&t)[S][N], float (&tw)[GATED ? S : 1][N], float (&e)[N]) {
+                const uint32_t at = base + 4u * (uint32_t)i * stride;
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    if constexpr (S == 1) {
+                        ld_own<N>(at, t[s]);
+                        if (GATED) ld_own<N>(at + 4u * u_off, tw[s]);
+                    } else {
+                        const uint32_t peer = map_rank(at, (uint32_t)s);
+                        ld_cluster<N>(peer, t[s]);
+                        if (GATED) ld_cluster<N>(peer + 4u * u_off, tw[GATED ? s : 0]);
+                    }
                 }
+                if (a.res.p) load_n<N>(a.res, first_row + i, col, p.n, e, a.status);
+            };
+            // the next row's loads run beside this row's arithmetic; one copy of the code, which is what fits the
+            // instruction cache
+            float t[S][N], tw[GATED ? S : 1][N], e[N];
+            int i = (int)rank + S * warp;
+            if (i < live) load(i, t, tw, e);
+#pragma unroll 1
+            for (; i < live; i += kStep) {
+                float v[N], w[N], r[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    v[j] = t[0][j];
+                    w[j] = GATED ? tw[0][j] : 0.0f;
+                    r[j] = e[j];
+#pragma unroll
+                    for (int s = 1; s < S; ++s) {
+                        v[j] += t[s][j];
+                        if (GATED) w[j] += tw[GATED ? s : 0][j];
+                    }
+                }
+                if (i + kStep < live) load(i + kStep, t, tw, e);
+                if (col < p.n) finish_n<GATED, N>(a, p, first_row + i, col, v, w, b, b2, r);
             }
-        } else {
-            const int cols = (int)min((long long)a.bn, p.n - col0);
-            const int first = a.splits > 1 ? 16 * (int)rank : 0, step = 16 * a.splits;
-            for (int c = first; c < cols; c += step) {
-                float v[16], w[16];
-                if (a.splits > 1) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = w[j] = 0.0f;
-                    for (int s = 0; s < a.splits; ++s) {
-                        const uint32_t peer = map_rank(base, (uint32_t)s);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) v[j] += ld_cluster_f32(peer + (uint32_t)(c + j) * 512u);
-                        if (GATED) {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) w[j] += ld_cluster_f32(peer + (uint32_t)(a.bn + c + j) * 512u);
-                        }
-                    }
-                } else {
-                    uint32_t rv[16], rw[16];
-                    tmem_ld_32x32b_x16(taddr + c, rv);
-                    if (GATED) tmem_ld_32x32b_x16(taddr + a.bn + c, rw);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        v[j] = __uint_as_float(rv[j]);
-                        w[j] = GATED ? __uint_as_float(rw[j]) : 0.0f;
-                    }
-                }
-                if (prow < p.m) finish16<GATED>(a, p, prow, col0 + c, v, w, s_bias + c, s_bias + kMaxAccCols + c);
-            }
+        };
+        switch (a.splits) {
+        case 1: rows(ActTag<1>()); break;
+        case 2: rows(ActTag<2>()); break;
+        case 4: rows(ActTag<4>()); break;
+        default: rows(ActTag<8>()); break;
         }
     }
     if (a.splits > 1) cluster_sync();  // the others have read this CTA's sums
@@ -281,24 +296,46 @@ int tile_width(const TgProblem* t, int count)
     return bn;
 }
 
-// CTAs that each contraction is cut over.  Few tiles: 2, 4 or 8 (of at least
-// four steps each); and an fp32 output's anyway, so that no sum inside the
-// tensor cores passes 2048 elements where 8 CTAs are enough for that (over 8192
-// elements one sum was 1.0e-6 off, four added up in fp32 0.25e-6).
-int cuts(const TgProblem* t, int count)
+// CTAs that each contraction is cut over, 1, 2, 4 or 8 (of at least two steps
+// each), and an estimate of the time in 10 ns.  Measured: a round of CTAs (two
+// an SM) takes 6 us beside its steps and 8 us each one after the first, a step
+// 0.3 us where a CTA has its SM to itself and 0.5 us where two share it, joining
+// the parts 1 us (777 x 2736 -> 1024: 19.9 us whole, 14.1 / 13.5 / 21.5 cut in 2
+// / 4 / 8; 512 x 4096 -> 4096: 27.3, 20.9, 29.2, 47.8).  An fp32 output's
+// contraction is cut anyway, so that no sum inside the tensor cores passes 1024
+// elements where 8 CTAs are enough for that (see tgemm_pair.cu).
+struct Cut {
+    int splits;
+    long long time;
+};
+Cut choose_cut(const TgProblem* t, int count)
 {
-    const int bn = tile_width(t, count), sm = device_sm_count();
-    long long tiles = 0, nk = 0, longest = 0;
+    const int bn = tile_width(t, count);
+    const long long sm = device_sm_count();
+    long long tiles = 0, work = 0, nk = 0, longest = 0;
+    bool alike = true;
     for (int i = 0; i < count; ++i) {
         const long long steps = steps_of(t[i]);
         const bool swap = swapped(t[i]);
-        tiles += ((swap ? t[i].n : t[i].m) + 127) / 128 * (((swap ? t[i].m : t[i].n) + bn - 1) / bn);
+        const long long n = ((swap ? t[i].n : t[i].m) + 127) / 128 * (((swap ? t[i].m : t[i].n) + bn - 1) / bn);
+        tiles += n;
+        work += n * steps;
+        alike = alike && (!i || steps == nk);
         if (steps > nk) nk = steps;
         if (t[i].y.dt == SADMM_FP32 && steps > longest) longest = steps;
     }
-    int splits = 1;
-    while (splits < 8 && ((tiles * splits * 2 <= 2 * sm && nk >= 8 * splits) || longest > 32 * splits)) splits *= 2;
-    return splits;
+    Cut best = {1, 0};
+    for (int s = 1; s <= 8; s *= 2) {
+        if (s > 1 && nk < 2 * s) break;
+        const long long ctas = tiles * s, steps = (nk + s - 1) / s;
+        const long long rounds = (ctas + 2 * sm - 1) / (2 * sm);
+        long long busiest = steps * (alike ? rounds : 1);  // steps of one place for a CTA
+        if (!alike && busiest < work / (2 * sm)) busiest = work / (2 * sm);
+        const long long time = 600 + 800 * (rounds - 1) + busiest * (ctas > sm ? 50 : 30) + (s > 1 ? 100 : 0) +
+                               (s == 8 && ctas > sm ? 250 : 0);  // clusters of eight, two CTAs an SM
+        if (s == 1 || time < best.time || longest > 16 * best.splits) best = {s, time};
+    }
+    return best;
 }
 
 sadmm_status launch_tiles(const TgProblem* t, int count, int splits, cudaStream_t s)
@@ -342,7 +379,8 @@ sadmm_status launch_tiles(const TgProblem* t, int count, int splits, cudaStream_
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     if (a.stages > steps) a.stages = steps;
     size_t smem = (size_t)a.stages * a.stage_bytes;
-    if (splits > 1 && smem < (size_t)a.acc_cols * 512) smem = (size_t)a.acc_cols * 512;
+    const size_t staged = 4 * (size_t)(swap ? a.acc_cols * kSwapStride : 128 * (a.acc_cols + 4));
+    if (smem < staged) smem = staged;
     smem += 1024;
     if (gated) return swap ? run<true, true>(maps, a, smem, s) : run<false, true>(maps, a, smem, s);
     return swap ? run<true, false>(maps, a, smem, s) : run<false, false>(maps, a, smem, s);
@@ -365,16 +403,12 @@ sadmm_status launch_tgemm(const TgProblem* all, int count, cudaStream_t s)
     for (int i = 0; i < count; ++i)
         if (!all[i].skip) t[wanted++] = all[i];
     if (!wanted) return SADMM_OK;
+    const Cut cut = choose_cut(all, count);
     if (!swapped(all[0])) {
-        const bool gated = all->mode == kTgGated;
-        const TgPairChoice c = choose_tgemm_pair(all, count);
-        long long work = 0;  // steps of 128-row tiles
-        for (int i = 0; i < count; ++i)
-            work += (all[i].m + 127) / 128 * ((all[i].n + (gated ? 63 : 127)) / (gated ? 64 : 128)) * steps_of(all[i]);
-        if (c.cycles < work * 560 / device_sm_count() + 6000)
+        if (choose_tgemm_pair(all, count).time < cut.time)
             return launch_tgemm_pair(t, wanted, choose_tgemm_pair(t, wanted).bn, s);
     }
-    return launch_tiles(t, wanted, cuts(all, count), s);
+    return launch_tiles(t, wanted, cut.splits, s);
 }
 
 }  // namespace sadmm

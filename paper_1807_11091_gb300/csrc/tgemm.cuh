@@ -61,10 +61,10 @@ sadmm_status launch_tgemm(const TgProblem* t, int count, cudaStream_t s);
 
 // The same by CTA pairs (tgemm_pair.cu) with tiles of 256 x bn, bn a multiple
 // of 64 up to 256; choose_tgemm_pair gives the width it takes and an estimate
-// of its cycles.
+// of the time in 10 ns.
 struct TgPairChoice {
     int bn;
-    long long cycles;
+    long long time;
 };
 TgPairChoice choose_tgemm_pair(const TgProblem* t, int count);
 sadmm_status launch_tgemm_pair(const TgProblem* t, int count, int bn, cudaStream_t s);

@@ -9,6 +9,7 @@
 
 #include "act.cuh"
 #include "common.cuh"
+#include "output.cuh"
 #include "internal.h"
 #include "tgemm.cuh"
 
@@ -22,16 +23,6 @@ constexpr int kBox = 8192;        // one 64 x 64 bf16 box
 constexpr int kPTile = 2 * kBox;  // 128 rows x 64
 constexpr int kTgProducts = 3;    // products of a launch, at most
 constexpr int kTgMaps = 7;        // and their tensor maps
-
-// An output matrix as the epilogue stores it.  vec: 2 / 1 / 0 for rows on
-// 32-byte / 16-byte / other boundaries.
-struct Out {
-    void* p;
-    long long ld;
-    long long total;  // elements from p to the end of the last row
-    int bf16;
-    int vec;
-};
 
 // One product of a launch.  The P side is the tile's 128-row side: the output's
 // rows, or its columns where the tiles are swapped.
@@ -69,36 +60,6 @@ struct TgArgs {
 };
 
 // ------------------------------------------------------------- device PTX --
-
-SADMM_DEV uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
-// Every thread of every CTA of the cluster calls it.
-SADMM_DEV void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-
-SADMM_DEV uint32_t map_rank(uint32_t saddr, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
-    return a;
-}
-
-SADMM_DEV float ld_cluster_f32(uint32_t a)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
-}
-
-// Waits for the 128 epilogue threads.
-SADMM_DEV void epi_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // Shared-memory matrix descriptor of a row-contiguous (MN-major) operand held
 // as 64-row boxes of 64 contraction elements with the 128-byte swizzle: within
@@ -215,21 +176,80 @@ SADMM_DEV void add16(const Out& o, long long r, long long c, long long n, float 
     }
 }
 
-SADMM_DEV void store1(const Out& o, long long r, long long c, float v, int* status)
+// The same for N neighbouring columns, 2 or 4 (c a multiple of N).
+template <int N>
+SADMM_DEV void store_n(const Out& o, long long r, long long c, long long n, const float (&v)[N], int* status)
 {
     const long long at = r * o.ld + c;
-    if (!dbg_in(at, o.total, status)) return;
-    if (o.bf16)
-        static_cast<__nv_bfloat16*>(o.p)[at] = __float2bfloat16_rn(v);
-    else
-        static_cast<float*>(o.p)[at] = v;
+    if (c + N <= n && o.vec && dbg_in(at, o.total, status) && dbg_in(at + N - 1, o.total, status)) {
+        if (o.bf16) {
+            uint32_t w[N / 2];
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+            __nv_bfloat16* p = static_cast<__nv_bfloat16*>(o.p) + at;
+            if constexpr (N == 4)
+                *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+            else
+                *reinterpret_cast<uint32_t*>(p) = w[0];
+        } else {
+            float* p = static_cast<float*>(o.p) + at;
+            if constexpr (N == 4)
+                *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+            else
+                *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (c + j >= n || !dbg_in(at + j, o.total, status)) continue;
+        if (o.bf16)
+            static_cast<__nv_bfloat16*>(o.p)[at + j] = __float2bfloat16_rn(v[j]);
+        else
+            static_cast<float*>(o.p)[at + j] = v[j];
+    }
 }
 
-SADMM_DEV float load1(const Out& o, long long r, long long c, int* status)
+// N neighbouring columns of o, zero at or past n.
+template <int N>
+SADMM_DEV void load_n(const Out& o, long long r, long long c, long long n, float (&v)[N], int* status)
 {
     const long long at = r * o.ld + c;
-    if (!dbg_in(at, o.total, status)) return 0.0f;
-    return o.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(o.p)[at]) : static_cast<const float*>(o.p)[at];
+    if (c + N <= n && o.vec && dbg_in(at, o.total, status) && dbg_in(at + N - 1, o.total, status)) {
+        if (o.bf16) {
+            const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(static_cast<const __nv_bfloat16*>(o.p) + at);
+            uint32_t w[N / 2];
+            if constexpr (N == 4) {
+                const uint2 q = *reinterpret_cast<const uint2*>(p);
+                w[0] = q.x;
+                w[N / 2 - 1] = q.y;
+            } else {
+                w[0] = *reinterpret_cast<const uint32_t*>(p);
+            }
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) {
+                v[2 * j] = __uint_as_float(w[j] << 16);
+                v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            }
+        } else {
+            const float* p = static_cast<const float*>(o.p) + at;
+            if constexpr (N == 4) {
+                const float4 q = *reinterpret_cast<const float4*>(p);
+                v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+            } else {
+                const float2 q = *reinterpret_cast<const float2*>(p);
+                v[0] = q.x; v[1] = q.y;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        v[j] = 0.0f;
+        if (c + j >= n || !dbg_in(at + j, o.total, status)) continue;
+        v[j] = o.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(o.p)[at + j])
+                      : static_cast<const float*>(o.p)[at + j];
+    }
 }
 
 // Sixteen columns of one output row: sb / sb2 are the tile's biases in shared memory.
@@ -237,11 +257,21 @@ template <bool GATED>
 SADMM_DEV void finish16(const TgArgs& a, const TgProduct& p, long long r, long long c, float (&v)[16], float (&w)[16],
                         const float* sb, const float* sb2)
 {
+    if (a.bias) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] += sb[j];
+        for (int j = 0; j < 16; j += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(sb + j);
+            v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+        }
+    }
     if (GATED) {
+        if (a.bias2) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] += sb2[j];
+            for (int j = 0; j < 16; j += 4) {
+                const float4 b = *reinterpret_cast<const float4*>(sb2 + j);
+                w[j] += b.x; w[j + 1] += b.y; w[j + 2] += b.z; w[j + 3] += b.w;
+            }
+        }
         if (a.u.p) store16(a.u, r, c, p.n, w, a.status);
     }
     if (a.z.p) store16(a.z, r, c, p.n, v, a.status);
@@ -258,22 +288,30 @@ SADMM_DEV void finish16(const TgArgs& a, const TgProduct& p, long long r, long l
     store16(p.y, r, c, p.n, v, a.status);
 }
 
-// One element.
-template <bool GATED>
-SADMM_DEV void finish1(const TgArgs& a, const TgProduct& p, long long r, long long c, float v, float w, float b, float b2)
+// N neighbouring columns; b and b2 are their biases, e their residual.
+template <bool GATED, int N>
+SADMM_DEV void finish_n(const TgArgs& a, const TgProduct& p, long long r, long long c, float (&v)[N], float (&w)[N],
+                        const float (&b)[N], const float (&b2)[N], const float (&e)[N])
 {
-    v += b;
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] += b[j];
     if (GATED) {
-        w += b2;
-        if (a.u.p) store1(a.u, r, c, w, a.status);
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] += b2[j];
+        if (a.u.p) store_n<N>(a.u, r, c, p.n, w, a.status);
     }
-    if (a.z.p) store1(a.z, r, c, v, a.status);
-    with_act(a.act, [&](auto tag) { v = act_f32<decltype(tag)::value>(v); });
-    if (GATED) v *= w;
-    if (a.res.p) v += load1(a.res, r, c, a.status);
-    store1(p.y, r, c, v, a.status);
+    if (a.z.p) store_n<N>(a.z, r, c, p.n, v, a.status);
+    with_act(a.act, [&](auto tag) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = act_f32<decltype(tag)::value>(v[j]);
+    });
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (GATED) v[j] *= w[j];
+        if (a.res.p) v[j] += e[j];
+    }
+    store_n<N>(p.y, r, c, p.n, v, a.status);
 }
-
 
 // One operand's part of a stage: `rows` rows from row0, 64 contraction elements from k0.
 SADMM_DEV void load_part(uint8_t* dst, const CUtensorMap* map, uint64_t* bar, int kmajor, int rows, int row0, int k0)
@@ -302,19 +340,6 @@ bool encode(CUtensorMap* map, const TgOperand& o, int rows_per_tile)
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(o.p), gdim, gstride, box, estride,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-Out make_out(const TgMatrix& m, long long rows, long long cols)
-{
-    Out o;
-    const long long es = m.dt == SADMM_BF16 ? 2 : 4;
-    o.p = m.p;
-    o.ld = m.ld;
-    o.total = (rows - 1) * m.ld + cols;
-    o.bf16 = m.dt == SADMM_BF16;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(m.p) | (uintptr_t)(m.ld * es);
-    o.vec = at % 32 == 0 ? 2 : at % 16 == 0 ? 1 : 0;
-    return o;
 }
 
 // What the kernels' arguments have in common: the products' outputs, and the

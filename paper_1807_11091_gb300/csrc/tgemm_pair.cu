@@ -12,8 +12,10 @@
 //               half of the columns
 // Two accumulators in TMEM: a tile's epilogue runs beside the next tile's
 // products.  fp32 outputs of long contractions (LONG) are added up over
-// accumulators of kLongSteps steps each, in registers, because sums of
-// thousands of terms inside the tensor cores lose digits.
+// accumulators of kLongSteps steps each, in registers, because a sum inside the
+// tensor cores loses digits as it grows longer (relative error of weight
+// gradients: 0.24e-6 over 256 terms, 0.48e-6 over 512, 1.0e-6 over 1024, 2.1e-6
+// over 2048).
 #include "tgemm_dev.cuh"
 
 namespace sadmm {
@@ -22,7 +24,7 @@ namespace {
 constexpr int kPairThreads = 320;
 constexpr int kPairStages = 10;          // at most
 constexpr int kPairSmem = 192 * 1024;    // of stages
-constexpr int kLongSteps = 32;          // 2048 contraction elements
+constexpr int kLongSteps = 8;           // 512 contraction elements
 
 // ------------------------------------------------------------- device PTX --
 
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     __shared__ uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_holder;
     __shared__ volatile int abort_flag;
-    __shared__ float s_bias[2][256];  // by tile parity; gated: the second half is u's
+    __shared__ __align__(16) float s_bias[2][256];  // by tile parity; gated: the second half is u's
     // warp-uniform to the compiler, which keeps the issue loop's descriptors in uniform registers: an MMA and its
     // stage then cost less to issue than to run (4096^3: 86.5 -> 83.7 us)
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -164,7 +166,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         tmem_relinquish2();
     }
     pdl_wait();  // nothing above reads global memory
-    pdl_trigger();
     tc_fence_before();
     __syncthreads();
     cluster_sync();  // barriers and TMEM of both CTAs are there
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             const long long row = (long long)pl.mt * 256 + rank * 128 + q * 32 + lane;
             const long long col0 = (long long)pl.nt * cols;
             const int live = (int)min((long long)cols, p.n - col0);  // columns inside the output
-            {
+            if (a.bias || a.bias2) {
                 const int j = threadIdx.x - 64;
                 float b = 0.0f;
                 if (j < cols) {
@@ -438,9 +439,11 @@ void by_length(const TgProblem* t, int count, const TgProblem** order)
 
 }  // namespace
 
-// The tile width whose busiest pair costs least: a step of 64 contraction
-// elements takes 540 cycles at 256 columns (the MMAs' 512) and hardly less
-// below, because issuing a stage takes about 470.
+// The tile width whose busiest pair costs least.  Measured: a step of 64
+// contraction elements takes 0.34 us at 256 columns (0.27 us of MMAs) and hardly
+// less below, because issuing a stage takes about 470 cycles; beside its steps a
+// launch takes 5.4 us at 256 columns and 4.6 at 64, most of it the last
+// epilogue (1024^3: 10.8 us at 256, 10.0 at 128, 9.5 at 64).
 TgPairChoice choose_tgemm_pair(const TgProblem* t, int count)
 {
     const TgProblem* order[kTgProducts];
@@ -448,8 +451,9 @@ TgPairChoice choose_tgemm_pair(const TgProblem* t, int count)
     TgPairChoice best = {0, 0};
     for (int bn = 256; bn >= 64; bn -= 64) {
         const Schedule w = schedule_of(order, count, bn, device_sm_count() / 2);
-        const long long cycles = w.steps * (bn == 256 ? 540 : bn == 192 ? 520 : 490) + 6000 + bn * 12;
-        if (!best.bn || cycles < best.cycles) best = {bn, cycles};
+        const long long time = w.steps * (bn == 256 ? 34 : bn == 192 ? 33 : bn == 128 ? 31 : 30) +
+                               (bn == 256 ? 540 : bn == 192 ? 520 : bn == 128 ? 500 : 460);
+        if (!best.bn || time < best.time) best = {bn, time};
     }
     return best;
 }

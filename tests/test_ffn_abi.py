@@ -104,7 +104,7 @@ def test_too_large_is_unsupported(make_args, wide):
 
 @pytest.mark.parametrize("make_args", [linear_bwd, gated_bwd, ln_bwd])
 def test_workspace_is_checked(make_args):
-    a = make_args()
+    a = make_args(act=1, z=P[6], ldz=32) if make_args is linear_bwd else make_args()
     need = getattr(sadmm, f"sadmm_{CALLS[make_args]}_workspace_size")(a)
     assert need > 0
     for ws, nbytes in ((None, need), (P[11], need - 1), (P[11] + 16, need)):
@@ -112,14 +112,17 @@ def test_workspace_is_checked(make_args):
 
 
 def test_workspace_sizes():
-    """Aligned matrices are read where they lie; any other is copied, its rows to multiples of 8."""
+    """Aligned matrices are read where they lie; any other is copied, its rows to multiples of 8,
+    except for a few tokens, which are read as they are."""
     size = sadmm.sadmm_linear_fwd_workspace_size
-    assert size(linear_fwd()) == 0
-    assert size(linear_fwd(ldx=68)) == 4 * 64 * 2
-    assert size(linear_fwd(x=P[0] + 2)) == 4 * 64 * 2
-    assert size(linear_fwd(n_in=61, ldx=61, ldw=61)) == 4 * 64 * 2 + 32 * 64 * 2
-    assert sadmm.sadmm_gated_fwd_workspace_size(gated_fwd(ldwu=65)) == 32 * 64 * 2
-    assert sadmm.sadmm_linear_bwd_workspace_size(linear_bwd(db=None)) == 0
+    assert size(linear_fwd(tokens=40)) == 0
+    assert size(linear_fwd(tokens=40, ldx=68)) == 40 * 64 * 2
+    assert size(linear_fwd(tokens=40, x=P[0] + 2)) == 40 * 64 * 2
+    assert size(linear_fwd(tokens=40, n_in=61, ldx=61, ldw=61)) == 40 * 64 * 2 + 32 * 64 * 2
+    assert size(linear_fwd(tokens=1, n_in=61, ldx=61, ldw=61)) == 0
+    assert sadmm.sadmm_gated_fwd_workspace_size(gated_fwd(tokens=40, ldwu=65)) == 32 * 64 * 2
+    assert sadmm.sadmm_gated_fwd_workspace_size(gated_fwd(tokens=1, ldwu=65)) == 0
+    assert sadmm.sadmm_linear_bwd_workspace_size(linear_bwd()) == 0
     assert sadmm.sadmm_linear_bwd_workspace_size(linear_bwd(db=None, act=1, z=P[6], ldz=32)) == 4 * 32 * 2
     assert sadmm.sadmm_layernorm_bwd_workspace_size(ln_bwd(dgamma=None, dbeta=None)) == 0
 

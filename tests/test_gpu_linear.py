@@ -318,3 +318,19 @@ def test_leading_dimensions_and_streams():
     torch.cuda.current_stream().wait_stream(side)
     done()
     assert all(torch.equal(t, ref) for t in got)
+
+
+def test_backward_passes_in_a_row():
+    """More clusters than the device holds at once, each pass's kernels close behind the ones before,
+    from an idle device: the products' clusters must not take the places of those that have not started."""
+    s, g = lib(), F.gen(12)
+    T, K, N = 1025, 1024, 2731
+    dy, x = F.matrix(g, T, N, scale=0.01), F.matrix(g, T, K)
+    W, z = F.matrix(g, N, K, scale=K ** -0.5), F.matrix(g, T, N)
+    first = s.linear_backward(dy, x, W, z=z, act=s.SADMM_ACT_GELU)
+    for i in range(600):
+        got = s.linear_backward(dy, x, W, z=z, act=s.SADMM_ACT_GELU)
+        if i % 8 == 0:
+            torch.cuda.synchronize()
+    done()
+    assert all(torch.equal(a, b) for a, b in zip(got, first))
