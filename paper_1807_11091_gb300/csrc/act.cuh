@@ -6,10 +6,26 @@
 
 namespace sadmm {
 
+// Codes beside sadmm_act: the same functions for results that are rounded to
+// bf16, by act_slope_f32's faster forms.
+constexpr int kGeluBf16 = 4, kSiluBf16 = 5;
+inline int act_for(int act, bool bf16)
+{
+    return !bf16 ? act : act == SADMM_ACT_GELU ? kGeluBf16 : act == SADMM_ACT_SILU ? kSiluBf16 : act;
+}
+
+template <int ACT>
+SADMM_DEV void act_slope_f32(float z, float& a, float& s);
+
 // act(z): max(z, 0) (NaN kept); z Phi(z) with the normal distribution Phi; z sigmoid(z).
 template <int ACT>
 SADMM_DEV float act_f32(float z)
 {
+    if (ACT == kGeluBf16 || ACT == kSiluBf16) {
+        float a, s;
+        act_slope_f32<ACT == kGeluBf16 ? SADMM_ACT_GELU : SADMM_ACT_SILU>(z, a, s);
+        return a;
+    }
     if (ACT == SADMM_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if (ACT == SADMM_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
     if (ACT == SADMM_ACT_SILU) return __fdividef(z, 1.0f + expf(-z));
@@ -56,6 +72,8 @@ SADMM_DEV void with_act(int act, F f)
     case SADMM_ACT_RELU: f(ActTag<SADMM_ACT_RELU>()); break;
     case SADMM_ACT_GELU: f(ActTag<SADMM_ACT_GELU>()); break;
     case SADMM_ACT_SILU: f(ActTag<SADMM_ACT_SILU>()); break;
+    case kGeluBf16: f(ActTag<kGeluBf16>()); break;
+    case kSiluBf16: f(ActTag<kSiluBf16>()); break;
     default: f(ActTag<SADMM_ACT_NONE>()); break;
     }
 }

@@ -418,7 +418,7 @@ struct BwdArgs {
 };
 
 template <typename X, typename Y, bool VEC, int CAP, int E>
-__global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 1 ? 3 : 2) k_ln_bwd(const BwdArgs a)
+__global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? (E == 1 ? 2 : 1) : CAP && E == 1 ? 3 : 2) k_ln_bwd(const BwdArgs a)
 {
     constexpr bool BLOCK = CAP > 0;
     extern __shared__ __align__(128) uint8_t ring[];
@@ -651,7 +651,7 @@ constexpr int kBwdShortCols = 2048;  // backward: up to here 8 elements a thread
 int block_threads(int cols, int e) { return (int)round_up((cols + 8 * e - 1) / (8 * e), 32); }
 
 // Blocks an SM holds: of eight warps with a row each, or of one row, where the
-// kernels' registers allow 768 threads (forward) and 512 (backward).
+// kernels' registers allow 768 threads (forward: 16 elements each; backward: 8).
 int fwd_blocks_per_sm(int cols)
 {
     if (cols <= kWarpCols) return 3;
@@ -662,8 +662,7 @@ int bwd_blocks_per_sm(int cols)
 {
     if (cols <= kWarpCols) return 2;
     if (cols <= kBwdShortCols) return 768 / block_threads(cols, 1) < 4 ? 768 / block_threads(cols, 1) : 4;
-    const int threads = block_threads(cols, 2);
-    return threads > 256 ? 1 : 512 / threads < 4 ? 512 / threads : 4;
+    return cols <= 4096 ? 2 : 1;
 }
 
 // Blocks of the backward: each leaves a partial sum.
@@ -757,7 +756,7 @@ sadmm_status bwd(const BwdArgs& a, cudaStream_t s)
     if (a.cols <= 256) return bwd_run<X, Y, VEC, 0, 1>(a, s);
     if (a.cols <= kWarpCols) return bwd_run<X, Y, VEC, 0, 2>(a, s);
     if (a.cols <= kBwdShortCols) return bwd_run<X, Y, VEC, 256, 1>(a, s);
-    if (a.cols <= 4096) return bwd_run<X, Y, VEC, 256, 2>(a, s);
+    if (a.cols <= 4096) return bwd_run<X, Y, VEC, 512, 1>(a, s);
     if (a.cols <= kBwdBlockCols) return bwd_run<X, Y, VEC, 512, 2>(a, s);
     cudaError_t err = cudaSuccess;
     if (a.dx) err = launch_pdl(k_ln_bwd_long<X, Y>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);

@@ -81,10 +81,11 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
     }
     pdl_wait();  // nothing above reads what an earlier kernel may write
-    if (a.splits == 1) pdl_trigger();  // (clusters do not: see common.cuh)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // (clusters do not: see common.cuh; and not before this CTA has its TMEM, which the next kernel may want too)
+    if (a.splits == 1) pdl_trigger();
     const uint32_t tmem = tmem_holder;
 
     if (warp == 0) {

@@ -357,7 +357,7 @@ void fill_common(TgArgs& a, const TgProblem* t, int count)
     }
     a.bias = t->bias;
     a.bias2 = t->bias2;
-    a.act = t->act;
+    a.act = act_for(t->act, t->y.dt == SADMM_BF16);
     if (t->residual.p) a.res = make_out(t->residual, t->m, t->n);
     if (t->z.p) a.z = make_out(t->z, t->m, t->n);
     if (t->u.p) a.u = make_out(t->u, t->m, t->n);
