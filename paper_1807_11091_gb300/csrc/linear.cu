@@ -127,7 +127,7 @@ SADMM_DEV float f32(float v) { return v; }
 // sums: over a thread's rows in order, then the CTA's threads, then the
 // cluster's CTAs in rank order.
 template <bool GATED, bool VEC, typename DY>
-__global__ void __launch_bounds__(kDactThreads, GATED ? 3 : VEC ? 4 : 2) k_dact(const DactArgs a)
+__global__ void __launch_bounds__(kDactThreads, GATED || !VEC ? 3 : 4) k_dact(const DactArgs a)
 {
     constexpr int N = VEC ? 8 : 2;              // columns of a thread
     constexpr int L = VEC ? 32 : 8;             // rows at a time
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kDactThreads, GATED ? 3 : VEC ? 4 : 2) k_dact(
     with_act(a.z ? a.act : SADMM_ACT_NONE, [&](auto tag) {
         constexpr int A = decltype(tag)::value;
         constexpr bool Z = GATED || A != SADMM_ACT_NONE;
-        constexpr int U = VEC ? (Z ? 2 : 4) : 8;  // turns whose loads are in flight together
+        constexpr int U = VEC && !Z ? 4 : VEC ? 2 : 4;  // turns whose loads are in flight together
         // one row's values: sums them up and writes the copies
         auto row = [&](long long r, const Raw<DY, N>& rd, const Raw<bf16, N>& rz, const Raw<bf16, N>& ru) {
             float d[N], e[N];
@@ -161,14 +161,15 @@ __global__ void __launch_bounds__(kDactThreads, GATED ? 3 : VEC ? 4 : 2) k_dact(
                 d[j] = f32(rd.e[j]);
                 float act = 0.0f, slope = 1.0f;
                 if (Z) act_slope_f32<A>(f32(rz.e[j]), act, slope);
+                // (products and sums not fused: the sums' bits do not depend on whether the products are also stored)
                 if (GATED) {
-                    e[j] = d[j] * act;
-                    d[j] = d[j] * f32(ru.e[j]) * slope;
-                    su[j] += e[j];
+                    e[j] = __fmul_rn(d[j], act);
+                    d[j] = __fmul_rn(__fmul_rn(d[j], f32(ru.e[j])), slope);
+                    su[j] = __fadd_rn(su[j], e[j]);
                 } else if (A != SADMM_ACT_NONE) {
-                    d[j] *= slope;
+                    d[j] = __fmul_rn(d[j], slope);
                 }
-                s[j] += d[j];
+                s[j] = __fadd_rn(s[j], d[j]);
             }
             if (VEC) {
                 if (a.dz && cl * 8 < left) {

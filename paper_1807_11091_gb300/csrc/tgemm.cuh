@@ -60,7 +60,7 @@ inline bool tg_aligned(const void* p, long long ld)
 sadmm_status launch_tgemm(const TgProblem* t, int count, cudaStream_t s);
 
 // The same by CTA pairs (tgemm_pair.cu) with tiles of 256 x bn, bn a multiple
-// of 64 up to 256; choose_tgemm_pair gives the width it takes and an estimate
+// of 64 (of 32 where choose_tgemm_pair says so) up to 256; choose_tgemm_pair gives the width it takes and an estimate
 // of the time in 10 ns.
 struct TgPairChoice {
     int bn;

@@ -443,16 +443,20 @@ void by_length(const TgProblem* t, int count, const TgProblem** order)
 // contraction elements takes 0.34 us at 256 columns (0.27 us of MMAs) and hardly
 // less below, because issuing a stage takes about 470 cycles; beside its steps a
 // launch takes 5.4 us at 256 columns and 4.6 at 64, most of it the last
-// epilogue (1024^3: 10.8 us at 256, 10.0 at 128, 9.5 at 64).
+// epilogue (1024^3: 10.8 us at 256, 10.0 at 128, 9.5 at 64).  Widths are
+// multiples of 64, or of 32 where the columns' operand is contiguous along the
+// contraction (no whole 64-row boxes) and not a gated pair's.
 TgPairChoice choose_tgemm_pair(const TgProblem* t, int count)
 {
     const TgProblem* order[kTgProducts];
     by_length(t, count, order);
+    int grain = t->mode == kTgGated ? 64 : 32;
+    for (int i = 0; i < count; ++i)
+        if (!t[i].b[0].kmajor) grain = 64;
     TgPairChoice best = {0, 0};
-    for (int bn = 256; bn >= 64; bn -= 64) {
+    for (int bn = 256; bn >= 64; bn -= grain) {
         const Schedule w = schedule_of(order, count, bn, device_sm_count() / 2);
-        const long long time = w.steps * (bn == 256 ? 34 : bn == 192 ? 33 : bn == 128 ? 31 : 30) +
-                               (bn == 256 ? 540 : bn == 192 ? 520 : bn == 128 ? 500 : 460);
+        const long long time = w.steps * (28 + bn / 48 + (bn == 256)) + 430 + bn * 2 / 5;
         if (!best.bn || time < best.time) best = {bn, time};
     }
     return best;
