@@ -2,8 +2,10 @@
 
 Each translation unit compiles in parallel; the objects link into one shared
 library with the CUDA runtime linked statically, so the library loads
-alongside any other CUDA user in the process.  No cmake, no torch extension
-machinery: the C ABI in include/sadmm.h is the only interface.
+alongside any other CUDA user in the process.  No cmake: the C ABI in
+include/sadmm.h is the library's only interface.  One host file beside it,
+csrc/torch_ffn.cpp, is compiled against the torch of this interpreter: the
+feed-forward functions' arguments and outputs as torch tensors.
 
 The debug library (_build/debug/libsadmm.so, -DSADMM_DEBUG) adds index checks
 to the kernels' global loads and stores: an index outside its buffer skips the

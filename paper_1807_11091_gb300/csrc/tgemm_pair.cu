@@ -6,7 +6,7 @@
 // shared memory feeds twice the products of a single CTA's tile; the gated
 // pair's second CTA holds the columns of Wu where the first has those of Wg.
 // Per CTA, ten warps:
-//   warp 0      TMA producer, six stages of 64 contraction elements
+//   warp 0      TMA producer, 192 KB of stages of 64 contraction elements
 //   warp 1      TMEM allocator; in the pair's first CTA, issuer of the MMAs
 //   warps 2-9   epilogue: TMEM lane = tile row, each half of the warps takes
 //               half of the columns
@@ -15,7 +15,14 @@
 // accumulators of kLongSteps steps each, in registers, because a sum inside the
 // tensor cores loses digits as it grows longer (relative error of weight
 // gradients: 0.24e-6 over 256 terms, 0.48e-6 over 512, 1.0e-6 over 1024, 2.1e-6
-// over 2048).
+// over 2048; 8192 x 5120 -> 2048's gradients take 238 us with sums of 2048, 254
+// with sums of 512).
+//
+// Bound by the tensor pipe: 8192 x 4096 -> 2 x 10240 (the gated pair, both
+// pre-activations kept) in 770 to 880 us over boxes, 1780 to 1560 TFLOP/s, where
+// the power limit sets the clock (a library product alone: 1946 for a moment,
+// 1740 sustained).  Smaller products lose their last round of tiles: 4096^3 in
+// 86 us (1600 TFLOP/s) with four rounds of 224 columns.
 #include "tgemm_dev.cuh"
 
 namespace sadmm {
@@ -24,7 +31,7 @@ namespace {
 constexpr int kPairThreads = 320;
 constexpr int kPairStages = 10;          // at most
 constexpr int kPairSmem = 192 * 1024;    // of stages
-constexpr int kLongSteps = 8;           // 512 contraction elements
+constexpr int kLongSteps = 12;          // 768 contraction elements
 
 // ------------------------------------------------------------- device PTX --
 

@@ -2,8 +2,9 @@
 
 The functions named like the C entry points (``sadmm_*``) marshal arguments and
 nothing else: every step of the path runs in the CUDA library.  The torch
-helpers at the end (``project_groups``, ``PrunedConv``) only allocate device
-memory with torch and pass raw pointers and the current stream through.
+helpers at the end (``project_groups``, ``PrunedConv``, and the feed-forward
+functions ``layer_norm``, ``linear``, ``gated``) only allocate device memory with
+torch and pass raw pointers and the current stream through.
 
 There is no CPU fallback: when the library cannot be built or loaded, every
 call raises.
