@@ -18,6 +18,11 @@
 // which leave their sums in shared memory and add each other's up in rank
 // order, so that results do not depend on timing and no scratch memory is
 // needed.
+//
+// Bound by latency at the sizes that come here: a launch takes 6 us beside its
+// steps (first loads, joining, the last stores).  777 x 2736 -> 1024 takes 13.2 us,
+// 1024^3 10, 17 tokens of 8192 -> 8192 26.6 (their weights alone 20), the gated
+// pair of 17 tokens 2048 -> 2 x 5464 11.
 #include "tgemm_dev.cuh"
 
 namespace sadmm {
