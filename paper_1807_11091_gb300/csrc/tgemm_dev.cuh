@@ -22,7 +22,9 @@ namespace {
 constexpr int kBox = 8192;        // one 64 x 64 bf16 box
 constexpr int kPTile = 2 * kBox;  // 128 rows x 64
 constexpr int kTgProducts = 3;    // products of a launch, at most
-constexpr int kTgMaps = 7;        // and their tensor maps
+// and their tensor maps: a gated pair's gradients have four for the sum of dx, and two for either weights' gradient,
+// which share x's only where x is the Q side (tiles not swapped)
+constexpr int kTgMaps = 8;
 
 // One product of a launch.  The P side is the tile's 128-row side: the output's
 // rows, or its columns where the tiles are swapped.
