@@ -251,26 +251,36 @@ PyObject* wrap_all(const Output (&o)[N])
 
 // ------------------------------------------------------------------ stream --
 
-// The call's device, stream and scratch.  A stream other than torch's current
-// one (given as its handle) is recorded on every tensor allocated here, so that
-// their memory is not handed out before its kernels are done.
+// The call's device, stream and scratch.  A stream other than torch's current one
+// (given as its handle) is the current one while the call allocates: a block of the
+// allocator's pool of another stream may be one that this stream's kernels, already
+// enqueued, still use.  What the call is given is recorded on the stream, and what it
+// returns on the caller's, where it will be read, so that neither's memory is handed
+// out while it is in use there.  That the inputs are ready on the stream is for the
+// caller to see to.
 struct Call {
     c10::cuda::OptionalCUDAGuard guard;
+    c10::cuda::OptionalCUDAStreamGuard current;
     at::AutoDispatchBelowADInplaceOrView no_autograd;
     c10::Device device;
     bool other;
     cudaStream_t stream;
+    std::optional<c10::cuda::CUDAStream> callers, own;
     Tensor scratch;
 
-    Call(const Tensor& t, PyObject* s) : device(t.device()), other(s != Py_None)
+    Call(const Tensor& t, PyObject* s) : device(t.device()), other(false)
     {
         if (device.index() != c10::cuda::current_device()) guard.set_device(device);
-        if (other) {
-            stream = static_cast<cudaStream_t>(PyLong_AsVoidPtr(s));
-            if (PyErr_Occurred()) throw PythonError();
-        } else {
-            stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
-        }
+        callers = c10::cuda::getCurrentCUDAStream(device.index());
+        stream = callers->stream();
+        if (s == Py_None) return;
+        const cudaStream_t given = static_cast<cudaStream_t>(PyLong_AsVoidPtr(s));
+        if (PyErr_Occurred()) throw PythonError();
+        if (given == stream) return;
+        other = true;
+        stream = given;
+        own = c10::cuda::getStreamFromExternal(given, device.index());
+        current.reset_stream(*own);
     }
     void* workspace(const Tensor& like, size_t bytes)
     {
@@ -279,14 +289,15 @@ struct Call {
         scratch = at::empty_strided(at::IntArrayRef(size, 1), at::IntArrayRef(stride, 1), like.options().dtype(at::kByte));
         return scratch.data_ptr();
     }
+    // Before the launch: the n arguments of the call and its outputs.
     template <int N>
-    void used(const Output (&o)[N]) const
+    void uses(PyObject* const* v, int n, const Output (&o)[N]) const
     {
         if (!other) return;
-        const c10::Stream s = c10::cuda::getStreamFromExternal(stream, device.index()).unwrap();
-        if (scratch.defined()) scratch.record_stream(s);
+        for (int i = 0; i < n; ++i)
+            if (THPVariable_Check(v[i])) THPVariable_Unpack(v[i]).record_stream(own->unwrap());
         for (const Output& x : o)
-            if (x.t.defined()) x.t.record_stream(s);
+            if (x.t.defined()) x.t.record_stream(callers->unwrap());
     }
 };
 
@@ -331,8 +342,8 @@ PyObject* layer_norm(PyObject* const* v)
     a.ydt = dtype_of(o[0].t.scalar_type(), "out");
     a.mean = static_cast<float*>(o[1].p);
     a.rstd = static_cast<float*>(o[2].p);
+    call.uses(v, 8, o);
     ok(entry.layernorm_fwd(&a, call.stream), "sadmm_layernorm_fwd");
-    call.used(o);
     return stats ? wrap_all(o) : wrap(o[0]);
 }
 
@@ -369,8 +380,8 @@ PyObject* layer_norm_backward(PyObject* const* v)
     a.dbeta = static_cast<float*>(o[2].p);
     const size_t n = entry.layernorm_bwd_size(&a);
     void* ws = call.workspace(x, n);
+    call.uses(v, 10, o);
     ok(entry.layernorm_bwd(&a, ws, n, call.stream), "sadmm_layernorm_bwd");
-    call.used(o);
     return wrap_all(o);
 }
 
@@ -409,8 +420,8 @@ PyObject* linear(PyObject* const* v)
     a.ldz = o[1].ld;
     const size_t n = apart(m) || apart(w) ? entry.linear_fwd_size(&a) : 0;
     void* ws = call.workspace(x, n);
+    call.uses(v, 9, o);
     ok(entry.linear_fwd(&a, ws, n, call.stream), "sadmm_linear_fwd");
-    call.used(o);
     return save ? wrap_all(o) : wrap(o[0]);
 }
 
@@ -457,8 +468,8 @@ PyObject* linear_backward(PyObject* const* v)
     a.db = static_cast<float*>(o[2].p);
     const size_t n = entry.linear_bwd_size(&a);
     void* ws = call.workspace(x, n);
+    call.uses(v, 11, o);
     ok(entry.linear_bwd(&a, ws, n, call.stream), "sadmm_linear_bwd");
-    call.used(o);
     return wrap_all(o);
 }
 
@@ -499,8 +510,8 @@ PyObject* gated(PyObject* const* v)
     a.ldu = o[2].ld;
     const size_t n = apart(m) || apart(wg) || apart(wu) ? entry.gated_fwd_size(&a) : 0;
     void* ws = call.workspace(x, n);
+    call.uses(v, 9, o);
     ok(entry.gated_fwd(&a, ws, n, call.stream), "sadmm_gated_fwd");
-    call.used(o);
     return save ? wrap_all(o) : wrap(o[0]);
 }
 
@@ -555,8 +566,8 @@ PyObject* gated_backward(PyObject* const* v)
     a.dbu = static_cast<float*>(o[4].p);
     const size_t n = entry.gated_bwd_size(&a);
     void* ws = call.workspace(x, n);
+    call.uses(v, 13, o);
     ok(entry.gated_bwd(&a, ws, n, call.stream), "sadmm_gated_bwd");
-    call.used(o);
     return wrap_all(o);
 }
 

@@ -756,6 +756,9 @@ def pack_batch(convs, stream=None) -> None:
 # output of odd width are rows on 32-byte boundaries, so that the next call
 # reads them where they lie: such an output is a view of a wider buffer.  A bad
 # argument raises TypeError or ValueError here, or SadmmError from the library.
+# With `stream` the call's kernels, outputs and scratch are that stream's: its
+# inputs have to be ready there, and whoever reads its outputs on another stream
+# has that one wait.
 # The checks, outputs and scratch are those of csrc/torch_ffn.cpp, because on a
 # few tokens they are what a call costs.
 
