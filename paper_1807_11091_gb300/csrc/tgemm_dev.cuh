@@ -254,7 +254,7 @@ SADMM_DEV void load_n(const Out& o, long long r, long long c, long long n, float
     }
 }
 
-// Sixteen columns of one output row: sb / sb2 are the tile's biases in shared memory.
+// Sixteen columns of one output row: sb / sb2 are their biases in shared memory.
 template <bool GATED>
 SADMM_DEV void finish16(const TgArgs& a, const TgProduct& p, long long r, long long c, float (&v)[16], float (&w)[16],
                         const float* sb, const float* sb2)

@@ -90,8 +90,6 @@ SADMM_DEV void mbar_arrive_cluster(uint32_t bar)
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-SADMM_DEV void epi_sync_pair() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
 // ------------------------------------------------------------------ kernel --
 
 // The k-th tile of pair i of n: the tiles of the longest contraction (the first
@@ -147,7 +145,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     __shared__ uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_holder;
     __shared__ volatile int abort_flag;
-    __shared__ __align__(16) float s_bias[2][256];  // by tile parity; gated: the second half is u's
+    // each epilogue warp's columns (gated: of g, then of u): its own copy, so that no warp waits for another, which
+    // may have given up its wait for an accumulator and left the loop over tiles
+    __shared__ __align__(16) float s_bias[8][128];
     // warp-uniform to the compiler, which keeps the issue loop's descriptors in uniform registers: an MMA and its
     // stage then cost less to issue than to run (4096^3: 86.5 -> 83.7 us)
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -271,27 +271,26 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
         const int cols = GATED ? half : a.bn;        // output columns of a tile
         const int c_begin = part * (cols >> 1), c_end = c_begin + (cols >> 1);
-        int buf = 0, parity = 0;
+        float* sb = s_bias[warp - 2];
+        int buf = 0;
         uint32_t bphase = 0;
         bool ok = true;
-        for (int i = 0, t; ok && (t = tile_of(a, me, pairs, i)) >= 0; ++i, parity ^= 1) {
+        for (int i = 0, t; ok && (t = tile_of(a, me, pairs, i)) >= 0; ++i) {
             const Place pl = place(a, t);
             const TgProduct& p = a.prod[pl.prod];
             const long long row = (long long)pl.mt * 256 + rank * 128 + q * 32 + lane;
             const long long col0 = (long long)pl.nt * cols;
             const int live = (int)min((long long)cols, p.n - col0);  // columns inside the output
             if (a.bias || a.bias2) {
-                const int j = threadIdx.x - 64;
-                float b = 0.0f;
-                if (j < cols) {
-                    if (a.bias && j < live) b = a.bias[col0 + j];
-                } else if (GATED && j < 2 * cols && a.bias2 && j - cols < live) {
-                    b = a.bias2[col0 + j - cols];
+                __syncwarp();  // the last tile's have been read
+#pragma unroll
+                for (int j = lane; j < 128; j += 32) {
+                    const int at = GATED ? j & 63 : j, c = c_begin + at;
+                    const float* from = GATED && j >= 64 ? a.bias2 : a.bias;
+                    sb[j] = from && c < c_end && c < live ? from[col0 + c] : 0.0f;
                 }
-                s_bias[parity][j] = b;
-                epi_sync_pair();
+                __syncwarp();
             }
-            const float* sb = s_bias[parity];
             float sum[LONG ? 8 : 1][16];
             for (int k = 0; k < p.nk; k += LONG ? p.steps : p.nk) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], bphase, &abort_flag, a.status));
@@ -312,7 +311,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                                 sum[h][j] = k ? sum[h][j] + __uint_as_float(r[j]) : __uint_as_float(r[j]);
                             if (last && row < p.m && c < live) {
                                 float w[16];
-                                finish16<false>(a, p, row, col0 + c, sum[h], w, sb + c, sb);
+                                finish16<false>(a, p, row, col0 + c, sum[h], w, sb + 16 * h, sb);
                             }
                         }
                     }
@@ -328,7 +327,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                             v[j] = __uint_as_float(rv[j]);
                             w[j] = GATED ? __uint_as_float(rw[j]) : 0.0f;
                         }
-                        if (row < p.m) finish16<GATED>(a, p, row, col0 + c, v, w, sb + c, sb + cols + c);
+                        if (row < p.m) finish16<GATED>(a, p, row, col0 + c, v, w, sb + c - c_begin, sb + 64 + c - c_begin);
                     }
                 }
                 tc_fence_before();
