@@ -28,9 +28,9 @@ struct Copies {
     int cols[3];
 };
 
-// Matrix blockIdx.y, a warp a row's 1024 elements (segment blockIdx.z), a lane 8
-// elements (16 bytes) at a time, all in flight together.  Inside
-// a row they come from the two aligned 16-byte words that hold them (funnel
+// Matrix blockIdx.y, a warp a row's 1024 elements (segments blockIdx.z, blockIdx.z +
+// gridDim.z, ...), a lane 8 elements (16 bytes) at a time, all in flight together.
+// Inside a row they come from the two aligned 16-byte words that hold them (funnel
 // shifts), at the row's ends one by one.
 __global__ void __launch_bounds__(256) k_realign(const Copies a)
 {
@@ -46,30 +46,32 @@ __global__ void __launch_bounds__(256) k_realign(const Copies a)
         const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) >> 1);
         const uint4* from = reinterpret_cast<const uint4*>(row - off);
         const int sh = (off & 1) * 16, w0 = off >> 1;
+        for (int z = blockIdx.z * 128 + lane; z < words; z += gridDim.z * 128) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int i = (blockIdx.z * 4 + k) * 32 + lane;
-            if (i >= words) break;
-            const int c = i * 8;
-            uint4 o;
-            if (c >= off && c + 16 <= cols) {
-                const uint4 lo = __ldg(from + i), hi = __ldg(from + i + 1);
-                // words w0 .. w0 + 4 of the eight (w0 is the row's: the same for the warp)
-                uint32_t v0, v1, v2, v3, v4;
-                if (w0 == 0) v0 = lo.x, v1 = lo.y, v2 = lo.z, v3 = lo.w, v4 = hi.x;
-                else if (w0 == 1) v0 = lo.y, v1 = lo.z, v2 = lo.w, v3 = hi.x, v4 = hi.y;
-                else if (w0 == 2) v0 = lo.z, v1 = lo.w, v2 = hi.x, v3 = hi.y, v4 = hi.z;
-                else v0 = lo.w, v1 = hi.x, v2 = hi.y, v3 = hi.z, v4 = hi.w;
-                o = make_uint4(__funnelshift_r(v0, v1, sh), __funnelshift_r(v1, v2, sh), __funnelshift_r(v2, v3, sh),
-                               __funnelshift_r(v3, v4, sh));
-            } else {
-                uint32_t e[8];
+            for (int k = 0; k < 4; ++k) {
+                const int i = z + 32 * k;
+                if (i >= words) break;
+                const int c = i * 8;
+                uint4 o;
+                if (c >= off && c + 16 <= cols) {
+                    const uint4 lo = __ldg(from + i), hi = __ldg(from + i + 1);
+                    // words w0 .. w0 + 4 of the eight (w0 is the row's: the same for the warp)
+                    uint32_t v0, v1, v2, v3, v4;
+                    if (w0 == 0) v0 = lo.x, v1 = lo.y, v2 = lo.z, v3 = lo.w, v4 = hi.x;
+                    else if (w0 == 1) v0 = lo.y, v1 = lo.z, v2 = lo.w, v3 = hi.x, v4 = hi.y;
+                    else if (w0 == 2) v0 = lo.z, v1 = lo.w, v2 = hi.x, v3 = hi.y, v4 = hi.z;
+                    else v0 = lo.w, v1 = hi.x, v2 = hi.y, v3 = hi.z, v4 = hi.w;
+                    o = make_uint4(__funnelshift_r(v0, v1, sh), __funnelshift_r(v1, v2, sh), __funnelshift_r(v2, v3, sh),
+                                   __funnelshift_r(v3, v4, sh));
+                } else {
+                    uint32_t e[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    e[j] = c + j < cols ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + j) : 0u;
-                o = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                    for (int j = 0; j < 8; ++j)
+                        e[j] = c + j < cols ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + j) : 0u;
+                    o = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                }
+                to[i] = o;
             }
-            to[i] = o;
         }
     }
 }
@@ -353,7 +355,9 @@ struct Filler {
     {
         if (!n) return SADMM_OK;
         const long long blocks = (rows + 7) / 8, most = 8ll * device_sm_count();
-        const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)n, (unsigned)((widest + 1023) / 1024));
+        const long long segments = (widest + 1023) / 1024;
+        const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)n,
+                        (unsigned)(segments < 65535 ? segments : 65535));
         return launch_pdl(k_realign, grid, dim3(256), 0, s, c) == cudaSuccess
                    ? SADMM_OK
                    : SADMM_ECUDA;
