@@ -19,6 +19,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <optional>
 #include <stdexcept>
 #include <string>
@@ -82,6 +83,25 @@ const Tensor& tensor(PyObject* o, const char* name)
     if (!t.is_cuda()) fail(PyExc_TypeError, std::string(name) + " must be a CUDA tensor");
     return t;
 }
+
+// The call's x.  Its other tensors have to be on the same device, where the kernels
+// run that are handed their pointers.
+struct Named {
+    PyObject* o;
+    const char* name;
+};
+const Tensor& first(PyObject* o, std::initializer_list<Named> others)
+{
+    const Tensor& x = tensor(o, "x");
+    for (const Named& n : others) {
+        if (n.o == Py_None) continue;
+        const Tensor& t = tensor(n.o, n.name);
+        if (t.device() != x.device())
+            fail(PyExc_ValueError, std::string(n.name) + " is on " + t.device().str() + ", x on " + x.device().str());
+    }
+    return x;
+}
+
 const Tensor* tensor_or_none(PyObject* o, const char* name) { return o == Py_None ? nullptr : &tensor(o, name); }
 
 ScalarType dtype_arg(PyObject* o, ScalarType otherwise)
@@ -315,7 +335,7 @@ int width(int64_t n)
 // x, gamma, beta, eps, out_dtype, stats, out, stream
 PyObject* layer_norm(PyObject* const* v)
 {
-    const Tensor& x = tensor(v[0], "x");
+    const Tensor& x = first(v[0], {{v[1], "gamma"}, {v[2], "beta"}, {v[6], "out"}});
     const Matrix m = matrix(x, "x");
     const double eps = PyFloat_AsDouble(v[3]);
     if (eps == -1.0 && PyErr_Occurred()) throw PythonError();
@@ -350,7 +370,7 @@ PyObject* layer_norm(PyObject* const* v)
 // dy, x, mean, rstd, gamma, dres, want_dx, want_dgamma, want_dbeta, stream
 PyObject* layer_norm_backward(PyObject* const* v)
 {
-    const Tensor& x = tensor(v[1], "x");
+    const Tensor& x = first(v[1], {{v[0], "dy"}, {v[2], "mean"}, {v[3], "rstd"}, {v[4], "gamma"}, {v[5], "dres"}});
     const Matrix m = matrix(x, "x");
     const Matrix dy = matrix_of(tensor(v[0], "dy"), "dy", m.rows, m.cols, std::nullopt);
     Matrix dres;
@@ -388,7 +408,7 @@ PyObject* layer_norm_backward(PyObject* const* v)
 // x, W, bias, residual, act, out_dtype, save, out, stream
 PyObject* linear(PyObject* const* v)
 {
-    const Tensor& x = tensor(v[0], "x");
+    const Tensor& x = first(v[0], {{v[1], "W"}, {v[2], "bias"}, {v[3], "residual"}, {v[7], "out"}});
     const Matrix m = matrix_of(x, "x", -1, x.dim() ? x.size(-1) : 0, at::kBFloat16);
     const Matrix w = matrix_of(tensor(v[1], "W"), "W", -1, m.cols, at::kBFloat16);
     const Tensor* residual = tensor_or_none(v[3], "residual");
@@ -428,11 +448,12 @@ PyObject* linear(PyObject* const* v)
 // dy, x, W, z, act, want_dx, want_dw, want_db, dx_dtype, dw_dtype, stream
 PyObject* linear_backward(PyObject* const* v)
 {
-    const Tensor &dyt = tensor(v[0], "dy"), &x = tensor(v[1], "x"), &wt = tensor(v[2], "W");
+    const int act = number(v[4]);
+    const Tensor& x = first(v[1], {{v[0], "dy"}, {v[2], "W"}, {act != SADMM_ACT_NONE ? v[3] : Py_None, "z"}});
+    const Tensor &dyt = tensor(v[0], "dy"), &wt = tensor(v[2], "W");
     const Matrix dy = matrix(dyt, "dy");
     const Matrix m = matrix_of(x, "x", dy.rows, x.dim() ? x.size(-1) : 0, at::kBFloat16);
     const Matrix w = matrix_of(wt, "W", dy.cols, m.cols, at::kBFloat16);
-    const int act = number(v[4]);
     Matrix z;
     if (act != SADMM_ACT_NONE) {
         if (v[3] == Py_None) fail(PyExc_TypeError, "the gradient of an activation needs z");
@@ -476,7 +497,7 @@ PyObject* linear_backward(PyObject* const* v)
 // x, Wg, Wu, bg, bu, act, save, out, stream
 PyObject* gated(PyObject* const* v)
 {
-    const Tensor& x = tensor(v[0], "x");
+    const Tensor& x = first(v[0], {{v[1], "Wg"}, {v[2], "Wu"}, {v[3], "bg"}, {v[4], "bu"}, {v[7], "out"}});
     const Matrix m = matrix_of(x, "x", -1, x.dim() ? x.size(-1) : 0, at::kBFloat16);
     const Matrix wg = matrix_of(tensor(v[1], "Wg"), "Wg", -1, m.cols, at::kBFloat16);
     const Matrix wu = matrix_of(tensor(v[2], "Wu"), "Wu", wg.rows, m.cols, at::kBFloat16);
@@ -518,7 +539,8 @@ PyObject* gated(PyObject* const* v)
 // dh, x, Wg, Wu, g, u, act, want_dx, want_dw, want_db, dx_dtype, dw_dtype, stream
 PyObject* gated_backward(PyObject* const* v)
 {
-    const Tensor &dht = tensor(v[0], "dh"), &x = tensor(v[1], "x"), &wgt = tensor(v[2], "Wg"), &wut = tensor(v[3], "Wu");
+    const Tensor& x = first(v[1], {{v[0], "dh"}, {v[2], "Wg"}, {v[3], "Wu"}, {v[4], "g"}, {v[5], "u"}});
+    const Tensor &dht = tensor(v[0], "dh"), &wgt = tensor(v[2], "Wg"), &wut = tensor(v[3], "Wu");
     const Matrix m = matrix_of(x, "x", -1, x.dim() ? x.size(-1) : 0, at::kBFloat16);
     const Matrix dh = matrix_of(dht, "dh", m.rows, dht.dim() ? dht.size(-1) : 0, at::kBFloat16);
     const Matrix wg = matrix_of(wgt, "Wg", dh.cols, m.cols, at::kBFloat16);
