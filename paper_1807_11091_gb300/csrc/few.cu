@@ -31,6 +31,7 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 constexpr int kFewWarps = 8;
+constexpr int kLongRuns = 64;  // pieces of 32 elements until two accumulators have 1024 terms each
 
 struct FewArgs {
     const bf16* x;
@@ -250,8 +251,11 @@ SADMM_DEV void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, ui
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// NT times 8 tokens at most.  fp32 sums alternate between two accumulators.
-template <int NT, bool GATED, bool ALIGNED>
+// NT times 8 tokens at most.  fp32 sums alternate between two accumulators.  LONG:
+// these join the warp's sum in shared memory after 1024 terms each, because a sum
+// inside the MMAs loses about 1e-9 of itself per term.  For long fp32 outputs alone:
+// a bf16 one does not show it, and the loop is some 5 % slower with the joins in it.
+template <int NT, bool GATED, bool ALIGNED, bool LONG>
 __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant__ FewArgs a)
 {
     constexpr int M = GATED ? 2 : 1;  // weight matrices
@@ -293,12 +297,35 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
                 mma_16x8(d[which][m][q], w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w, x[q].z, x[q].w);
             }
     };
+    // lane (g, t) holds rows g, g + 8 and tokens 2t, 2t + 1 (of each eight)
+    bool begun = false;  // whether the warp's sum has
+    auto join_sums = [&]() {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float& sum = red[warp][m][g + (j >> 1) * 8][8 * q + 2 * t + (j & 1)];
+                    const float v = d[0][m][q][j] + d[1][m][q][j];
+                    sum = LONG && begun ? sum + v : v;
+                    d[0][m][q][j] = d[1][m][q][j] = 0.0f;
+                }
+        begun = true;
+    };
+    int runs = 0;  // since they were joined
+    auto count_run = [&]() {
+        if (!LONG || runs++ < kLongRuns / kAhead) return;
+        join_sums();
+        runs = 1;
+    };
     // a warp takes runs of 32 kAhead elements, `share` warps in turn
     const int step = a.share * 32 * kAhead;
     int c = part * 32 * kAhead;
     if constexpr (ALIGNED) {
-#pragma unroll 2
+#pragma unroll (LONG ? 1 : 2)
         for (; c + 32 * kAhead <= a.n_in; c += step) {
+            count_run();
             uint4 w[kAhead][M][2], x[kAhead][NT];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -319,6 +346,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
     constexpr int kBatch = ALIGNED || kAhead == 2 ? kAhead : kAhead / 2;
 #pragma unroll 1
     for (; c < a.n_in; c += step) {
+        count_run();
 #pragma unroll 1
         for (int i0 = 0; i0 < kAhead && c + 32 * i0 < a.n_in; i0 += kBatch) {
             Words w[kBatch][M][2], x[kBatch][NT];
@@ -350,14 +378,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
             }
         }
     }
-    // lane (g, t) holds rows g, g + 8 and tokens 2t, 2t + 1 (of each eight)
-#pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-        for (int q = 0; q < NT; ++q)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                red[warp][m][g + (j >> 1) * 8][8 * q + 2 * t + (j & 1)] = d[0][m][q][j] + d[1][m][q][j];
+    join_sums();
     __syncthreads();
     // consecutive threads take consecutive outputs of a token
     for (int i = threadIdx.x; i < groups * 16 * a.tokens; i += kFewWarps * 32) {
@@ -397,9 +418,17 @@ sadmm_status run(FewArgs& a, bool aligned, cudaStream_t s)
     a.share = 1;
     while (a.share < kFewWarps && groups * a.share < 8ll * device_sm_count()) a.share *= 2;
     const int per = kFewWarps / a.share;
-    void (*kernel)(FewArgs) = k_few<NT, GATED, true>;
+    void (*kernel)(FewArgs) = k_few<NT, GATED, true, false>;
     if constexpr (NT == 1) {
-        if (!aligned) kernel = k_few<NT, GATED, false>;
+        if (!aligned) kernel = k_few<NT, GATED, false, false>;
+    }
+    if constexpr (!GATED) {
+        if (!a.y.bf16 && a.n_in > 32 * kLongRuns * a.share) {
+            kernel = k_few<NT, GATED, true, true>;
+            if constexpr (NT == 1) {
+                if (!aligned) kernel = k_few<NT, GATED, false, true>;
+            }
+        }
     }
     return launch_pdl(kernel, dim3((unsigned)((groups + per - 1) / per)), dim3(kFewWarps * 32), 0, s, a) == cudaSuccess
                ? SADMM_OK
