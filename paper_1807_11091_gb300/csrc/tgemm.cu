@@ -17,7 +17,11 @@
 // tiles are few or uneven the contraction is cut over the CTAs of a cluster,
 // which leave their sums in shared memory and add each other's up in rank
 // order, so that results do not depend on timing and no scratch memory is
-// needed.
+// needed.  Where eight CTAs are not enough to keep an fp32 output's sums inside the
+// tensor cores to 1024 terms (LONG), these go to registers by kLongSteps steps,
+// through two accumulators in turn (dW of 64 units over 65536 tokens in one sum of
+// 8192 a CTA: off by 9.1e-6 in norm, so by 0.72e-6; 40 tokens of 16384 -> 5000: 50.1
+// us and 52.7).
 //
 // Bound by latency at the sizes that come here: a launch takes 6 us beside its
 // steps (first loads, joining, the last stores).  777 x 2736 -> 1024 takes 13.2 us,
@@ -33,13 +37,13 @@ constexpr int kMaxStages = 8;
 constexpr int kPrefetchSteps = 32;
 constexpr int kSwapStride = 132;  // floats of a staged row of 128, so that neither way in or out has bank conflicts
 
-template <bool SWAP, bool GATED>
-__global__ void __launch_bounds__(kThreads, 2)
+template <bool SWAP, bool GATED, bool LONG>
+__global__ void __launch_bounds__(kThreads, LONG ? 1 : 2)
     k_tgemm(const __grid_constant__ TgMaps maps, const __grid_constant__ TgArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full, drain;
+    __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_holder;
     __shared__ volatile int abort_flag;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;  // uniform
@@ -59,7 +63,10 @@ __global__ void __launch_bounds__(kThreads, 2)
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
-        mbar_init(&acc_full, 1);
+        for (int b = 0; b < (LONG ? 2 : 1); ++b) {
+            mbar_init(&acc_full[b], 1);
+            if (LONG) mbar_init(&acc_empty[b], 4);  // the warps that read the sums
+        }
         mbar_init(&drain, 1);
         abort_flag = 0;
         fence_mbar_init();
@@ -124,24 +131,37 @@ __global__ void __launch_bounds__(kThreads, 2)
     } else if (warp == 1) {
         const uint32_t pstep = p.p_kmajor ? 2u : 128u, qstep = p.q_kmajor ? 2u : 128u;  // 16 elements, in 16 bytes
         bool ok = true;
-        int s = 0;
-        uint32_t phase = 0;
+        int s = 0, buf = 0, held = 0;  // LONG: the accumulator and its steps
+        uint32_t phase = 0, bphase = 0, d = tmem;
         for (int i = 0; i < nk; ++i) {
+            if constexpr (LONG) {
+                ok = held != 0 || mbar_wait_warp(&acc_empty[buf], bphase ^ 1u, &abort_flag, a.status);
+                if (!ok) break;
+                d = tmem + (uint32_t)buf * a.acc_cols;
+            }
             if (!mbar_wait_warp(&full[s], phase, &abort_flag, a.status)) { ok = false; break; }
             tc_fence_after();
             const uint32_t st = smem_u32(smem + (size_t)s * a.stage_bytes);
             const uint64_t pd = sdesc(st, p.p_kmajor), qd = sdesc(st + a.q_off, p.q_kmajor);
+            const int before = LONG ? held : i;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                mma_bf16_ss_elect(tmem, pd + kk * pstep, qd + kk * qstep, p.idesc, (i | kk) != 0);
+                mma_bf16_ss_elect(d, pd + kk * pstep, qd + kk * qstep, p.idesc, (before | kk) != 0);
                 if (GATED && SWAP)
-                    mma_bf16_ss_elect(tmem + a.bn, pd + (kPTile >> 4) + kk * pstep, qd + kk * qstep, p.idesc,
-                                      (i | kk) != 0);
+                    mma_bf16_ss_elect(d + a.bn, pd + (kPTile >> 4) + kk * pstep, qd + kk * qstep, p.idesc,
+                                      (before | kk) != 0);
             }
             mma_commit_elect(&empty[s]);
             if (++s == a.stages) { s = 0; phase ^= 1u; }
+            if constexpr (LONG) {
+                if (++held == p.acc_steps || i + 1 == nk) {
+                    mma_commit_elect(&acc_full[buf]);
+                    held = 0;
+                    if (++buf == 2) { buf = 0; bphase ^= 1u; }
+                }
+            }
         }
-        if (ok) mma_commit_elect(&acc_full);
+        if (!LONG && ok) mma_commit_elect(&acc_full[0]);
         mma_commit_elect(&drain);
         if (lane == 0) {
             const unsigned long long t0 = globaltimer();
@@ -158,7 +178,54 @@ __global__ void __launch_bounds__(kThreads, 2)
     const int live = (int)min((long long)(SWAP ? a.bn : 128), p.m - (SWAP ? col0 : row0));  // rows
     const uint32_t stride = SWAP ? kSwapStride : a.acc_cols + 4;                             // floats of a staged row
     const uint32_t u_off = SWAP ? (uint32_t)a.bn * kSwapStride : (uint32_t)a.bn;             // gated: from g to u
-    if (warp >= 2 && warp < 6 && __all_sync(0xffffffffu, mbar_wait(&acc_full, 0, &abort_flag, a.status))) {
+    if constexpr (LONG) {  // (not the gated pair)
+        if (warp >= 2 && warp < 6) {
+            const int q = warp & 3, trow = q * 32 + lane, columns = SWAP ? live : (int)a.acc_cols;
+            const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
+            float sum[8][16];  // 128 columns at most
+#pragma unroll
+            for (int h = 0; h < 8; ++h)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[h][j] = 0.0f;
+            bool ok = true;
+            int buf = 0;
+            uint32_t bphase = 0;
+            for (int i = 0; i < nk; i += p.acc_steps) {
+                ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], bphase, &abort_flag, a.status));
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int h = 0; h < 8; ++h) {
+                    if (16 * h >= columns) continue;
+                    uint32_t r[16];
+                    tmem_ld_32x32b_x16(taddr + (uint32_t)buf * a.acc_cols + 16 * h, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[h][j] += __uint_as_float(r[j]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                if (++buf == 2) { buf = 0; bphase ^= 1u; }
+            }
+            if (ok) {  // the last accumulator is there, so the stages have been read
+#pragma unroll
+                for (int h = 0; h < 8; ++h) {
+                    if (16 * h >= columns) continue;
+                    if (SWAP) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) part[(16 * h + j) * kSwapStride + trow] = sum[h][j];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4)
+                            *reinterpret_cast<float4*>(part + trow * stride + 16 * h + j) =
+                                make_float4(sum[h][j], sum[h][j + 1], sum[h][j + 2], sum[h][j + 3]);
+                    }
+                }
+            }
+        }
+    }
+    if (!LONG && warp >= 2 && warp < 6 && __all_sync(0xffffffffu, mbar_wait(&acc_full[0], 0, &abort_flag, a.status))) {
         const int q = warp & 3, trow = q * 32 + lane;
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
         tc_fence_after();
@@ -255,13 +322,13 @@ __global__ void __launch_bounds__(kThreads, 2)
 
 // -------------------------------------------------------------------- host --
 
-template <bool SWAP, bool GATED>
+template <bool SWAP, bool GATED, bool LONG>
 sadmm_status run(const TgMaps& maps, const TgArgs& a, size_t smem, cudaStream_t s)
 {
     static bool configured[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
-    auto kern = k_tgemm<SWAP, GATED>;
+    auto kern = k_tgemm<SWAP, GATED, LONG>;
     if (!configured[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 112 * 1024) != cudaSuccess)
             return SADMM_ECUDA;
@@ -309,7 +376,7 @@ int tile_width(const TgProblem* t, int count)
 // the parts 1 us (777 x 2736 -> 1024: 19.9 us whole, 14.1 / 13.5 / 21.5 cut in 2
 // / 4 / 8; 512 x 4096 -> 4096: 27.3, 20.9, 29.2, 47.8).  An fp32 output's
 // contraction is cut anyway, so that no sum inside the tensor cores passes 1024
-// elements where 8 CTAs are enough for that (see tgemm_pair.cu).
+// elements where 8 CTAs are enough for that (elsewhere: LONG).
 struct Cut {
     int splits;
     long long time;
@@ -370,13 +437,19 @@ sadmm_status launch_tiles(const TgProblem* t, int count, int splits, cudaStream_
     a.tiles = (int)tiles;
     a.splits = splits;
     int steps = 1;
+    bool lng = false;
     for (int i = 0; i < count; ++i) {
-        a.prod[i].steps = (a.prod[i].nk + splits - 1) / splits;
-        if (a.prod[i].steps > steps) steps = a.prod[i].steps;
+        TgProduct& p = a.prod[i];
+        p.steps = p.acc_steps = (p.nk + splits - 1) / splits;
+        if (p.steps > steps) steps = p.steps;
+        if (!gated && !p.y.bf16 && p.steps > 16) {
+            p.acc_steps = kLongSteps;
+            lng = true;
+        }
     }
     a.acc_cols = (uint32_t)(gated ? 2 * bn : bn);
     uint32_t cols = 32;
-    while (cols < a.acc_cols) cols <<= 1;
+    while (cols < (lng ? 2 : 1) * a.acc_cols) cols <<= 1;
     a.tmem_cols = cols;
     a.q_off = gated && swap ? 2 * kPTile : kPTile;
     a.stage_bytes = a.q_off + (uint32_t)n_mma * 128u;
@@ -388,8 +461,9 @@ sadmm_status launch_tiles(const TgProblem* t, int count, int splits, cudaStream_
     const size_t staged = 4 * (size_t)(swap ? a.acc_cols * kSwapStride : 128 * (a.acc_cols + 4));
     if (smem < staged) smem = staged;
     smem += 1024;
-    if (gated) return swap ? run<true, true>(maps, a, smem, s) : run<false, true>(maps, a, smem, s);
-    return swap ? run<true, false>(maps, a, smem, s) : run<false, false>(maps, a, smem, s);
+    if (gated) return swap ? run<true, true, false>(maps, a, smem, s) : run<false, true, false>(maps, a, smem, s);
+    if (lng) return swap ? run<true, false, true>(maps, a, smem, s) : run<false, false, true>(maps, a, smem, s);
+    return swap ? run<true, false, false>(maps, a, smem, s) : run<false, false, false>(maps, a, smem, s);
 }
 
 }  // namespace

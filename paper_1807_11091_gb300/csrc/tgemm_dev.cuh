@@ -26,6 +26,12 @@ constexpr int kTgProducts = 3;    // products of a launch, at most
 // which share x's only where x is the Q side (tiles not swapped)
 constexpr int kTgMaps = 8;
 
+// fp32 outputs of long contractions (LONG) are added up over accumulators of
+// kLongSteps steps each, in registers, because a sum inside the tensor cores loses
+// digits as it grows longer (relative error of weight gradients: 0.24e-6 over 256
+// terms, 0.48e-6 over 512, 1.0e-6 over 1024, 2.1e-6 over 2048).
+constexpr int kLongSteps = 12;  // 768 contraction elements
+
 // One product of a launch.  The P side is the tile's 128-row side: the output's
 // rows, or its columns where the tiles are swapped.
 struct TgProduct {
@@ -34,7 +40,8 @@ struct TgProduct {
     int first;                 // its first tile
     int p_tiles, q_tiles;
     int nk0, nk;               // 64-element contraction steps: of the first summand, of all
-    int steps;                 // steps of each CTA of a cluster (tgemm.cu), of an accumulator (tgemm_pair.cu)
+    int steps;                 // steps of each CTA of a cluster (tgemm.cu)
+    int acc_steps;             // steps that an accumulator holds before it is added to the sums in registers
     int pm, qm;                // maps; the second summand's (gated: the second weights') follow
     int p_kmajor, q_kmajor;
     uint32_t idesc;

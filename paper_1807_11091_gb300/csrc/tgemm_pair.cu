@@ -11,12 +11,9 @@
 //   warps 2-9   epilogue: TMEM lane = tile row, each half of the warps takes
 //               half of the columns
 // Two accumulators in TMEM: a tile's epilogue runs beside the next tile's
-// products.  fp32 outputs of long contractions (LONG) are added up over
-// accumulators of kLongSteps steps each, in registers, because a sum inside the
-// tensor cores loses digits as it grows longer (relative error of weight
-// gradients: 0.24e-6 over 256 terms, 0.48e-6 over 512, 1.0e-6 over 1024, 2.1e-6
-// over 2048; 8192 x 5120 -> 2048's gradients take 238 us with sums of 2048, 254
-// with sums of 512).
+// products.  fp32 outputs of long contractions (LONG) are added up in registers
+// over accumulators of kLongSteps steps each (8192 x 5120 -> 2048's gradients take
+// 238 us with sums of 2048 terms, 254 with sums of 512).
 //
 // Bound by the tensor pipe: 8192 x 4096 -> 2 x 10240 (the gated pair, both
 // pre-activations kept) in 770 to 880 us over boxes, 1780 to 1560 TFLOP/s, where
@@ -31,7 +28,6 @@ namespace {
 constexpr int kPairThreads = 320;
 constexpr int kPairStages = 10;          // at most
 constexpr int kPairSmem = 192 * 1024;    // of stages
-constexpr int kLongSteps = 12;          // 768 contraction elements
 
 // ------------------------------------------------------------- device PTX --
 
@@ -238,7 +234,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 const int p_kmajor = p.p_kmajor, q_kmajor = p.q_kmajor, nk = p.nk;
                 const uint32_t idesc = p.idesc;
                 for (int k = 0; k < nk && ok;) {
-                    const int k1 = LONG ? min(k + p.steps, nk) : nk;
+                    const int k1 = LONG ? min(k + p.acc_steps, nk) : nk;
                     if (!mbar_wait_warp(&acc_empty[buf], bphase ^ 1u, &abort_flag, a.status)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem + (uint32_t)buf * 256u;
@@ -292,13 +288,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 __syncwarp();
             }
             float sum[LONG ? 8 : 1][16];
-            for (int k = 0; k < p.nk; k += LONG ? p.steps : p.nk) {
+            for (int k = 0; k < p.nk; k += LONG ? p.acc_steps : p.nk) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], bphase, &abort_flag, a.status));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t acc = taddr + (uint32_t)buf * 256u;
                 if (LONG) {
-                    const bool last = k + p.steps >= p.nk;
+                    const bool last = k + p.acc_steps >= p.nk;
 #pragma unroll
                     for (int h = 0; h < 8; ++h) {
                         const int c = c_begin + 16 * h;
@@ -327,7 +323,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                             v[j] = __uint_as_float(rv[j]);
                             w[j] = GATED ? __uint_as_float(rw[j]) : 0.0f;
                         }
-                        if (row < p.m) finish16<GATED>(a, p, row, col0 + c, v, w, sb + c - c_begin, sb + 64 + c - c_begin);
+                        const float* b = sb + c - c_begin;
+                        if (row < p.m) finish16<GATED>(a, p, row, col0 + c, v, w, b, b + 64);
                     }
                 }
                 tc_fence_before();
@@ -496,9 +493,9 @@ sadmm_status launch_tgemm_pair(const TgProblem* problems, int count, int bn, cud
                             i ? &t[i - 1] : nullptr))
             return SADMM_ECUDA;
         p.idesc = idesc_bf16_f32(256, bn) | (p.p_kmajor ? 0u : 1u << 15) | (p.q_kmajor ? 0u : 1u << 16);
-        p.steps = p.nk;
+        p.acc_steps = p.nk;
         if (!gated && !p.y.bf16 && p.nk > kLongSteps) {
-            p.steps = kLongSteps;
+            p.acc_steps = kLongSteps;
             lng = true;
         }
         boxes = boxes || !p.q_kmajor;
