@@ -3,6 +3,8 @@
 // Nothing is enqueued before every argument has been checked.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "internal.h"
 
 namespace sadmm {
@@ -23,6 +25,26 @@ bool matrix(const void* p, int dt, long long ld, long long cols)
 bool matrix_or_null(const void* p, int dt, long long ld, long long cols) { return !p || matrix(p, dt, ld, cols); }
 bool vec32(const void* p) { return at_element(p, SADMM_FP32); }
 
+// Whether every output given is at an address of its own, apart from the other
+// outputs and the inputs.
+bool distinct(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs)
+{
+    for (const void* const* o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o) continue;
+        for (const void* const* p = outputs.begin(); p != o; ++p)
+            if (*p == *o) return false;
+        for (const void* i : inputs)
+            if (i == *o) return false;
+    }
+    return true;
+}
+
+// An output that may take an input's place: elsewhere, or on the same rows.
+bool in_place(const void* out, long long ldo, const void* in, long long ldi, long long rows)
+{
+    return out != in || ldo == ldi || rows == 1;
+}
+
 constexpr long long kMaxRows = 0x7fffff00ll;   // row tiles and coordinates are 32-bit
 constexpr int kMaxWidth = 1 << 28;
 
@@ -38,8 +60,11 @@ sadmm_status check(const sadmm_layernorm_fwd_args* a)
     const sadmm_status st = extents(a->rows, a->cols, 1);
     if (st != SADMM_OK) return st;
     if (!vec32(a->gamma) || !vec32(a->beta) || !vec32(a->mean) || !vec32(a->rstd)) return SADMM_EINVAL;
-    if (a->rows && (!matrix(a->x, a->xdt, a->ldx, a->cols) || !matrix(a->y, a->ydt, a->ldy, a->cols)))
+    if (!a->rows) return SADMM_OK;
+    if (!matrix(a->x, a->xdt, a->ldx, a->cols) || !matrix(a->y, a->ydt, a->ldy, a->cols)) return SADMM_EINVAL;
+    if (!distinct({a->y, a->mean, a->rstd}, {a->gamma, a->beta}) || !distinct({a->mean, a->rstd}, {a->x}))
         return SADMM_EINVAL;
+    if (a->y == a->x && (a->xdt != a->ydt || !in_place(a->y, a->ldy, a->x, a->ldx, a->rows))) return SADMM_EINVAL;
     return SADMM_OK;
 }
 
@@ -56,7 +81,10 @@ sadmm_status check(const sadmm_layernorm_bwd_args* a)
     if (!a->mean || !a->rstd || !matrix(a->x, a->xdt, a->ldx, a->cols) || !matrix(a->dy, a->dydt, a->lddy, a->cols) ||
         !matrix_or_null(a->dres, a->xdt, a->lddres, a->cols) || !matrix_or_null(a->dx, a->xdt, a->lddx, a->cols))
         return SADMM_EINVAL;
-    if (a->dx && (a->dx == a->x || a->dx == a->dy)) return SADMM_EINVAL;
+    if (!distinct({a->dx, a->dgamma, a->dbeta}, {a->x, a->dy, a->gamma, a->mean, a->rstd}) ||
+        !distinct({a->dgamma, a->dbeta}, {a->dres}))
+        return SADMM_EINVAL;
+    if (a->dres && !in_place(a->dx, a->lddx, a->dres, a->lddres, a->rows)) return SADMM_EINVAL;
     return SADMM_OK;
 }
 
@@ -70,7 +98,8 @@ sadmm_status check(const sadmm_linear_fwd_args* a)
     if (!matrix(a->x, SADMM_BF16, a->ldx, a->n_in) || !matrix(a->y, a->ydt, a->ldy, a->n_out) ||
         !matrix_or_null(a->residual, a->ydt, a->ldr, a->n_out) || !matrix_or_null(a->z, SADMM_BF16, a->ldz, a->n_out))
         return SADMM_EINVAL;
-    if (a->y == a->x || a->y == a->w || a->y == a->z || (a->z && (a->z == a->x || a->z == a->w))) return SADMM_EINVAL;
+    if (!distinct({a->y, a->z}, {a->x, a->w, a->bias}) || !distinct({a->z}, {a->residual})) return SADMM_EINVAL;
+    if (!in_place(a->y, a->ldy, a->residual, a->ldr, a->tokens)) return SADMM_EINVAL;
     return SADMM_OK;
 }
 
@@ -87,8 +116,8 @@ sadmm_status check(const sadmm_linear_bwd_args* a)
     if (a->act != SADMM_ACT_NONE && !matrix(a->z, SADMM_BF16, a->ldz, a->n_out)) return SADMM_EINVAL;
     if (a->dx && !matrix(a->w, SADMM_BF16, a->ldw, a->n_in)) return SADMM_EINVAL;
     if (a->dw && !matrix(a->x, SADMM_BF16, a->ldx, a->n_in)) return SADMM_EINVAL;
-    if (a->dx && (a->dx == a->x || a->dx == a->dy || a->dx == a->w || a->dx == a->z)) return SADMM_EINVAL;
-    if (a->dw && (a->dw == a->x || a->dw == a->dy || a->dw == a->w || a->dw == a->dx)) return SADMM_EINVAL;
+    if (!distinct({a->dx, a->dw, a->db}, {a->dy, a->x, a->w}) || !distinct({a->dx}, {a->z})) return SADMM_EINVAL;
+    if (a->act != SADMM_ACT_NONE && !distinct({a->dw, a->db}, {a->z})) return SADMM_EINVAL;
     return SADMM_OK;
 }
 
@@ -104,14 +133,7 @@ sadmm_status check(const sadmm_gated_fwd_args* a)
     if (!matrix(a->x, SADMM_BF16, a->ldx, a->n_in) || !matrix(a->h, SADMM_BF16, a->ldh, a->n_hidden) ||
         !matrix_or_null(a->g, SADMM_BF16, a->ldg, a->n_hidden) || !matrix_or_null(a->u, SADMM_BF16, a->ldu, a->n_hidden))
         return SADMM_EINVAL;
-    const void* const in[3] = {a->x, a->wg, a->wu};
-    const void* const out[3] = {a->h, a->g, a->u};
-    for (int o = 0; o < 3; ++o) {
-        if (!out[o]) continue;
-        for (int i = 0; i < 3; ++i)
-            if (out[o] == in[i] || (i != o && out[o] == out[i])) return SADMM_EINVAL;
-    }
-    return SADMM_OK;
+    return distinct({a->h, a->g, a->u}, {a->x, a->wg, a->wu, a->bg, a->bu}) ? SADMM_OK : SADMM_EINVAL;
 }
 
 sadmm_status check(const sadmm_gated_bwd_args* a)
@@ -130,14 +152,8 @@ sadmm_status check(const sadmm_gated_bwd_args* a)
     if (a->dx && (!matrix(a->wg, SADMM_BF16, a->ldwg, a->n_in) || !matrix(a->wu, SADMM_BF16, a->ldwu, a->n_in)))
         return SADMM_EINVAL;
     if (a->dwg && !matrix(a->x, SADMM_BF16, a->ldx, a->n_in)) return SADMM_EINVAL;
-    const void* const in[6] = {a->dh, a->x, a->wg, a->wu, a->g, a->u};
-    const void* const out[3] = {a->dx, a->dwg, a->dwu};
-    for (int o = 0; o < 3; ++o) {
-        if (!out[o]) continue;
-        for (int i = 0; i < 6; ++i)
-            if (out[o] == in[i] || (i < o && out[o] == out[i])) return SADMM_EINVAL;
-    }
-    return SADMM_OK;
+    return distinct({a->dx, a->dwg, a->dwu, a->dbg, a->dbu}, {a->dh, a->x, a->wg, a->wu, a->g, a->u}) ? SADMM_OK
+                                                                                                       : SADMM_EINVAL;
 }
 
 // Scratch: `need` bytes on a 256-byte boundary.
