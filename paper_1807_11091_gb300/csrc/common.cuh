@@ -196,6 +196,11 @@ SADMM_DEV bool dbg_in(long long i, long long n, int* status)
 #else
 SADMM_DEV bool dbg_in(long long, long long, int*) { return true; }
 #endif
+// The same for n neighbours from i on, of `total`.
+SADMM_DEV bool dbg_run(long long i, long long n, long long total, int* status)
+{
+    return dbg_in(i, total, status) && dbg_in(i + n - 1, total, status);
+}
 
 // ---------------------------------------------------------------- mbarrier --
 

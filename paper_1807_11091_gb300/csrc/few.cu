@@ -75,10 +75,10 @@ struct Words {
 };
 
 template <bool ALIGNED>
-SADMM_DEV void fetch(Words& v, const bf16* row, int c, int n)
+SADMM_DEV void fetch(Words& v, const bf16* row, int c, int n, int* status)
 {
     const int off = ALIGNED ? 0 : place(row);
-    const bool in = inside(off, c, n);
+    const bool in = inside(off, c, n) && dbg_run(c - off, off ? 16 : 8, n, status);
     v.lo = ld_if(row + c - off, in);
     if constexpr (!ALIGNED) v.hi = ld_if(row + c - off + 8, in && off);
 }
@@ -206,6 +206,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_one(const __grid_constant
 #pragma unroll 2
         for (; c + 8 <= a.n_in; c += step) {
             uint4 w[R];
+            if (!dbg_run(c, 8, a.n_in, a.status)) break;
 #pragma unroll
             for (int r = 0; r < R; ++r) w[r] = ld_stream(reinterpret_cast<const uint4*>(row[r] + c));
             multiply(w, __ldg(reinterpret_cast<const uint4*>(a.x + c)));
@@ -215,8 +216,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_one(const __grid_constant
     for (; c < a.n_in; c += step) {
         Words w[R], x;
 #pragma unroll
-        for (int r = 0; r < R; ++r) fetch<ALIGNED>(w[r], row[r], c, a.n_in);
-        fetch<ALIGNED>(x, a.x, c, a.n_in);
+        for (int r = 0; r < R; ++r) fetch<ALIGNED>(w[r], row[r], c, a.n_in, a.status);
+        fetch<ALIGNED>(x, a.x, c, a.n_in, a.status);
         uint4 v[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) v[r] = settle<ALIGNED>(w[r], row[r], c, a.n_in);
@@ -329,7 +330,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
             uint4 w[kAhead][M][2], x[kAhead][NT];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int k = c + 32 * i + 8 * t;
+                int k = c + 32 * i + 8 * t;
+                if (!dbg_run(k, 8, a.n_in, a.status)) k = 0;  // the row's start instead
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
                     w[i][m][0] = ld_stream(reinterpret_cast<const uint4*>(row[m][0] + k));
@@ -355,11 +357,11 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
                 const int k = c + 32 * (i0 + i) + 8 * t;
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
-                    fetch<ALIGNED>(w[i][m][0], row[m][0], k, a.n_in);
-                    fetch<ALIGNED>(w[i][m][1], row[m][1], k, a.n_in);
+                    fetch<ALIGNED>(w[i][m][0], row[m][0], k, a.n_in, a.status);
+                    fetch<ALIGNED>(w[i][m][1], row[m][1], k, a.n_in, a.status);
                 }
 #pragma unroll
-                for (int q = 0; q < NT; ++q) fetch<ALIGNED>(x[i][q], xr[q], k, a.n_in);
+                for (int q = 0; q < NT; ++q) fetch<ALIGNED>(x[i][q], xr[q], k, a.n_in, a.status);
             }
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {

@@ -26,6 +26,7 @@ struct Copies {
     bf16* dst[3];
     long long ld[3], ldd[3], rows[3];
     int cols[3];
+    int* status;
 };
 
 // Matrix blockIdx.y, a warp a row's 1024 elements (segments blockIdx.z, blockIdx.z +
@@ -53,7 +54,7 @@ __global__ void __launch_bounds__(256) k_realign(const Copies a)
                 if (i >= words) break;
                 const int c = i * 8;
                 uint4 o;
-                if (c >= off && c + 16 <= cols) {
+                if (c >= off && c + 16 <= cols && dbg_run(c - off, 16, cols, a.status)) {
                     const uint4 lo = __ldg(from + i), hi = __ldg(from + i + 1);
                     // words w0 .. w0 + 4 of the eight (w0 is the row's: the same for the warp)
                     uint32_t v0, v1, v2, v3, v4;
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(256) k_realign(const Copies a)
                         e[j] = c + j < cols ? __ldg(reinterpret_cast<const unsigned short*>(row) + c + j) : 0u;
                     o = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
                 }
-                to[i] = o;
+                if (dbg_run(c, 8, a.ldd[m], a.status)) to[i] = o;
             }
         }
     }
@@ -95,6 +96,7 @@ struct DactArgs {
     int act;
     int cluster;               // CTAs of a strip, in one cluster where sums are wanted
     int sums;
+    int* status;
 };
 
 // N consecutive elements, as they lie in memory.
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(kDactThreads, GATED || !VEC ? 3 : 4) k_dact(co
                 s[j] = __fadd_rn(s[j], d[j]);
             }
             if (VEC) {
-                if (a.dz && cl * 8 < left) {
+                if (a.dz && cl * 8 < left && dbg_run(c0 + cl * 8, 8, a.ldd, a.status) && dbg_in(r, a.rows, a.status)) {
                     __align__(16) Raw<bf16, 8> o;
 #pragma unroll
                     for (int j = 0; j < N; ++j) o.e[j] = __float2bfloat16_rn(d[j]);
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(kDactThreads, GATED || !VEC ? 3 : 4) k_dact(co
             } else if (a.dz) {
 #pragma unroll
                 for (int j = 0; j < N; ++j)
-                    if (col(j) < padded) {
+                    if (col(j) < padded && dbg_in(c0 + col(j), a.ldd, a.status) && dbg_in(r, a.rows, a.status)) {
                         a.dz[r * a.ldd + c0 + col(j)] = __float2bfloat16_rn(d[j]);
                         if (GATED) a.du[r * a.ldd + c0 + col(j)] = __float2bfloat16_rn(e[j]);
                     }
@@ -198,13 +200,18 @@ __global__ void __launch_bounds__(kDactThreads, GATED || !VEC ? 3 : 4) k_dact(co
         };
         auto load = [&](auto inside, long long r, Raw<DY, N>& rd, Raw<bf16, N>& rz, Raw<bf16, N>& ru) {
             if constexpr (decltype(inside)::value) {
+                if (!dbg_run(c0 + cl * 8, 8, a.cols, a.status) || !dbg_in(r, a.rows, a.status)) {
+                    rd = {}, rz = {}, ru = {};
+                    return;
+                }
                 load_raw(dy + r * a.lddy + cl * 8, rd);
                 if (Z) load_raw(zp + r * a.ldz + cl * 8, rz);
                 if (GATED) load_raw(up + r * a.ldu + cl * 8, ru);
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const bool in = col(j) < left;  // past the end: zeros
+                    // past the end: zeros
+                    const bool in = col(j) < left && dbg_in(c0 + col(j), a.cols, a.status) && dbg_in(r, a.rows, a.status);
                     rd.e[j] = in ? dy[r * a.lddy + col(j)] : DY(0.0f);
                     if (Z) rz.e[j] = in ? zp[r * a.ldz + col(j)] : bf16(0.0f);
                     if (GATED) ru.e[j] = in ? up[r * a.ldu + col(j)] : bf16(0.0f);
@@ -259,7 +266,7 @@ __global__ void __launch_bounds__(kDactThreads, GATED || !VEC ? 3 : 4) k_dact(co
         float v = 0.0f;
         for (int i = 0; i < a.cluster; ++i) v += ld_cluster_f32(map_rank(smem_u32(&csum[which][c]), (uint32_t)i));
         float* out = which ? a.dbu : a.db;
-        if (out && c < left) out[c0 + c] = v;
+        if (out && c < left && dbg_in(c0 + c, a.cols, a.status)) out[c0 + c] = v;
     }
     cluster_sync();  // the others have read this CTA's sums
 }
@@ -286,6 +293,7 @@ sadmm_status run_dact(const DactArgs& a, cudaStream_t s)
 sadmm_status launch_dact(DactArgs a, bool gated, bool fp32, cudaStream_t s)
 {
     a.sums = a.db || a.dbu;
+    a.status = device_status_ptr();
     // with sums at most a cluster's CTAs share a strip's rows, of at least 32 each; without, chunks of 128
     if (a.sums) {
         a.cluster = 1;
@@ -351,9 +359,10 @@ struct Filler {
         if (o.ld > widest) widest = o.ld;
         ++n;
     }
-    sadmm_status run(cudaStream_t s) const
+    sadmm_status run(cudaStream_t s)
     {
         if (!n) return SADMM_OK;
+        c.status = device_status_ptr();
         const long long blocks = (rows + 7) / 8, most = 8ll * device_sm_count();
         const long long segments = (widest + 1023) / 1024;
         const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)n,

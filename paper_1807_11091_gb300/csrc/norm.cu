@@ -104,32 +104,36 @@ SADMM_DEV unsigned long long fma2(unsigned long long a, unsigned long long b, un
 template <bool VEC>
 struct Cols {
     int g, t, cols;
+    int* status;
     // Whether element (k, j) is inside the row.
     SADMM_DEV bool in(int k, int j) const { return at(k, j) < cols; }
     SADMM_DEV int at(int k, int j) const { return VEC ? (k * g + t) * 8 + j : (8 * k + j) * g + t; }
     SADMM_DEV bool whole(int k) const { return VEC && at(k, 0) + 8 <= cols; }
+    // Index checks of a whole eight and of one element.
+    SADMM_DEV bool ok(int k) const { return dbg_run(at(k, 0), 8, cols, status); }
+    SADMM_DEV bool ok(int k, int j) const { return dbg_in(at(k, j), cols, status); }
 };
 
 template <bool VEC, typename T>
 SADMM_DEV void load_row(const T* p, const Cols<VEC>& c, int k, float fill, float (&v)[8])
 {
-    if (c.whole(k)) {
+    if (c.whole(k) && c.ok(k)) {
         load_vec(p + c.at(k, 0), v);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c.at(k, j) < c.cols ? to_f32(p[c.at(k, j)]) : fill;
+        for (int j = 0; j < 8; ++j) v[j] = c.at(k, j) < c.cols && c.ok(k, j) ? to_f32(p[c.at(k, j)]) : fill;
     }
 }
 
 template <bool VEC, typename T>
 SADMM_DEV void store_row(T* p, const Cols<VEC>& c, int k, const float (&v)[8])
 {
-    if (c.whole(k)) {
+    if (c.whole(k) && c.ok(k)) {
         store_vec(p + c.at(k, 0), v);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (c.at(k, j) < c.cols) put(p + c.at(k, j), v[j]);
+            if (c.at(k, j) < c.cols && c.ok(k, j)) put(p + c.at(k, j), v[j]);
     }
 }
 
@@ -233,6 +237,14 @@ struct Part {
         const uintptr_t a = reinterpret_cast<uintptr_t>(p + r * ld);
         return (uint32_t)(((a + (uintptr_t)cols * sizeof(T) + 15) & ~uintptr_t(15)) - (a & ~uintptr_t(15)));
     }
+    // Index check of a copy: in row r where rows are aligned, else in the span from the matrix's first element to its
+    // last.
+    SADMM_DEV bool ok(long long r, int* status) const
+    {
+        const long long at = (from(r) - reinterpret_cast<const uint8_t*>(p));
+        const long long total = ((rows - 1) * ld + cols) * (long long)sizeof(T);
+        return dbg_in(r, rows, status) && dbg_run(at, bytes(r), total, status);
+    }
     // Room for a copy of any row.
     static __host__ __device__ int room(int cols) { return (cols * (int)sizeof(T) + 32 + 127) / 128 * 128; }
     // The k-th eight of row r, from its copy at `s` (NULL: from global memory).
@@ -281,7 +293,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 256 || CAP == 0 ? 3 : 
     __shared__ volatile int abort_flag;
     const int G = BLOCK ? blockDim.x : 32, R = BLOCK ? 1 : blockDim.x / 32;
     const int group = BLOCK ? 0 : threadIdx.x >> 5;
-    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols};
+    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols, a.status};
     const long long first = (long long)blockIdx.x * R + group, step = (long long)gridDim.x * R;
     const Part<VEC, X> x = {static_cast<const X*>(a.x), a.ldx, a.rows, a.cols};
     const int room = Part<VEC, X>::room(a.cols);
@@ -298,7 +310,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 256 || CAP == 0 ? 3 : 
     pdl_trigger();
     auto fetch = [&](long long r, int s) {  // by the group's first thread
         if (r >= a.rows) return;
-        if (x.copied(r)) {
+        if (x.copied(r) && x.ok(r, a.status)) {
             mbar_arrive_expect_tx(&bar[s], x.bytes(r));
             bulk_load(mine + s * room, x.from(r), x.bytes(r), &bar[s]);
         } else {
@@ -435,7 +447,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 
     __shared__ volatile int abort_flag;
     const int G = BLOCK ? blockDim.x : 32, R = BLOCK ? 1 : blockDim.x / 32;
     const int warp = threadIdx.x >> 5, group = BLOCK ? 0 : warp;
-    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols};
+    const Cols<VEC> c = {G, BLOCK ? (int)threadIdx.x : (int)(threadIdx.x & 31), a.cols, a.status};
     const long long first = (long long)blockIdx.x * R + group, step = (long long)gridDim.x * R;
     const Part<VEC, X> x = {static_cast<const X*>(a.x), a.ldx, a.rows, a.cols};
     const Part<VEC, Y> dy = {static_cast<const Y*>(a.dy), a.lddy, a.rows, a.cols};
@@ -455,7 +467,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 
     pdl_trigger();
     auto fetch = [&](long long r, int s) {  // by the group's first thread
         if (r >= a.rows) return;
-        if (x.copied(r)) {
+        if (x.copied(r) && x.ok(r, a.status) && dy.ok(r, a.status) && (!a.dres || dres.ok(r, a.status))) {
             uint8_t* to = mine + s * room;
             mbar_arrive_expect_tx(&bar[s], x.bytes(r) + dy.bytes(r) + (a.dres ? dres.bytes(r) : 0u));
             bulk_load(to, x.from(r), x.bytes(r), &bar[s]);
