@@ -11,7 +11,7 @@
 // Nothing is staged.  Warps that share rows join their sums in shared memory in
 // warp order.  Rows that do not start on 16-byte boundaries are read as the
 // aligned words around them, shifted into place.  k_one is for one token of
-// ragged or unaligned rows.
+// ragged rows.
 //
 // Measured against the tile kernels (us, the same call repeated in a graph, so that
 // weights below the L2's size stay there): 1 token 5120 -> 2048 4.7 (9.1), 8192 ->
@@ -161,12 +161,13 @@ SADMM_DEV void join(float (&v)[V], int lane, int& index)
     }
 }
 
-// One token on the CUDA cores, where rows are ragged or off 16-byte boundaries.  A
-// group of warps takes U outputs (gated: of two weight rows each); a lane multiplies
-// its 16-byte pieces in pairs (fma.f32x2, fp32 sums).  Here
-// and by k_few: 1001 -> 1001 3.3 and 5.7 us, 5119 -> 2047 8.5 and 13.4, 704 -> 704 2.0
-// and 2.5; the gated pair 2047 -> 2 x 5461 16.9 and 17.2 (14.2 with the pieces' shifts
-// chosen by branches, where the single linear layer took 10.9).
+// One token on the CUDA cores, where rows are ragged or (not the gated pair's) off
+// 16-byte boundaries.  A group of warps takes U outputs (gated: of two weight rows
+// each); a lane multiplies its 16-byte pieces in pairs (fma.f32x2, fp32 sums).  Here
+// and by k_few, over weights from DRAM: 1001 -> 1001 3.4 and 3.7 us, 5119 -> 2047 10.1
+// and 12.0; the gated pair of 5000 -> 2 x 1500, aligned, 7.2 and 12.0; off 16-byte
+// boundaries, where k_few serves it, 333 -> 2 x 777 5.7 and 3.7, 1023 -> 2 x 2731 8.1
+// and 6.5, 2047 -> 2 x 5461 20.5 and 20.8.
 template <int U, bool GATED, bool ALIGNED>
 __global__ void __launch_bounds__(kFewWarps * 32, 2) k_one(const __grid_constant__ FewArgs a)
 {
@@ -260,9 +261,11 @@ template <int NT, bool GATED, bool ALIGNED, bool LONG>
 __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant__ FewArgs a)
 {
     constexpr int M = GATED ? 2 : 1;  // weight matrices
-    // pieces of 32 elements in flight (8 tokens of 8192 -> 8192: 18.8 us with 8, 24.0 with 4; the gated pair and more
-    // tokens have no registers for as many: 16 tokens 23.6 with 4, 24.4 with 8)
-    constexpr int kAhead = NT == 4 || GATED ? 2 : NT == 2 ? 4 : 8;
+    // pieces of 32 elements in flight (8 tokens of 8192 -> 8192: 18.8 us with 8, 24.0 with 4; the gated pair, more
+    // tokens and rows off 16-byte boundaries have no registers for as many: 16 tokens 23.6 with 4, 24.4 with 8; with 8,
+    // 4 and 2 unaligned, over weights from DRAM, 2 tokens of 333 -> 777 5.9, 3.6, 2.9, of 1001 -> 1001 6.3, 3.7, 4.2, of
+    // 5119 -> 2047 15.8, 12.1, 13.5, of 8191 -> 8191 58, 50, 48)
+    constexpr int kAhead = NT == 4 || GATED ? 2 : NT == 2 || !ALIGNED ? 4 : 8;
     __shared__ float red[kFewWarps][M][16][8 * NT + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int part = warp % a.share, group = warp / a.share, groups = kFewWarps / a.share;
@@ -344,16 +347,16 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
             for (int i = 0; i < kAhead; ++i) multiply(i & 1, w[i], x[i]);
         }
     }
-    // the ragged end, and rows off 16-byte boundaries: again all loads of a batch before its products
-    constexpr int kBatch = ALIGNED || kAhead == 2 ? kAhead : kAhead / 2;
+    // the ragged end, and rows off 16-byte boundaries: again all loads before their products (the inner loop has one
+    // turn; without it the compiler lays the same code out worse: the gated pair of 333 -> 2 x 777 3.7 us, 4.8)
 #pragma unroll 1
     for (; c < a.n_in; c += step) {
         count_run();
 #pragma unroll 1
-        for (int i0 = 0; i0 < kAhead && c + 32 * i0 < a.n_in; i0 += kBatch) {
-            Words w[kBatch][M][2], x[kBatch][NT];
+        for (int i0 = 0; i0 < kAhead && c + 32 * i0 < a.n_in; i0 += kAhead) {
+            Words w[kAhead][M][2], x[kAhead][NT];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
+            for (int i = 0; i < kAhead; ++i) {
                 const int k = c + 32 * (i0 + i) + 8 * t;
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) k_few(const __grid_constant
                 for (int q = 0; q < NT; ++q) fetch<ALIGNED>(x[i][q], xr[q], k, a.n_in, a.status);
             }
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
+            for (int i = 0; i < kAhead; ++i) {
                 const int k = c + 32 * (i0 + i) + 8 * t;
                 if (c + 32 * (i0 + i) >= a.n_in) break;  // the whole warp
                 uint4 v[M][2], u[NT];
@@ -406,8 +409,11 @@ sadmm_status run_one(FewArgs& a, bool aligned, cudaStream_t s)
     a.share = 1;
     while (a.share < kFewWarps && (a.n_in >= 2048 * a.share || groups * a.share < 16ll * device_sm_count())) a.share *= 2;
     const int per = kFewWarps / a.share;
-    return launch_pdl(aligned ? k_one<U, GATED, true> : k_one<U, GATED, false>,
-                      dim3((unsigned)((groups + per - 1) / per)), dim3(kFewWarps * 32), 0, s, a) == cudaSuccess
+    void (*kernel)(FewArgs) = k_one<U, GATED, true>;
+    if constexpr (!GATED) {
+        if (!aligned) kernel = k_one<U, GATED, false>;
+    }
+    return launch_pdl(kernel, dim3((unsigned)((groups + per - 1) / per)), dim3(kFewWarps * 32), 0, s, a) == cudaSuccess
                ? SADMM_OK
                : SADMM_ECUDA;
 }
@@ -498,7 +504,7 @@ sadmm_status launch_few_gated(const sadmm_gated_fwd_args& f, cudaStream_t s)
     a.act = f.act;
     a.status = device_status_ptr();
     const bool aligned = few_aligned(f);
-    if (f.tokens == 1 && (!aligned || f.n_in % 256)) return run_one<2, true>(a, aligned, s);
+    if (f.tokens == 1 && aligned && f.n_in % 256) return run_one<2, true>(a, aligned, s);
     return f.tokens <= 8 ? run<1, true>(a, aligned, s) : run<2, true>(a, aligned, s);
 }
 
