@@ -18,12 +18,24 @@ class FeedForward:
 
     Wg, Wu [H][D] and Wd [D][H] are kept in buffers whose rows start on 32-byte
     boundaries, so that an odd number of units costs nothing.
+
+    ``saved`` is what the last forward(train=True) of the object kept: its input
+    and activations.  They live until the next such pass, or until ``saved`` is
+    set to None.  A program with several passes in flight (micro-batches,
+    threads) keeps each pass's own and hands it to its backward:
+
+        y = block.forward(x, train=True); kept = block.saved
+        ...
+        dx, grads = block.backward(dy, saved=kept)
+
+    (threads that share an object take its ``saved`` under the lock of their
+    forward).  Nothing here is recorded for torch's autograd.
     """
 
     def __init__(self, gamma, beta, Wg, Wu, Wd, bias=None, act: int = sadmm.SADMM_ACT_SILU, eps: float = 1e-5):
         self.gamma, self.beta, self.bias, self.act, self.eps = gamma, beta, bias, act, eps
         self.Wg, self.Wu, self.Wd = (self._rows(w) for w in (Wg, Wu, Wd))
-        self._saved = None
+        self.saved = None
 
     @staticmethod
     def _rows(w):
@@ -59,12 +71,18 @@ class FeedForward:
             return sadmm.linear(h, self.Wd, self.bias, residual=x)
         n, mean, rstd = sadmm.layer_norm(x, self.gamma, self.beta, self.eps, out_dtype=torch.bfloat16, stats=True)
         h, g, u = sadmm.gated(n, self.Wg, self.Wu, act=self.act, save=True)
-        self._saved = (x, n, mean, rstd, h, g, u)
+        self.saved = (x, n, mean, rstd, h, g, u)
         return sadmm.linear(h, self.Wd, self.bias, residual=x)
 
-    def backward(self, dy, dw_dtype=None):
-        """Gradients of the last forward(train=True) for dy (of x's type): dx and a dict of the weights'."""
-        x, n, mean, rstd, h, g, u = self._saved
+    def backward(self, dy, dw_dtype=None, saved=None):
+        """Gradients for dy (of x's shape and type) of the pass that `saved` is of, otherwise of the
+        last forward(train=True): dx and a dict of the weights'."""
+        saved = self.saved if saved is None else saved
+        if saved is None:
+            raise RuntimeError("backward needs a forward(train=True) before it")
+        x, n, mean, rstd, h, g, u = saved
+        if dy.shape != x.shape:
+            raise ValueError(f"dy is {tuple(dy.shape)}, the pass's x {tuple(x.shape)}")
         dh, dWd, db = sadmm.linear_backward(dy, h, self.Wd, want_db=self.bias is not None, dw_dtype=dw_dtype)
         dn, dWg, dWu, _, _ = sadmm.gated_backward(dh, n, self.Wg, self.Wu, g, u, act=self.act, dw_dtype=dw_dtype)
         dx, dgamma, dbeta = sadmm.layer_norm_backward(dn, x, mean, rstd, self.gamma, dres=dy)
