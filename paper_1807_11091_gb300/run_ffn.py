@@ -1,4 +1,4 @@
-"""Prunes, runs and retrains one gated feed-forward block, and times it.
+"""Prunes one gated feed-forward block, runs its forward and backward pass, and times both.
 
     python -m paper_1807_11091_gb300.run_ffn --tokens 4096 --d 1024 --hidden 4096 --keep 0.5
 

@@ -759,6 +759,9 @@ def pack_batch(convs, stream=None) -> None:
 # With `stream` the call's kernels, outputs and scratch are that stream's: its
 # inputs have to be ready there, and whoever reads its outputs on another stream
 # has that one wait.
+# `out` is written in its own type, whatever out_dtype says.  Nothing is recorded
+# for torch's autograd: a result requires no gradient even where an argument does,
+# and the ..._backward functions give the gradients.
 # The checks, outputs and scratch are those of csrc/torch_ffn.cpp, because on a
 # few tokens they are what a call costs.
 
@@ -808,7 +811,9 @@ def linear(x, W, bias=None, residual=None, act: int = SADMM_ACT_NONE, out_dtype=
 def linear_backward(dy, x, W, z=None, act: int = SADMM_ACT_NONE, want_dx: bool = True, want_dw: bool = True,
                     want_db: bool = True, dx_dtype=None, dw_dtype=None, stream=None):
     """Runs sadmm_linear_bwd: (dx, dW, db), None where not wanted.  dx and dW are
-    bf16 unless dx_dtype / dw_dtype say fp32; dW has W's row stride."""
+    bf16 unless dx_dtype / dw_dtype say fp32; dW has W's row stride.  dy act'(z) (an
+    fp32 dy itself) is rounded to bf16 once for the products, whatever their types;
+    db is summed before that."""
     return (_ffn_module or _ffn()).linear_backward(dy, x, W, z, act, want_dx, want_dw, want_db, dx_dtype, dw_dtype,
                                                    _handle(stream))
 
@@ -823,7 +828,8 @@ def gated_backward(dh, x, Wg, Wu, g, u, act: int = SADMM_ACT_SILU, want_dx: bool
                    want_db: bool = False, dx_dtype=None, dw_dtype=None, stream=None):
     """Runs sadmm_gated_bwd: (dx, dWg, dWu, dbg, dbu), None where not wanted.  dx and
     the weights' gradients are bf16 unless dx_dtype / dw_dtype say fp32; the
-    latter have their weights' row strides."""
+    latter have their weights' row strides.  dg and du are rounded to bf16 once for
+    the products, whatever their types; dbg and dbu are summed before that."""
     return (_ffn_module or _ffn()).gated_backward(dh, x, Wg, Wu, g, u, act, want_dx, want_dw, want_db, dx_dtype,
                                                   dw_dtype, _handle(stream))
 
