@@ -64,9 +64,10 @@ SADMM_DEV int atom_add_acq_rel_gpu(int* p, int v)
 // completed and its memory is visible, so it comes before the first read of
 // anything an earlier kernel wrote.  pdl_trigger() lets the next kernel of the
 // stream be scheduled once every CTA of this one has issued it (or exited).
-// A kernel launched in clusters does not trigger: clusters of the next kernel
-// that were let in early, and waited, took the places of this one's that had
-// not started yet, and both stood still.
+// A kernel launched in clusters does not trigger: with it, a kernel of more
+// clusters than fit at once and the clusters of the next one stood still together
+// (seen after 10 to 600 passes; as the instruction is documented, all of the former's
+// CTAs should have started by then).
 // A kernel's completion means that of every kernel before it: each one waits,
 // at its start or (k_grid_conv's late_wait) at its end.
 SADMM_DEV void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -13,13 +13,15 @@
 // Two accumulators in TMEM: a tile's epilogue runs beside the next tile's
 // products.  fp32 outputs of long contractions (LONG) are added up in registers
 // over accumulators of kLongSteps steps each (8192 x 5120 -> 2048's gradients take
-// 238 us with sums of 2048 terms, 254 with sums of 512).
+// 238 us with sums of 2048 terms, 250 to 255 over boxes with these of 768, 254 with
+// sums of 512).
 //
 // Bound by the tensor pipe: 8192 x 4096 -> 2 x 10240 (the gated pair, both
 // pre-activations kept) in 770 to 880 us over boxes, 1780 to 1560 TFLOP/s, where
 // the power limit sets the clock (a library product alone: 1946 for a moment,
 // 1740 sustained).  Smaller products lose their last round of tiles: 4096^3 in
-// 86 us (1600 TFLOP/s) with four rounds of 224 columns.
+// 86 us (1600 TFLOP/s) with four rounds of 224 columns, 104 to 106 with GELU, z kept
+// and inputs that change between calls.
 #include "tgemm_dev.cuh"
 
 namespace sadmm {
