@@ -57,3 +57,12 @@ def test_input_gradient_of_many_units(T, K, H):
     dx = sadmm.gated_backward(dh, x, Wg, Wu, g, u, act=sadmm.SADMM_ACT_NONE, want_dw=False, dx_dtype=FP32)[0]
     assert sadmm.device_status() == 0
     assert off(dx, 0.5 * dh.double() @ Wg.double() + dh.double() @ Wu.double()) < 1.5e-6
+
+
+@pytest.mark.parametrize("T,K,H,xdt,wdt", [(100, 64, 20000, FP32, BF16), (130, 40, 9000, FP32, FP32),
+                                           (4000, 70, 66, BF16, FP32), (20000, 66, 70, FP32, FP32)])
+def test_products_of_long_and_short_contractions_together(T, K, H, xdt, wdt):
+    """All gradients of one call, some cut and some not, within the bounds of the other sizes' test."""
+    import test_gpu_linear as L
+    L.test_gated_backward(T, K, H, "silu", xdt, wdt, "padded")
+    L.test_linear_backward(T, K, H, "silu", BF16, xdt, wdt, "padded")
