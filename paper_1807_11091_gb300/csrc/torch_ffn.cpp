@@ -314,8 +314,11 @@ struct Call {
     void uses(PyObject* const* v, int n, const Output (&o)[N]) const
     {
         if (!other) return;
-        for (int i = 0; i < n; ++i)
-            if (THPVariable_Check(v[i])) THPVariable_Unpack(v[i]).record_stream(own->unwrap());
+        for (int i = 0; i < n; ++i) {
+            if (!THPVariable_Check(v[i])) continue;
+            const Tensor& t = THPVariable_Unpack(v[i]);
+            if (t.is_cuda()) t.record_stream(own->unwrap());  // (an argument that is not read may lie anywhere)
+        }
         for (const Output& x : o)
             if (x.t.defined()) x.t.record_stream(callers->unwrap());
     }

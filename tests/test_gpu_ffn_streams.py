@@ -109,3 +109,15 @@ def test_the_current_or_default_stream_by_name(given):
         y = s.linear(x, W, stream=name)
     torch.cuda.synchronize()
     assert torch.equal(y, ref)
+
+
+def test_an_argument_that_is_not_read_may_lie_anywhere():
+    """z without an activation is ignored, on a given stream too."""
+    s, side = lib(), torch.cuda.Stream()
+    g = F.gen(2)
+    dy, x, W = F.matrix(g, 40, 64), F.matrix(g, 40, 128), F.matrix(g, 64, 128)
+    want = s.linear_backward(dy, x, W)
+    side.wait_stream(torch.cuda.current_stream())
+    got = s.linear_backward(dy, x, W, z=torch.zeros(3), stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and s.device_status() == 0
