@@ -504,7 +504,11 @@ sadmm_status launch_few_gated(const sadmm_gated_fwd_args& f, cudaStream_t s)
     a.act = f.act;
     a.status = device_status_ptr();
     const bool aligned = few_aligned(f);
-    if (f.tokens == 1 && aligned && f.n_in % 256) return run_one<2, true>(a, aligned, s);
+    // one token of short rows goes to k_few where its groups of 16 units are more than the SMs (333 -> 2 x 5461 4.4 us and
+    // by k_one 5.4, 1023 -> 2 x 2731 4.7 and 5.3; below 2432 units or from 2000 columns on k_one is the faster or level:
+    // 2047 -> 2 x 2300 5.3 and 7.4, -> 2 x 4001 8.0 and 7.7, 5000 -> 2 x 5461 23.7 and 28.3)
+    const bool one = f.n_hidden <= 16 * device_sm_count() || f.n_in >= 2000;
+    if (f.tokens == 1 && aligned && f.n_in % 256 && one) return run_one<2, true>(a, aligned, s);
     return f.tokens <= 8 ? run<1, true>(a, aligned, s) : run<2, true>(a, aligned, s);
 }
 

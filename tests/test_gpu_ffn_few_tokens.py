@@ -32,6 +32,9 @@ def test_linear_of_few_tokens(T, K, N, act, bias, res, dt, save):
     (13, 2050, 130, "relu", True, True),
     (16, 515, 2731, "silu", True, True),
     (16, 2048, 5461, "none", False, False),
+    (1, 1023, 2731, "silu", True, True),
+    (1, 1023, 2400, "gelu", True, True),
+    (1, 2047, 2731, "relu", False, True),
 ])
 def test_gated_of_few_tokens(T, K, H, act, bias, save):
     L.test_gated(T, K, H, act, bias, save, "padded")
