@@ -17,9 +17,41 @@ inline int act_for(int act, bool bf16)
 template <int ACT>
 SADMM_DEV void act_slope_f32(float z, float& a, float& s);
 
-// act(z): max(z, 0) (NaN kept); z Phi(z) with the normal distribution Phi, whose
-// tail (1 + erf would leave none of its digits at z = -5) CUDA's function gives to
-// five units; z sigmoid(z).
+// 2^x for x <= 0, 0 below 2^-126; within 2 units.
+SADMM_DEV float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// z Phi(z) with the normal distribution Phi, of which 1 + erf would leave no digit in
+// the tail: Phi's smaller side is exp(-z^2 / 2) t P(t), t = 1 / (1 + 0.3 |z|), with P of
+// degree 7 fitted to that quotient for |z| up to 13.5 (least maximum of the relative
+// error, 1.3e-7; with its rounding 4.4e-7).  The exponent c z^2, c = -log2(e) / 2, is
+// taken in two parts, because the power would enlarge its rounding.  4096^3 in fp32
+// takes 134 us so and with erf, 205 with CUDA's normcdff, which is as exact.
+SADMM_DEV float gelu_f32(float z)
+{
+    const float w = fminf(fabsf(z), 15.0f);  // past which the smaller side is 0
+    constexpr float c = -0.721347511f, c_low = -9.62981517e-09f;
+    const float s = w * w, h = s * c;
+    const float low = fmaf(s, c, -h) + fmaf(s, c_low, fmaf(w, w, -s) * c);
+    const float p = exp2_fast(h), e = fmaf(p, low * 0.693147181f, p);
+    const float t = __fdividef(1.0f, 1.0f + 0.3f * w);
+    float g = 0.0359317213f;
+    g = fmaf(g, t, -0.158275947f);
+    g = fmaf(g, t, 0.208206505f);
+    g = fmaf(g, t, -0.0553937592f);
+    g = fmaf(g, t, 0.129469156f);
+    g = fmaf(g, t, 0.0996375084f);
+    g = fmaf(g, t, 0.120798357f);
+    g = fmaf(g, t, 0.119626388f);
+    const float q = e * (t * g);
+    return z * (z > 0.0f ? 1.0f - q : q);
+}
+
+// act(z): max(z, 0) (NaN kept); gelu_f32; z sigmoid(z).
 template <int ACT>
 SADMM_DEV float act_f32(float z)
 {
@@ -29,7 +61,7 @@ SADMM_DEV float act_f32(float z)
         return a;
     }
     if (ACT == SADMM_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == SADMM_ACT_GELU) return z * normcdff(z);
+    if (ACT == SADMM_ACT_GELU) return gelu_f32(z);
     if (ACT == SADMM_ACT_SILU) return __fdividef(z, 1.0f + expf(-z));
     return z;
 }

@@ -44,6 +44,21 @@ def test_activation(name, T, dt):
 
 
 @pytest.mark.parametrize("name", ACTS)
+@pytest.mark.parametrize("T", [1, 40, 600])
+def test_activation_of_fp32_values(name, T):
+    """Pre-activations with all of fp32's digits: x is zero, the bias the values.  As above for fp32; the
+    functions' arguments enter products that the tail enlarges, and must not lose digits there."""
+    from paper_1807_11091_gb300 import sadmm
+    z = torch.rand(20000, generator=F.gen(3), device="cuda") * 25 - 12.5
+    x, W = torch.zeros(T, 8, dtype=BF16, device="cuda"), torch.zeros(z.numel(), 8, dtype=BF16, device="cuda")
+    y = sadmm.linear(x, W, z, act=F.ACTS[name], out_dtype=FP32)
+    assert sadmm.device_status() == 0
+    want = F.act(name, z.double())[0].expand(T, -1)
+    over = (y.double() - want).abs() - (8 * U32 * want.abs() + 2.0 ** -126)
+    assert (over <= 0).all(), float(z[int(over.argmax()) % z.numel()])
+
+
+@pytest.mark.parametrize("name", ACTS)
 def test_slope(name):
     """db of one token is dy act'(z) before any rounding to bf16: within 2^-16 of the slope's terms
     (1/128 of the rounding that dz takes)."""
