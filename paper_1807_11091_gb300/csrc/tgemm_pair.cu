@@ -17,7 +17,7 @@
 // sums of 512).
 //
 // Bound by the tensor pipe: 8192 x 4096 -> 2 x 10240 (the gated pair, both
-// pre-activations kept) in 770 to 880 us over boxes, 1780 to 1560 TFLOP/s, where
+// pre-activations kept) in 770 to 893 us over boxes, 1780 to 1540 TFLOP/s, where
 // the power limit sets the clock (a library product alone: 1946 for a moment,
 // 1740 sustained).  Smaller products lose their last round of tiles: 4096^3 in
 // 86 us (1600 TFLOP/s) with four rounds of 224 columns, 104 to 106 with GELU, z kept
