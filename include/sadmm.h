@@ -65,7 +65,11 @@ typedef enum {
     SADMM_EBOUNDS = -5       /* debug build: a device-side index check failed */
 } sadmm_status;
 
-typedef enum { SADMM_BF16 = 0, SADMM_FP32 = 1 } sadmm_dtype;
+typedef enum {
+    SADMM_BF16 = 0,
+    SADMM_FP32 = 1,
+    SADMM_E4M3 = 2 /* 8 bits with scales: outputs of the calls that say so */
+} sadmm_dtype;
 
 /* Column (GEMM-column) pruning kind.  Filter (row) pruning is always
  * available through k_filters / n_filt and combines with any of these. */
@@ -819,6 +823,236 @@ typedef struct {
 } sadmm_gated_bwd_args;
 size_t sadmm_gated_bwd_workspace_size(const sadmm_gated_bwd_args* a);
 sadmm_status sadmm_gated_bwd(const sadmm_gated_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Feed-forward operators with 8-bit operands: a pruned block's products at half
+ * the bytes and twice the rate of bf16.
+ *
+ *   sadmm_rmsnorm_fwd / _bwd   root-mean-square norm, the residual's addition
+ *                              before it, its output in 8 bits where wanted
+ *   sadmm_quantize             a matrix (and its transpose) in 8 bits
+ *   sadmm_gated8_fwd / _bwd    sadmm_gated_... of 8-bit operands
+ *   sadmm_linear8_fwd / _bwd   sadmm_linear_... of 8-bit operands
+ *
+ * An 8-bit matrix has e4m3 values q (4 significant bits, largest 448) and an
+ * fp32 scale s for each block: 128 neighbouring columns of one row, or with
+ * `tile` of 128 rows (the last ones may be smaller).  It stands for q s.
+ * Whatever is made 8-bit here has
+ *     s = max(largest finite |x| of the block, 2^-96) / 448,   q = e4m3(x / s),
+ * both quotients in fp32 and q rounded to nearest even; an infinity or NaN
+ * becomes NaN and leaves the rest of its block alone.  A product of 8-bit
+ * matrices is the sum over blocks of both scales times the sum of the products
+ * of the block's values: inside a block in the tensor cores, between blocks by
+ * fp32 multiply-adds.  Scales are read as they are; the product of two that meet has to
+ * be an fp32 number.
+ *
+ * The conventions of the feed-forward operators above hold, with these
+ * additions: an 8-bit matrix is read where it lies if its base is 16-byte
+ * aligned and its row stride a multiple of 16, otherwise copied to the
+ * workspace; scales may have any strides, also 0 (below 2^38), and lie on fp32
+ * boundaries.
+ */
+typedef struct {
+    const void* q;          /* e4m3 [rows][cols] */
+    long long ld;           /* row stride of q */
+    const float* s;         /* scale of row r (tile: of rows 128 r ...), block b: s[r * s_row + b * s_block] */
+    long long s_row, s_block;
+    int tile;
+} sadmm_q8;
+
+typedef struct { /* the same as an output; its scales' strides are at least 1 and keep them apart */
+    void* q;
+    long long ld;
+    float* s;
+    long long s_row, s_block;
+} sadmm_q8_out;
+
+/*
+ * h = x + residual (fp32, rounded once to the residual's type; without a
+ * residual h = x); y = gamma h rstd, rstd = (avg h^2 + eps)^(-1/2) of each row.
+ *   x         [rows][cols] of type xdt (bf16 or fp32).
+ *   residual  [rows][cols] of type rdt or NULL.
+ *   h         [rows][cols] of type rdt or NULL: the sum, which the backward pass reads.  It
+ *             may be the residual itself, or x of the same type, with the same row stride.
+ *   gamma     [cols] or NULL (1).
+ *   y         [rows][cols] of type ydt (bf16 or fp32), or SADMM_E4M3: y8 with blocks of one
+ *             row, made of the fp32 values.  A bf16 or fp32 y may be x in x's place.
+ *   rstd      [rows] or NULL: kept for the backward pass.
+ *   eps       >= 0, finite.
+ */
+typedef struct {
+    long long rows;
+    int cols;
+    const void* x;
+    long long ldx;
+    int xdt;
+    const void* residual;
+    long long ldr;
+    int rdt;
+    void* h;
+    long long ldh;
+    const float* gamma;
+    float eps;
+    void* y;
+    long long ldy;
+    int ydt;
+    sadmm_q8_out y8;
+    float* rstd;
+} sadmm_rmsnorm_fwd_args;
+sadmm_status sadmm_rmsnorm_fwd(const sadmm_rmsnorm_fwd_args* a, void* stream);
+
+/*
+ * Its backward pass.  With hhat = h rstd and d = gamma dy:
+ *   dx     = rstd (d - hhat avg(d hhat)) + dres   [rows][cols] of type hdt: the gradient
+ *            of h, so of x and of the residual alike
+ *   dgamma = sum over rows of dy hhat             [cols]
+ * Types, dres and what may be NULL as in sadmm_layernorm_bwd.
+ */
+typedef struct {
+    long long rows;
+    int cols;
+    const void* h;
+    long long ldh;
+    int hdt;
+    const void* dy;
+    long long lddy;
+    int dydt;
+    const float* gamma;
+    const float* rstd;
+    const void* dres;
+    long long lddres;
+    void* dx;
+    long long lddx;
+    float* dgamma;
+} sadmm_rmsnorm_bwd_args;
+size_t sadmm_rmsnorm_bwd_workspace_size(const sadmm_rmsnorm_bwd_args* a);
+sadmm_status sadmm_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * x [rows][cols] of type xdt (bf16 or fp32) in 8 bits: `out`, and its
+ * transpose [cols][rows] `out_t` with blocks along x's rows; either may have q
+ * NULL.  With `tile` blocks are 128 x 128, the same for both.
+ */
+typedef struct {
+    long long rows, cols;
+    const void* x;
+    long long ldx;
+    int xdt;
+    int tile;
+    sadmm_q8_out out, out_t;
+} sadmm_quantize_args;
+sadmm_status sadmm_quantize(const sadmm_quantize_args* a, void* stream);
+
+/*
+ * y = act(z) + residual, z = x W^T + bias, of 8-bit x [tokens][n_in] and
+ * w [n_out][n_in]; the rest as in sadmm_linear_fwd.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_out;
+    sadmm_q8 x, w;
+    const float* bias;
+    const void* residual;
+    long long ldr;
+    int act;
+    void* y;
+    long long ldy;
+    int ydt;
+    void* z;
+    long long ldz;
+} sadmm_linear8_fwd_args;
+size_t sadmm_linear8_fwd_workspace_size(const sadmm_linear8_fwd_args* a);
+sadmm_status sadmm_linear8_fwd(const sadmm_linear8_fwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass, dz = dy act'(z), made 8-bit with blocks of one row and 128
+ * columns for dx, of one column and 128 tokens for dw:
+ *   dx = dz W    [tokens][n_in] of type dxdt
+ *   dw = dz^T x  [n_out][n_in] of type dwdt
+ *   db = sum over tokens of dz, before that  [n_out]
+ *   xt  8-bit [n_in][tokens], x's transpose (read for dw);
+ *   wt  8-bit [n_in][n_out], w's (read for dx).
+ * The rest as in sadmm_linear_bwd.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_out;
+    const void* dy;
+    long long lddy;
+    int dydt;
+    sadmm_q8 xt, wt;
+    const void* z;
+    long long ldz;
+    int act;
+    void* dx;
+    long long lddx;
+    int dxdt;
+    void* dw;
+    long long lddw;
+    int dwdt;
+    float* db;
+} sadmm_linear8_bwd_args;
+size_t sadmm_linear8_bwd_workspace_size(const sadmm_linear8_bwd_args* a);
+sadmm_status sadmm_linear8_bwd(const sadmm_linear8_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * h = act(g) * u, g = x Wg^T + bg, u = x Wu^T + bu, of 8-bit x [tokens][n_in]
+ * and wg, wu [n_hidden][n_in].  h is bf16 (hdt SADMM_BF16), or with SADMM_E4M3
+ * 8-bit, h8, with blocks of one row, made of the fp32 values.  The rest as in
+ * sadmm_gated_fwd.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_hidden;
+    sadmm_q8 x, wg, wu;
+    const float* bg;
+    const float* bu;
+    int act;
+    void* h;
+    long long ldh;
+    int hdt;
+    sadmm_q8_out h8;
+    void* g;
+    long long ldg;
+    void* u;
+    long long ldu;
+} sadmm_gated8_fwd_args;
+size_t sadmm_gated8_fwd_workspace_size(const sadmm_gated8_fwd_args* a);
+sadmm_status sadmm_gated8_fwd(const sadmm_gated8_fwd_args* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass, dg = dh u act'(g), du = dh act(g), each made 8-bit as dz
+ * of sadmm_linear8_bwd:
+ *   dx  = dg Wg + du Wu   [tokens][n_in] of type dxdt
+ *   dwg = dg^T x, dwu = du^T x   [n_hidden][n_in] of type dwdt (both or neither)
+ *   dbg, dbu = sums over tokens of dg, du, before that   [n_hidden]
+ *   xt 8-bit [n_in][tokens];  wgt, wut 8-bit [n_in][n_hidden].
+ * The rest as in sadmm_gated_bwd.
+ */
+typedef struct {
+    long long tokens;
+    int n_in, n_hidden;
+    const void* dh;
+    long long lddh;
+    sadmm_q8 xt, wgt, wut;
+    const void* g;
+    long long ldg;
+    const void* u;
+    long long ldu;
+    int act;
+    void* dx;
+    long long lddx;
+    int dxdt;
+    void* dwg;
+    long long lddwg;
+    void* dwu;
+    long long lddwu;
+    int dwdt;
+    float* dbg;
+    float* dbu;
+} sadmm_gated8_bwd_args;
+size_t sadmm_gated8_bwd_workspace_size(const sadmm_gated8_bwd_args* a);
+sadmm_status sadmm_gated8_bwd(const sadmm_gated8_bwd_args* a, void* workspace, size_t ws_bytes, void* stream);
 
 /*
  * Failure-detection self-test; the paper has no counterpart.  Runs, in one

@@ -9,4 +9,5 @@ from .sadmm import (  # noqa: F401
     SADMM_ACT_NONE, SADMM_ACT_RELU, SADMM_ACT_GELU, SADMM_ACT_SILU,
     SadmmError, PrunedConv, project_groups, load, make_desc,
     layer_norm, layer_norm_backward, linear, linear_backward, gated, gated_backward,
+    SADMM_E4M3, rms_norm, rms_norm_backward, quantize, linear8, linear8_backward, gated8, gated8_backward,
 )

@@ -31,7 +31,7 @@ DEBUG_LIB = os.path.join(BUILD, "debug", "libsadmm.so")
 
 SOURCES = ["abi.cu", "project.cu", "pack.cu", "conv_fwd.cu", "conv_slab.cu", "admm.cu", "elements.cu", "gemm.cu",
            "bwd.cu", "bwd_slab.cu", "bwd_grid.cu", "conv_grid.cu", "sparse.cu", "abi_ffn.cu", "norm.cu", "linear.cu",
-           "tgemm.cu", "tgemm_pair.cu", "few.cu"]
+           "tgemm.cu", "tgemm_pair.cu", "few.cu", "abi_q8.cu", "rms.cu", "quant.cu", "linear8.cu", "q8gemm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -117,14 +117,15 @@ def build_torch_binding(force: bool = False) -> str:
     note = TORCH_LIB + ".for"
     if not force and os.path.exists(TORCH_LIB) and os.path.exists(note) and open(note).read() == made_for:
         t = os.path.getmtime(TORCH_LIB)
-        if all(os.path.getmtime(p) <= t for p in (src, os.path.join(INCLUDE, "sadmm.h"))):
+        deps = [os.path.join(CSRC, h) for h in ("torch_call.h", "torch_q8.h")] + [os.path.join(INCLUDE, "sadmm.h")]
+        if all(os.path.getmtime(p) <= t for p in [src] + deps):
             return TORCH_LIB
     os.makedirs(BUILD, exist_ok=True)
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
     tmp = TORCH_LIB + f".tmp{os.getpid()}"
     abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-I", INCLUDE,
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-I", INCLUDE, "-I", CSRC,
            "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
            "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
            "-isystem", os.path.join(cuda, "include"), src, "-o", tmp, "-L", os.path.join(base, "lib"),

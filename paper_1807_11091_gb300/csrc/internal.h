@@ -184,6 +184,20 @@ size_t layernorm_bwd_bytes(const sadmm_layernorm_bwd_args& a);
 sadmm_status launch_layernorm_fwd(const sadmm_layernorm_fwd_args& a, cudaStream_t s);
 sadmm_status launch_layernorm_bwd(const sadmm_layernorm_bwd_args& a, void* ws, cudaStream_t s);
 
+// ---- operators of 8-bit operands (rms.cu, quant.cu, linear8.cu) ----
+size_t rmsnorm_bwd_bytes(const sadmm_rmsnorm_bwd_args& a);
+sadmm_status launch_rmsnorm_fwd(const sadmm_rmsnorm_fwd_args& a, cudaStream_t s);
+sadmm_status launch_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_quantize(const sadmm_quantize_args& a, cudaStream_t s);
+size_t linear8_fwd_bytes(const sadmm_linear8_fwd_args& a);
+size_t linear8_bwd_bytes(const sadmm_linear8_bwd_args& a);
+size_t gated8_fwd_bytes(const sadmm_gated8_fwd_args& a);
+size_t gated8_bwd_bytes(const sadmm_gated8_bwd_args& a);
+sadmm_status launch_linear8_fwd(const sadmm_linear8_fwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_linear8_bwd(const sadmm_linear8_bwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_gated8_fwd(const sadmm_gated8_fwd_args& a, void* ws, cudaStream_t s);
+sadmm_status launch_gated8_bwd(const sadmm_gated8_bwd_args& a, void* ws, cudaStream_t s);
+
 // Tap-mask encoding of the gather table: 0 = one bit per tap (at most 31
 // taps), 1 = (kt,kh) row bits 0..15 and kw bits 16..30.  Bit 31 marks padding
 // columns and is never valid.

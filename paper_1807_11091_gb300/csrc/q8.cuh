@@ -1,0 +1,226 @@
+// q8.cuh -- 8-bit matrices (e4m3 values, an fp32 scale for each block of 128):
+// what their kernels share, and the host interface of the products.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "internal.h"
+#include "output.cuh"
+#include "tgemm.cuh"
+
+namespace sadmm {
+
+constexpr int kQBlock = 128;
+
+// ------------------------------------------------------------------- host --
+
+// One 8-bit operand of a product: `rows` rows of the output's row (or column)
+// index, each `k` long; aligned for the tensor-memory accelerator.
+struct Q8Operand {
+    const void* p;
+    long long rows, k, ld;
+    const float* s;
+    long long s_row, s_block;
+    int shift;             // rows of a scale: 1 << shift
+};
+
+// C = A B^T in one of tgemm.cuh's modes.  kTgGated with y8.q: y in 8 bits.
+struct Q8Problem {
+    int mode;
+    Q8Operand a[2], b[2];
+    long long m, n;
+    const float* bias;
+    const float* bias2;
+    int act;
+    TgMatrix y, residual, z, u;
+    sadmm_q8_out y8;
+};
+
+inline bool q8_aligned(const void* p, long long ld)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 15) == 0;
+}
+
+sadmm_status launch_q8_product(const Q8Problem& t, cudaStream_t s);
+
+// Matrices in 8 bits (quant.cu).  What is made 8-bit: x; dy act'(z) (z given); or
+// the gated pair's dg and du (u given), whose outputs are [0] and [1].  sums: column
+// sums of the values, or NULL.
+struct Q8Source {
+    const void* x;
+    long long ldx;
+    int xdt;
+    const void* z;
+    long long ldz;
+    const void* u;
+    long long ldu;
+    int act;
+    long long rows, cols;
+    int tile;
+    sadmm_q8_out out[2], out_t[2];
+    float* sums[2];
+};
+size_t q8_source_bytes(const Q8Source& a);  // scratch of the column sums
+sadmm_status launch_q8_source(const Q8Source& a, void* ws, cudaStream_t s);
+
+// ----------------------------------------------------------------- device --
+
+#ifdef __CUDACC__
+
+// A block's scale from its largest magnitude, and the quotients x / s of the
+// block as fp32 divisions round them: q = x r with r = 1 / s and one correction,
+// q + r (x - q s), which gives the nearest number where r is the nearest to 1 / s
+// (Markstein, 1990, theorem 8); an infinite x gives NaN.  A tenth of a division's
+// time a value (1 / s is taken once a block).
+struct Q8Scale {
+    float s, r;
+};
+constexpr float kE4m3Max = 448.0f;
+SADMM_DEV Q8Scale q8_scale(float top)
+{
+    Q8Scale q;
+    q.s = __fdiv_rn(fmaxf(top, 1.2621774483536189e-29f /* 2^-96 */), kE4m3Max);
+    q.r = __frcp_rn(q.s);
+    return q;
+}
+SADMM_DEV float q8_quotient(float x, const Q8Scale& k)
+{
+    const float q = __fmul_rn(x, k.r);
+    return __fmaf_rn(__fmaf_rn(-q, k.s, x), k.r, q);
+}
+// What x counts for in its block's largest magnitude.
+SADMM_DEV float q8_size(float x)
+{
+    const float a = fabsf(x);
+    return a < __int_as_float(0x7f800000) ? a : 0.0f;
+}
+SADMM_DEV uint32_t q8_two(float lo, float hi)
+{
+    return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+}
+SADMM_DEV uint32_t q8_four(float a, float b, float c, float d) { return q8_two(a, b) | q8_two(c, d) << 16; }
+
+// The largest of v over groups of 16 lanes.
+SADMM_DEV float max16(float v)
+{
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// A matrix as bytes: it starts at lo and ends at hi.
+struct Span {
+    const uint8_t *lo, *hi;
+};
+
+// The 16 bytes at p.  Off a 16-byte boundary they come from the two aligned words that
+// hold them, where these lie inside the matrix; else the `n` wanted ones one by
+// one, zeros after them.
+SADMM_DEV uint4 load16(const uint8_t* p, int n, const Span& m)
+{
+    const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+    const uint8_t* w = p - off;
+    if (off == 0 && p >= m.lo && p + 16 <= m.hi) return *reinterpret_cast<const uint4*>(p);
+    if (w >= m.lo && w + 32 <= m.hi) {
+        const uint4 a = *reinterpret_cast<const uint4*>(w), b = *reinterpret_cast<const uint4*>(w + 16);
+        uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) v[i] = v[i + 1];
+            v[6] = b.w;
+        }
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) v[i] = v[i + 2];
+        }
+        const int sh = (off & 3) * 8;
+        return make_uint4(__funnelshift_r(v[0], v[1], sh), __funnelshift_r(v[1], v[2], sh),
+                          __funnelshift_r(v[2], v[3], sh), __funnelshift_r(v[3], v[4], sh));
+    }
+    uint32_t v[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < n && p + i >= m.lo && p + i < m.hi) v[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// Eight neighbours of a bf16 (dt SADMM_BF16) or fp32 matrix at element p, `n` of
+// them wanted (at least one); zeros after those.
+SADMM_DEV void load8(const void* p, int dt, int n, const Span& m, float (&v)[8])
+{
+    const uint8_t* b = static_cast<const uint8_t*>(p);
+    if (dt == SADMM_BF16) {
+        const uint4 q = load16(b, 2 * n, m);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = __uint_as_float(w[j] << 16);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    } else {
+        const uint4 lo = load16(b, 4 * n, m);
+        const uint4 hi = n > 4 ? load16(b + 16, 4 * n - 16, m) : make_uint4(0, 0, 0, 0);
+        v[0] = __uint_as_float(lo.x); v[1] = __uint_as_float(lo.y);
+        v[2] = __uint_as_float(lo.z); v[3] = __uint_as_float(lo.w);
+        v[4] = __uint_as_float(hi.x); v[5] = __uint_as_float(hi.y);
+        v[6] = __uint_as_float(hi.z); v[7] = __uint_as_float(hi.w);
+    }
+    if (n < 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j >= n) v[j] = 0.0f;
+    }
+}
+
+// Eight neighbours to element p, of which n are inside the row.
+SADMM_DEV void store8(void* p, int dt, int n, const float (&v)[8])
+{
+    if (dt == SADMM_BF16) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p);
+        if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) o[j] = __float2bfloat16_rn(v[j]);
+    } else {
+        float* o = static_cast<float*>(p);
+        if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+            reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) o[j] = v[j];
+    }
+}
+
+// Eight bytes to p, of which n are inside the row.
+SADMM_DEV void store_bytes8(uint8_t* p, int n, uint32_t lo, uint32_t hi)
+{
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 7) == 0) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
+        return;
+    }
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
+        reinterpret_cast<uint32_t*>(p)[0] = lo;
+        reinterpret_cast<uint32_t*>(p)[1] = hi;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < n) p[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+}
+
+#endif
+
+}  // namespace sadmm

@@ -1,0 +1,455 @@
+// rms.cu -- root-mean-square norm of rows, with the residual's addition before
+// it and its output in 8 bits where wanted, forward and backward.
+//
+//   h = x + residual (rounded to the residual's type),  y = gamma h rstd,
+//   rstd = (avg h^2 + eps)^-1/2
+//   d = gamma dy,  dx = rstd (d - hhat avg(d hhat)) [+ dres],  hhat = h rstd
+//   dgamma = sum over rows of dy hhat
+#include "q8.cuh"
+
+namespace sadmm {
+namespace {
+
+SADMM_DEV float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The sum over a row's threads: a warp, or the block, whose warps' sums every
+// thread adds up in the same order.  `slot` alternates between calls.
+struct __align__(16) RowSums {
+    float v[2][32];
+};
+template <bool BLOCK>
+SADMM_DEV float row_sum(float v, RowSums& red, int slot)
+{
+    v = warp_sum(v);
+    if (BLOCK) {
+        const int n = blockDim.x >> 5;
+        if ((threadIdx.x & 31) == 0) red.v[slot][threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.0f;
+        for (int w = 0; w < n; w += 4) {  // the places past the last warp hold zeros
+            const float4 q = *reinterpret_cast<const float4*>(&red.v[slot][w]);
+            v += (q.x + q.y) + (q.z + q.w);
+        }
+    }
+    return v;
+}
+SADMM_DEV void clear(RowSums& red)
+{
+    for (int i = threadIdx.x; i < 64; i += blockDim.x) (&red.v[0][0])[i] = 0.0f;
+}
+
+SADMM_DEV float round_to(float v, int dt) { return dt == SADMM_BF16 ? __bfloat162float(__float2bfloat16_rn(v)) : v; }
+
+// Row r of a matrix of bf16 or fp32 elements.
+struct Rows {
+    const void* p;
+    long long ld, rows;
+    int dt, cols;
+    SADMM_DEV int size() const { return dt == SADMM_BF16 ? 2 : 4; }
+    SADMM_DEV Span span() const
+    {
+        const uint8_t* b = static_cast<const uint8_t*>(p);
+        return {b, b + ((rows - 1) * ld + cols) * size()};
+    }
+    SADMM_DEV void load(long long r, int c, const Span& m, float (&v)[8], int* status) const
+    {
+        const int n = min(8, cols - c);
+        if (n <= 0 || !dbg_in(r, rows, status) || !dbg_run(c, n, cols, status)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+            return;
+        }
+        load8(static_cast<const uint8_t*>(p) + (r * ld + c) * size(), dt, n, m, v);
+    }
+    SADMM_DEV void store(long long r, int c, const float (&v)[8], int* status) const
+    {
+        const int n = min(8, cols - c);
+        if (n <= 0 || !dbg_in(r, rows, status) || !dbg_run(c, n, cols, status)) return;
+        store8(const_cast<uint8_t*>(static_cast<const uint8_t*>(p)) + (r * ld + c) * size(), dt, n, v);
+    }
+};
+
+struct FwdArgs {
+    Rows x, res, h, y;    // p NULL: not there
+    sadmm_q8_out y8;
+    const float* gamma;
+    float* rstd;
+    long long rows;
+    int cols;
+    float eps, n;
+    int* status;
+};
+
+// Columns c .. c+7 of row r: the value of h that the norm reads.
+SADMM_DEV void load_h(const FwdArgs& a, long long r, int c, const Span& mx, const Span& mr, float (&v)[8])
+{
+    a.x.load(r, c, mx, v, a.status);
+    if (a.res.p) {
+        float e[8];
+        a.res.load(r, c, mr, e, a.status);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = round_to(v[j] + e[j], a.res.dt);
+    }
+}
+
+// Columns c .. c+7 of y; in 8 bits the 16 lanes of a block share its scale (all
+// 32 lanes of the warp call it).
+SADMM_DEV void finish8(const FwdArgs& a, long long r, int c, float rstd, float (&v)[8])
+{
+    if (a.gamma) {
+        const int n = min(8, a.cols - c);
+        const bool whole = n == 8 && (reinterpret_cast<uintptr_t>(a.gamma) & 15) == 0;
+        if (whole && dbg_run(c, 8, a.cols, a.status)) {
+            const float4 p = *reinterpret_cast<const float4*>(a.gamma + c), q = *reinterpret_cast<const float4*>(a.gamma + c + 4);
+            const float g[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = v[j] * rstd * g[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] * rstd * a.gamma[c + j] : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= rstd;
+    }
+    if (!a.y8.q) {
+        a.y.store(r, c, v, a.status);
+        return;
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, q8_size(v[j]));
+    const Q8Scale k = q8_scale(max16(top));
+    if (c >= a.cols || !dbg_in(c, a.cols, a.status) || !dbg_in(r, a.rows, a.status)) return;
+    if ((threadIdx.x & 15) == 0) a.y8.s[r * a.y8.s_row + c / kQBlock * a.y8.s_block] = k.s;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = q8_quotient(v[j], k);
+    store_bytes8(static_cast<uint8_t*>(a.y8.q) + r * a.y8.ld + c, a.cols - c, q8_four(v[0], v[1], v[2], v[3]),
+                 q8_four(v[4], v[5], v[6], v[7]));
+}
+
+// A row over a group of threads, a warp or a block, E times 8 neighbours each,
+// kept in registers between the sum and the output.
+template <bool BLOCK, int E>
+__global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rms_fwd(const FwdArgs a)
+{
+    __shared__ RowSums red;
+    const int G = BLOCK ? blockDim.x : 32, t = BLOCK ? threadIdx.x : threadIdx.x & 31;
+    const long long r = BLOCK ? (long long)blockIdx.x : (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (BLOCK) {
+        clear(red);
+        __syncthreads();
+    }
+    pdl_wait();
+    pdl_trigger();
+    if (r >= a.rows) return;
+    const Span mx = a.x.span(), mr = a.res.p ? a.res.span() : mx;
+    float v[E][8], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < E; ++k) load_h(a, r, (k * G + t) * 8, mx, mr, v[k]);
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+        if (a.h.p) a.h.store(r, (k * G + t) * 8, v[k], a.status);
+        float p = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p += v[k][j] * v[k][j];
+        sum += p;
+    }
+    const float rstd = rsqrtf(row_sum<BLOCK>(sum, red, 0) / a.n + a.eps);
+    if (t == 0 && a.rstd) a.rstd[r] = rstd;
+#pragma unroll
+    for (int k = 0; k < E; ++k) finish8(a, r, (k * G + t) * 8, rstd, v[k]);
+}
+
+// Rows of any length: a block a row, read twice (the sum from h where it is written,
+// which may be the residual's own place).
+__global__ void __launch_bounds__(1024) k_rms_fwd_long(const FwdArgs a)
+{
+    __shared__ RowSums red;
+    clear(red);
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    const long long r = blockIdx.x;
+    const Span mx = a.x.span(), mr = a.res.p ? a.res.span() : mx, mh = a.h.p ? a.h.span() : mx;
+    float sum = 0.0f;
+    for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
+        float v[8];
+        load_h(a, r, c, mx, mr, v);
+        if (a.h.p) a.h.store(r, c, v, a.status);
+        float p = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p += v[j] * v[j];
+        sum += p;
+    }
+    const float rstd = rsqrtf(row_sum<true>(sum, red, 0) / a.n + a.eps);
+    if (threadIdx.x == 0 && a.rstd) a.rstd[r] = rstd;
+    const int end = (a.cols + 255) & ~255;  // a whole warp's columns
+    for (int c = threadIdx.x * 8; c < end; c += 8192) {
+        float v[8];
+        if (a.h.p)
+            a.h.load(r, c, mh, v, a.status);
+        else
+            load_h(a, r, c, mx, mr, v);
+        finish8(a, r, c, rstd, v);
+    }
+}
+
+struct BwdArgs {
+    Rows h, dy, dres, dx;
+    const float* gamma;
+    const float* rstd;
+    float* part;          // [blocks][cols] partial dgamma; NULL: not wanted
+    long long rows;
+    int cols;
+    float inv_n;
+    int* status;
+};
+
+SADMM_DEV void load_gamma(const BwdArgs& a, int c, float (&g)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = !a.gamma ? 1.0f : c + j < a.cols ? a.gamma[c + j] : 0.0f;
+}
+
+// A block takes rows blockIdx.x, + gridDim.x, ...: its threads own columns, add up
+// their shares of dgamma in registers and leave one partial sum a block.
+template <int E>
+__global__ void __launch_bounds__(512) k_rms_bwd(const BwdArgs a)
+{
+    __shared__ RowSums red;
+    clear(red);
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    const int G = blockDim.x, t = threadIdx.x;
+    const Span mh = a.h.span(), my = a.dy.span(), md = a.dres.p ? a.dres.span() : mh;
+    float g[E][8], dg[E][8];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+        load_gamma(a, (k * G + t) * 8, g[k]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dg[k][j] = 0.0f;
+    }
+    int slot = 0;
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const float rstd = a.rstd[r];
+        float hv[E][8], dv[E][8], s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            a.h.load(r, (k * G + t) * 8, mh, hv[k], a.status);
+            a.dy.load(r, (k * G + t) * 8, my, dv[k], a.status);
+        }
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                hv[k][j] *= rstd;
+                dg[k][j] += dv[k][j] * hv[k][j];
+                dv[k][j] *= g[k][j];
+                s += dv[k][j] * hv[k][j];
+            }
+        const float m = row_sum<true>(s, red, slot) * a.inv_n;
+        slot ^= 1;
+        if (!a.dx.p) continue;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            float e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = 0.0f;
+            if (a.dres.p) a.dres.load(r, (k * G + t) * 8, md, e, a.status);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = rstd * (dv[k][j] - hv[k][j] * m) + e[j];
+            a.dx.store(r, (k * G + t) * 8, e, a.status);
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int k = 0; k < E; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = (k * G + t) * 8 + j;
+            if (c < a.cols) a.part[(long long)blockIdx.x * a.cols + c] = dg[k][j];
+        }
+}
+
+// Rows of any length: dx, a block a row, read twice.
+__global__ void __launch_bounds__(1024) k_rms_bwd_long(const BwdArgs a)
+{
+    __shared__ RowSums red;
+    clear(red);
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    const long long r = blockIdx.x;
+    const Span mh = a.h.span(), my = a.dy.span(), md = a.dres.p ? a.dres.span() : mh;
+    const float rstd = a.rstd[r];
+    float s = 0.0f;
+    for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
+        float h[8], d[8], g[8];
+        a.h.load(r, c, mh, h, a.status);
+        a.dy.load(r, c, my, d, a.status);
+        load_gamma(a, c, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += d[j] * g[j] * (h[j] * rstd);
+    }
+    const float m = row_sum<true>(s, red, 0) * a.inv_n;
+    for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
+        float h[8], d[8], g[8], e[8];
+        a.h.load(r, c, mh, h, a.status);
+        a.dy.load(r, c, my, d, a.status);
+        load_gamma(a, c, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = 0.0f;
+        if (a.dres.p) a.dres.load(r, c, md, e, a.status);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = rstd * (d[j] * g[j] - h[j] * rstd * m) + e[j];
+        a.dx.store(r, c, e, a.status);
+    }
+}
+
+// Rows of any length: partial dgamma of 2048 columns over the rows blockIdx.y,
+// blockIdx.y + gridDim.y, ...
+__global__ void __launch_bounds__(256) k_rms_cols_long(const BwdArgs a)
+{
+    pdl_wait();
+    pdl_trigger();
+    const Span mh = a.h.span(), my = a.dy.span();
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (c >= a.cols) return;
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (long long r = blockIdx.y; r < a.rows; r += gridDim.y) {
+        float h[8], d[8];
+        a.h.load(r, c, mh, h, a.status);
+        a.dy.load(r, c, my, d, a.status);
+        const float rstd = a.rstd[r];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += d[j] * (h[j] * rstd);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c + j < a.cols) a.part[(long long)blockIdx.y * a.cols + c + j] = s[j];
+}
+
+// out[c] = the sum of part[0 .. parts-1][c]: 32 groups of parts, then the groups in order.
+__global__ void __launch_bounds__(1024) k_rms_sums(const float* __restrict__ part, float* __restrict__ out, int cols,
+                                                   int parts)
+{
+    __shared__ float red[32][33];
+    pdl_wait();
+    pdl_trigger();
+    const int g = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * 32 + lane;
+    float v = 0.0f;
+    if (c < cols) {
+#pragma unroll 16
+        for (int k = g; k < parts; k += 32) v += part[(size_t)k * cols + c];
+    }
+    red[g][lane] = v;
+    __syncthreads();
+    v = warp_sum(red[lane][g]);
+    if (lane == 0 && blockIdx.x * 32 + g < cols) out[blockIdx.x * 32 + g] = v;
+}
+
+// -------------------------------------------------------------------- host --
+
+constexpr int kWarpCols = 512;          // up to here a warp takes a row
+constexpr int kFwdCols = 32768;         // up to here a row stays in registers (1024 threads of 32)
+constexpr int kBwdCols = 8192;          // backward: 512 threads of 16
+
+int row_threads(int cols, int e) { return (int)round_up((cols + 8 * e - 1) / (8 * e), 32); }
+
+int bwd_blocks(long long rows)
+{
+    const long long most = 2ll * device_sm_count();
+    return (int)(rows < most ? rows : most);
+}
+
+Rows rows_of(const void* p, long long ld, int dt, long long rows, int cols) { return {p, ld, rows, dt, cols}; }
+
+template <bool BLOCK, int E>
+cudaError_t fwd(const FwdArgs& a, cudaStream_t s)
+{
+    const long long grid = BLOCK ? a.rows : (a.rows + 7) / 8;
+    return launch_pdl(k_rms_fwd<BLOCK, E>, dim3((unsigned)grid), dim3(BLOCK ? row_threads(a.cols, E) : 256), 0, s, a);
+}
+
+}  // namespace
+
+sadmm_status launch_rmsnorm_fwd(const sadmm_rmsnorm_fwd_args& a, cudaStream_t s)
+{
+    if (a.rows == 0) return SADMM_OK;
+    FwdArgs f = {};
+    f.x = rows_of(a.x, a.ldx, a.xdt, a.rows, a.cols);
+    f.res = rows_of(a.residual, a.ldr, a.rdt, a.rows, a.cols);
+    f.h = rows_of(a.h, a.ldh, a.rdt, a.rows, a.cols);
+    f.y = rows_of(a.y, a.ldy, a.ydt, a.rows, a.cols);
+    if (a.ydt == SADMM_E4M3) f.y8 = a.y8;
+    f.gamma = a.gamma;
+    f.rstd = a.rstd;
+    f.rows = a.rows;
+    f.cols = a.cols;
+    f.eps = a.eps;
+    f.n = (float)a.cols;
+    f.status = device_status_ptr();
+    cudaError_t err;
+    if (a.cols <= 256)
+        err = fwd<false, 1>(f, s);
+    else if (a.cols <= kWarpCols)
+        err = fwd<false, 2>(f, s);
+    else if (a.cols <= 8192)
+        err = fwd<true, 2>(f, s);
+    else if (a.cols <= kFwdCols)
+        err = fwd<true, 4>(f, s);
+    else
+        err = launch_pdl(k_rms_fwd_long, dim3((unsigned)a.rows), dim3(1024), 0, s, f);
+    return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+}
+
+size_t rmsnorm_bwd_bytes(const sadmm_rmsnorm_bwd_args& a)
+{
+    return a.dgamma ? (size_t)bwd_blocks(a.rows) * (size_t)a.cols * 4 : 0;
+}
+
+sadmm_status launch_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args& a, void* ws, cudaStream_t s)
+{
+    if (a.rows == 0) {
+        if (a.dgamma && cudaMemsetAsync(a.dgamma, 0, (size_t)a.cols * 4, s) != cudaSuccess) return SADMM_ECUDA;
+        return SADMM_OK;
+    }
+    BwdArgs b = {};
+    b.h = rows_of(a.h, a.ldh, a.hdt, a.rows, a.cols);
+    b.dy = rows_of(a.dy, a.lddy, a.dydt, a.rows, a.cols);
+    b.dres = rows_of(a.dres, a.lddres, a.hdt, a.rows, a.cols);
+    b.dx = rows_of(a.dx, a.lddx, a.hdt, a.rows, a.cols);
+    b.gamma = a.gamma;
+    b.rstd = a.rstd;
+    b.part = a.dgamma ? static_cast<float*>(ws) : nullptr;
+    b.rows = a.rows;
+    b.cols = a.cols;
+    b.inv_n = (float)(1.0 / a.cols);
+    b.status = device_status_ptr();
+    const int blocks = bwd_blocks(a.rows);
+    cudaError_t err = cudaSuccess;
+    if (a.cols <= 2048) {
+        err = launch_pdl(k_rms_bwd<1>, dim3(blocks), dim3(row_threads(a.cols, 1)), 0, s, b);
+    } else if (a.cols <= kBwdCols) {
+        err = launch_pdl(k_rms_bwd<2>, dim3(blocks), dim3(row_threads(a.cols, 2)), 0, s, b);
+    } else {
+        if (a.dx) err = launch_pdl(k_rms_bwd_long, dim3((unsigned)a.rows), dim3(1024), 0, s, b);
+        if (err == cudaSuccess && b.part)
+            err = launch_pdl(k_rms_cols_long, dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)blocks), dim3(256), 0,
+                             s, b);
+    }
+    if (err == cudaSuccess && b.part)
+        err = launch_pdl(k_rms_sums, dim3((unsigned)((a.cols + 31) / 32)), dim3(1024), 0, s, b.part, a.dgamma, a.cols,
+                         blocks);
+    return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+}
+
+}  // namespace sadmm

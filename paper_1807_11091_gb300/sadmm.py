@@ -19,7 +19,7 @@ from typing import Optional, Sequence, Tuple
 from . import build as _build
 
 SADMM_OK, SADMM_EINVAL, SADMM_ECUDA, SADMM_ETIMEOUT, SADMM_EUNSUPPORTED, SADMM_EBOUNDS = 0, -1, -2, -3, -4, -5
-SADMM_BF16, SADMM_FP32 = 0, 1
+SADMM_BF16, SADMM_FP32, SADMM_E4M3 = 0, 1, 2
 SADMM_COL_NONE, SADMM_COL_SHAPE, SADMM_COL_CHANNEL = 0, 1, 2
 SADMM_FWD_ALL, SADMM_FWD_INPUT, SADMM_FWD_REST = 0, 1, 2
 
@@ -120,10 +120,23 @@ class PackItem(ctypes.Structure):
                 ("col_idx", ctypes.c_void_p), ("dev", ctypes.c_void_p), ("dev_bytes", ctypes.c_size_t)]
 
 
+class Q8(ctypes.Structure):
+    """sadmm_q8: an 8-bit operand."""
+    _fields_ = [("q", ctypes.c_void_p), ("ld", ctypes.c_longlong), ("s", ctypes.c_void_p),
+                ("s_row", ctypes.c_longlong), ("s_block", ctypes.c_longlong), ("tile", ctypes.c_int)]
+
+
+class Q8Out(ctypes.Structure):
+    """sadmm_q8_out: an 8-bit output."""
+    _fields_ = [("q", ctypes.c_void_p), ("ld", ctypes.c_longlong), ("s", ctypes.c_void_p),
+                ("s_row", ctypes.c_longlong), ("s_block", ctypes.c_longlong)]
+
+
 def _args(name: str, spec: str):
     """A ctypes mirror of sadmm_<name>_args: `spec` lists its fields as
-    <kind>:<field>, with l long long, i int, f float and p a pointer."""
-    kinds = {"l": ctypes.c_longlong, "i": ctypes.c_int, "f": ctypes.c_float, "p": ctypes.c_void_p}
+    <kind>:<field>, with l long long, i int, f float, p a pointer, m and o an
+    8-bit operand and output."""
+    kinds = {"l": ctypes.c_longlong, "i": ctypes.c_int, "f": ctypes.c_float, "p": ctypes.c_void_p, "m": Q8, "o": Q8Out}
     fields = [(f.split(":")[1], kinds[f.split(":")[0]]) for f in spec.split()]
     return type(name, (ctypes.Structure,), {"_fields_": fields})
 
@@ -140,6 +153,19 @@ GatedFwdArgs = _args("GatedFwdArgs", "l:tokens i:n_in i:n_hidden p:x l:ldx p:wg 
                      "p:h l:ldh p:g l:ldg p:u l:ldu")
 GatedBwdArgs = _args("GatedBwdArgs", "l:tokens i:n_in i:n_hidden p:dh l:lddh p:x l:ldx p:wg l:ldwg p:wu l:ldwu p:g l:ldg "
                      "p:u l:ldu i:act p:dx l:lddx i:dxdt p:dwg l:lddwg p:dwu l:lddwu i:dwdt p:dbg p:dbu")
+RmsNormFwdArgs = _args("RmsNormFwdArgs", "l:rows i:cols p:x l:ldx i:xdt p:residual l:ldr i:rdt p:h l:ldh p:gamma f:eps "
+                       "p:y l:ldy i:ydt o:y8 p:rstd")
+RmsNormBwdArgs = _args("RmsNormBwdArgs", "l:rows i:cols p:h l:ldh i:hdt p:dy l:lddy i:dydt p:gamma p:rstd p:dres l:lddres "
+                       "p:dx l:lddx p:dgamma")
+QuantizeArgs = _args("QuantizeArgs", "l:rows l:cols p:x l:ldx i:xdt i:tile o:out o:out_t")
+Linear8FwdArgs = _args("Linear8FwdArgs", "l:tokens i:n_in i:n_out m:x m:w p:bias p:residual l:ldr i:act p:y l:ldy i:ydt "
+                       "p:z l:ldz")
+Linear8BwdArgs = _args("Linear8BwdArgs", "l:tokens i:n_in i:n_out p:dy l:lddy i:dydt m:xt m:wt p:z l:ldz i:act p:dx l:lddx "
+                       "i:dxdt p:dw l:lddw i:dwdt p:db")
+Gated8FwdArgs = _args("Gated8FwdArgs", "l:tokens i:n_in i:n_hidden m:x m:wg m:wu p:bg p:bu i:act p:h l:ldh i:hdt o:h8 "
+                      "p:g l:ldg p:u l:ldu")
+Gated8BwdArgs = _args("Gated8BwdArgs", "l:tokens i:n_in i:n_hidden p:dh l:lddh m:xt m:wgt m:wut p:g l:ldg p:u l:ldu i:act "
+                      "p:dx l:lddx i:dxdt p:dwg l:lddwg p:dwu l:lddwu i:dwdt p:dbg p:dbu")
 
 
 _lib = None
@@ -218,8 +244,13 @@ def load():
     lib.sadmm_project_groups_noalloc.argtypes = [P(ConvDesc), vp, vp, ci, ci, ci, ci, vp, vp, vp, vp]
     lib.sadmm_layernorm_fwd.restype = ci
     lib.sadmm_layernorm_fwd.argtypes = [P(LayerNormFwdArgs), vp]
+    for name, args in (("rmsnorm_fwd", RmsNormFwdArgs), ("quantize", QuantizeArgs)):
+        call = getattr(lib, f"sadmm_{name}")
+        call.restype, call.argtypes = ci, [P(args), vp]
     for name, args in (("layernorm_bwd", LayerNormBwdArgs), ("linear_fwd", LinearFwdArgs),
-                       ("linear_bwd", LinearBwdArgs), ("gated_fwd", GatedFwdArgs), ("gated_bwd", GatedBwdArgs)):
+                       ("linear_bwd", LinearBwdArgs), ("gated_fwd", GatedFwdArgs), ("gated_bwd", GatedBwdArgs),
+                       ("rmsnorm_bwd", RmsNormBwdArgs), ("linear8_fwd", Linear8FwdArgs),
+                       ("linear8_bwd", Linear8BwdArgs), ("gated8_fwd", Gated8FwdArgs), ("gated8_bwd", Gated8BwdArgs)):
         size, call = getattr(lib, f"sadmm_{name}_workspace_size"), getattr(lib, f"sadmm_{name}")
         size.restype, size.argtypes = sz, [P(args)]
         call.restype, call.argtypes = ci, [P(args), vp, sz, vp]
@@ -435,6 +466,54 @@ def sadmm_gated_bwd_workspace_size(a: GatedBwdArgs) -> int:
 
 def sadmm_gated_bwd(a: GatedBwdArgs, workspace: Optional[int], ws_bytes: int, stream: Optional[int]) -> int:
     return load().sadmm_gated_bwd(ctypes.byref(a), workspace, int(ws_bytes), stream)
+
+
+def sadmm_rmsnorm_fwd(a: RmsNormFwdArgs, stream: Optional[int]) -> int:
+    return load().sadmm_rmsnorm_fwd(ctypes.byref(a), stream)
+
+
+def sadmm_rmsnorm_bwd_workspace_size(a: RmsNormBwdArgs) -> int:
+    return load().sadmm_rmsnorm_bwd_workspace_size(ctypes.byref(a))
+
+
+def sadmm_rmsnorm_bwd(a: RmsNormBwdArgs, workspace: Optional[int], ws_bytes: int, stream: Optional[int]) -> int:
+    return load().sadmm_rmsnorm_bwd(ctypes.byref(a), workspace, ws_bytes, stream)
+
+
+def sadmm_quantize(a: QuantizeArgs, stream: Optional[int]) -> int:
+    return load().sadmm_quantize(ctypes.byref(a), stream)
+
+
+def sadmm_linear8_fwd_workspace_size(a: Linear8FwdArgs) -> int:
+    return load().sadmm_linear8_fwd_workspace_size(ctypes.byref(a))
+
+
+def sadmm_linear8_fwd(a: Linear8FwdArgs, workspace: Optional[int], ws_bytes: int, stream: Optional[int]) -> int:
+    return load().sadmm_linear8_fwd(ctypes.byref(a), workspace, ws_bytes, stream)
+
+
+def sadmm_linear8_bwd_workspace_size(a: Linear8BwdArgs) -> int:
+    return load().sadmm_linear8_bwd_workspace_size(ctypes.byref(a))
+
+
+def sadmm_linear8_bwd(a: Linear8BwdArgs, workspace: Optional[int], ws_bytes: int, stream: Optional[int]) -> int:
+    return load().sadmm_linear8_bwd(ctypes.byref(a), workspace, ws_bytes, stream)
+
+
+def sadmm_gated8_fwd_workspace_size(a: Gated8FwdArgs) -> int:
+    return load().sadmm_gated8_fwd_workspace_size(ctypes.byref(a))
+
+
+def sadmm_gated8_fwd(a: Gated8FwdArgs, workspace: Optional[int], ws_bytes: int, stream: Optional[int]) -> int:
+    return load().sadmm_gated8_fwd(ctypes.byref(a), workspace, ws_bytes, stream)
+
+
+def sadmm_gated8_bwd_workspace_size(a: Gated8BwdArgs) -> int:
+    return load().sadmm_gated8_bwd_workspace_size(ctypes.byref(a))
+
+
+def sadmm_gated8_bwd(a: Gated8BwdArgs, workspace: Optional[int], ws_bytes: int, stream: Optional[int]) -> int:
+    return load().sadmm_gated8_bwd(ctypes.byref(a), workspace, ws_bytes, stream)
 
 
 def sadmm_selftest_wait(limit_us: int, arrive: int, result: Optional[int], stream: Optional[int]) -> int:
@@ -832,6 +911,67 @@ def gated_backward(dh, x, Wg, Wu, g, u, act: int = SADMM_ACT_SILU, want_dx: bool
     the products, whatever their types; dbg and dbu are summed before that."""
     return (_ffn_module or _ffn()).gated_backward(dh, x, Wg, Wu, g, u, act, want_dx, want_dw, want_db, dx_dtype,
                                                   dw_dtype, _handle(stream))
+
+
+# --------------------------------------------------------------------------
+# feed-forward operators with 8-bit operands, on torch tensors
+# --------------------------------------------------------------------------
+#
+# As above, and: an 8-bit matrix is a float8_e4m3fn tensor [rows][cols] and an fp32 tensor of
+# its scales, [rows][ceil(cols / 128)], or for tiles [ceil(rows / 128)][ceil(cols / 128)],
+# of any strides; the two follow each other as arguments and results.  Scales that a call
+# makes have those of a block of columns next to each other.  The transposes that the
+# backward passes read are quantize's (a weight's with tiles, so that both have its scales).
+
+
+def rms_norm(x, gamma=None, residual=None, eps: float = 1e-5, out_dtype=None, stats: bool = False, out=None, sum_out=None,
+             stream=None):
+    """Runs sadmm_rmsnorm_fwd over the last dimension of h = x + residual: y; with out_dtype
+    float8_e4m3fn y in 8 bits, two tensors.  With a residual the sum h (of the residual's
+    type, in sum_out where given: also the residual itself) follows, with `stats` rstd."""
+    return (_ffn_module or _ffn()).rms_norm(x, gamma, residual, eps, out_dtype, stats, out, sum_out, _handle(stream))
+
+
+def rms_norm_backward(dy, h, rstd, gamma=None, dres=None, want_dx: bool = True, want_dgamma: bool = True, stream=None):
+    """Runs sadmm_rmsnorm_bwd: (dx, dgamma), None where not wanted.  h is what the norm read (x
+    without a residual), dx its gradient; dres (of h's type) is added to dx."""
+    return (_ffn_module or _ffn()).rms_norm_backward(dy, h, rstd, gamma, dres, want_dx, want_dgamma, _handle(stream))
+
+
+def quantize(x, tiles: bool = False, transposed: bool = False, want_q: bool = True, stream=None):
+    """Runs sadmm_quantize: x (bf16 or fp32) in 8 bits, (q, scales); with `transposed` the transpose's
+    (qt, scales) follow, [cols][rows] with blocks along x's rows.  `tiles`: blocks of 128 x 128."""
+    return (_ffn_module or _ffn()).quantize(x, tiles, want_q, transposed, _handle(stream))
+
+
+def linear8(x, xs, W, Ws, bias=None, residual=None, act: int = SADMM_ACT_NONE, out_dtype=None, save: bool = False,
+            out=None, stream=None):
+    """Runs sadmm_linear8_fwd: linear() of 8-bit x and W."""
+    return (_ffn_module or _ffn()).linear8(x, xs, W, Ws, bias, residual, act, out_dtype, save, out, _handle(stream))
+
+
+def linear8_backward(dy, xt, xts, Wt, Wts, z=None, act: int = SADMM_ACT_NONE, want_dx: bool = True, want_dw: bool = True,
+                     want_db: bool = True, dx_dtype=None, dw_dtype=None, stream=None):
+    """Runs sadmm_linear8_bwd: (dx, dW, db), None where not wanted.  xt [in][tokens] and Wt
+    [in][out] are the transposes in 8 bits, read for dW and dx (None where that is not
+    wanted).  dx and dW are bf16 unless dx_dtype / dw_dtype say fp32."""
+    return (_ffn_module or _ffn()).linear8_backward(dy, xt, xts, Wt, Wts, z, act, want_dx, want_dw, want_db, dx_dtype,
+                                                    dw_dtype, _handle(stream))
+
+
+def gated8(x, xs, Wg, Wgs, Wu, Wus, bg=None, bu=None, act: int = SADMM_ACT_SILU, out_dtype=None, save: bool = False,
+           stream=None):
+    """Runs sadmm_gated8_fwd: h = act(x Wg^T + bg) * (x Wu^T + bu) of 8-bit operands, in 8 bits (two
+    tensors) or with out_dtype bf16 in that; with `save` g and u (bf16) follow."""
+    return (_ffn_module or _ffn()).gated8(x, xs, Wg, Wgs, Wu, Wus, bg, bu, act, out_dtype, save, _handle(stream))
+
+
+def gated8_backward(dh, xt, xts, Wgt, Wgts, Wut, Wuts, g, u, act: int = SADMM_ACT_SILU, want_dx: bool = True,
+                    want_dw: bool = True, want_db: bool = False, dx_dtype=None, dw_dtype=None, stream=None):
+    """Runs sadmm_gated8_bwd: (dx, dWg, dWu, dbg, dbu), None where not wanted; xt [in][tokens], Wgt
+    and Wut [in][hidden] as in linear8_backward."""
+    return (_ffn_module or _ffn()).gated8_backward(dh, xt, xts, Wgt, Wgts, Wut, Wuts, g, u, act, want_dx, want_dw, want_db,
+                                                   dx_dtype, dw_dtype, _handle(stream))
 
 
 def device_status(stream=None) -> int:
