@@ -133,6 +133,17 @@ bool zero(void* p, long long ld, int dt, long long rows, long long cols, cudaStr
 }
 bool zero(float* p, long long n, cudaStream_t s) { return !p || cudaMemsetAsync(p, 0, (size_t)n * 4, s) == cudaSuccess; }
 
+// Products of one call, by CTA pairs in one launch, or one after the other by single tiles.
+sadmm_status launch_q8_products(const Q8Problem* t, int n, cudaStream_t s)
+{
+    bool pairs = true;
+    for (int i = 0; i < n; ++i) pairs = pairs && t[i].m > 128;
+    if (pairs) return launch_q8_pair(t, n, s);
+    sadmm_status st = SADMM_OK;
+    for (int i = 0; i < n && st == SADMM_OK; ++i) st = launch_q8_product(t[i], s);
+    return st;
+}
+
 // What a call runs, with its places in the workspace.
 struct Forward {
     Q8Problem t;
@@ -190,7 +201,7 @@ sadmm_status run(Forward f, cudaStream_t s)
 {
     if (!f.t.m) return SADMM_OK;
     const sadmm_status st = run_copies(f.c, f.copies, s);
-    return st != SADMM_OK ? st : launch_q8_product(f.t, s);
+    return st != SADMM_OK ? st : launch_q8_products(&f.t, 1, s);
 }
 
 // The gradients: a source made 8-bit by rows (for dx) and by columns (for the
@@ -279,9 +290,11 @@ sadmm_status run(Backward b, cudaStream_t s)
 {
     sadmm_status st = run_copies(b.c, b.copies, s);
     if (st == SADMM_OK) st = launch_q8_source(b.src, b.src_ws, s);
-    if (st == SADMM_OK && b.want_dx) st = launch_q8_product(b.dx, s);
-    for (int i = 0; i < b.dws && st == SADMM_OK; ++i) st = launch_q8_product(b.dw[i], s);
-    return st;
+    Q8Problem t[3];
+    int n = 0;
+    if (b.want_dx) t[n++] = b.dx;
+    for (int i = 0; i < b.dws; ++i) t[n++] = b.dw[i];
+    return st == SADMM_OK && n ? launch_q8_products(t, n, s) : st;
 }
 
 }  // namespace

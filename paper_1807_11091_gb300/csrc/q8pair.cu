@@ -1,0 +1,657 @@
+// q8pair.cu -- products of large 8-bit matrices: a persistent kernel of CTA pairs,
+// one tile of 256 rows by 256 columns at a time (gated: 128 of either weight's).
+//
+// The pair shares each MMA (tcgen05.mma.cta_group::2, M 256): a CTA holds 128 of
+// the tile's rows and half of its columns' operand (gated: the second CTA Wu's
+// columns where the first has Wg's).  A block of 128 of the contraction is one stage
+// of shared memory and one accumulator in TMEM, of which there are two; the
+// epilogue's warps multiply it by its scales and add it to fp32 sums in registers
+// while the next block's products run.  Per CTA, twelve warps:
+//   warp 0      TMA producer
+//   warp 1      TMEM allocator; in the pair's first CTA, issuer of the MMAs
+//   warps 2, 3  the rows' and the columns' scales, by cp.async into a ring of blocks (in
+//               the sums' warps the addresses alone took 720 cycles a block, of 512)
+//   warps 4-11  sums and output: TMEM lane = tile row, each half of the warps
+//               takes half of the columns, 128 sums a thread
+#include <string.h>
+
+#include "q8.cuh"
+#include "tgemm_dev.cuh"
+
+namespace sadmm {
+namespace {
+
+constexpr int kThreads = 384;
+// Registers of a thread: 168 at launch (384 of them fill an SM), then these.
+constexpr int kFewRegs = 88, kManyRegs = 208;
+static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "more registers than the block was launched with");
+constexpr int kStages = 6;
+constexpr uint32_t kHalfBytes = 128 * kQBlock;        // 128 rows of one block
+constexpr uint32_t kStageBytes = 2 * kHalfBytes;
+constexpr int kProducts = 3;
+constexpr int kSlots = 3;                             // places of the ring of scales, four blocks each:
+constexpr int kColumns = 4 * 128;                     // [row][block], then [block][column], or where all columns of a
+constexpr int kSlotFloats = kColumns + 4 * 256;       // half (of a weight) have one scale [half][block]
+
+struct Scales {
+    const float* s;
+    long long s_row, s_block, rows;
+    int shift;
+};
+
+struct Product {
+    TgProduct t;           // y, m, n, first, p_tiles, q_tiles, nk0, nk are used
+    Scales ps[2], qs[2];   // of both summands; gated: qs of Wg and Wu
+    int sum;
+    int vec;               // the columns' scales are single rows'
+    int pm, qm;            // maps; the second summand's (gated: Wu's) follow
+};
+
+struct Maps {
+    CUtensorMap map[8];
+};
+
+struct Args {
+    Product prod[kProducts];
+    TgArgs t;              // products, tiles, res, z, u, bias, bias2, act, status are used
+    sadmm_q8_out y8;
+    uint32_t idesc;
+};
+
+// ------------------------------------------------------------- device PTX --
+
+SADMM_DEV void tmem_alloc2(uint32_t* dst, uint32_t ncols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(ncols)
+                 : "memory");
+}
+SADMM_DEV void tmem_relinquish2() { asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory"); }
+SADMM_DEV void tmem_dealloc2(uint32_t taddr, uint32_t ncols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+SADMM_DEV void tma_load_pair(void* dst, const void* tmap, uint32_t bar, int c0, int c1)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+        " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+        "l"(tmap), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+}
+SADMM_DEV void mma_f8_pair_elect(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b32 l;\n\telect.sync l|e, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate));
+}
+SADMM_DEV void commit_pair_elect(uint64_t* bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t.reg .b32 l;\n\t.reg .b16 m;\n\telect.sync l|e, 0xffffffff;\n\tmov.b16 m, 3;\n\t"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}" ::"r"(
+            smem_u32(bar))
+        : "memory");
+}
+SADMM_DEV void commit_own_elect(uint64_t* bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t.reg .b32 l;\n\telect.sync l|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+        : "memory");
+}
+// Arrival on a barrier of either CTA.  Its order is that of the CTA: what it hands over
+// is TMEM that has been read, and a release to the cluster waits for every copy in
+// flight (2500 cycles a block of the contraction, where its products take 512).
+SADMM_DEV void mbar_arrive_either(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Four bytes into shared memory, zero where `in` is false.
+SADMM_DEV void cp_async4(float* dst, const float* src, bool in)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+// Arrives on the barrier once this thread's copies so far have landed.
+SADMM_DEV void cp_async_arrive(uint64_t* bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+SADMM_DEV void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// ------------------------------------------------------------------ kernel --
+
+// Product, row tile and column tile of tile t, eight row tiles at a time so
+// that the tiles in flight share their operands in L2.
+struct Place {
+    int prod, mt, nt;
+};
+SADMM_DEV Place place(const Args& a, int t)
+{
+    constexpr int kGroup = 8;
+    Place p;
+    p.prod = 0;
+    while (p.prod + 1 < a.t.products && t >= a.prod[p.prod + 1].t.first) ++p.prod;
+    const TgProduct& d = a.prod[p.prod].t;
+    t -= d.first;
+    const int g = t / (kGroup * d.q_tiles);
+    const int rows = min(kGroup, d.p_tiles - g * kGroup);
+    t -= g * kGroup * d.q_tiles;
+    p.nt = t / rows;
+    p.mt = g * kGroup + t - p.nt * rows;
+    return p;
+}
+
+// The k-th tile of pair `me` of n: in turn, every other round backwards, so that the
+// pairs with the longer tiles of one round have the shorter ones of the next.
+SADMM_DEV int tile_of(const Args& a, int me, int n, int k)
+{
+    const int t = k * n + ((k & 1) ? n - 1 - me : me);
+    return t < a.t.tiles ? t : -1;
+}
+
+// The ring of scales, as the warps that fill it see it.
+struct Ring {
+    float* slots;
+    uint64_t *full, *empty;
+    volatile int* abort_flag;
+    int* status;
+    int s;
+    uint32_t phase;
+    // N scales a lane of each of the blocks k0 .. k1-1 of a tile's nk; which(j, scales, row) says whose.  They lie `apart`
+    // places apart from `at` on, `next` places further for the next of a place's four blocks.
+    template <int N, typename F>
+    SADMM_DEV bool fill(int k0, int k1, int nk, int at, int apart, int next, F which)
+    {
+        const float* from[N];
+        long long step[(N + 3) / 4];
+        uint32_t in = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const Scales* c;
+            long long r;
+            which(j, c, r);
+            const bool there = r < c->rows;
+            in |= (there ? 1u : 0u) << j;
+            from[j] = c->s + ((there ? r : 0) >> c->shift) * c->s_row;
+            if (j % 4 == 0) step[j / 4] = c->s_block;
+        }
+        for (int k = k0; k < k1; ++k) {
+            if ((k & 3) == 0 && !mbar_wait_warp(&empty[s], phase ^ 1u, abort_flag, status)) return false;
+            float* slot = slots + s * kSlotFloats + at + (k & 3) * next;
+            if (N > 1 || (threadIdx.x & 31) < 2) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    cp_async4(slot + j * apart, from[j], in >> j & 1u);
+                    from[j] += step[j / 4];
+                }
+            }
+            if ((k & 3) == 3 || k + 1 == nk) {
+                cp_async_arrive(&full[s]);
+                if (++s == kSlots) { s = 0; phase ^= 1u; }
+            }
+        }
+        return true;
+    }
+};
+
+// v += bias of columns c .. c+15, the same for the whole warp.
+SADMM_DEV void add_bias16(const float* bias, long long c, long long n, float (&v)[16])
+{
+    if (!bias) return;
+    if (c + 16 <= n && (reinterpret_cast<uintptr_t>(bias) & 15) == 0) {
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+            const float4 b = __ldg(reinterpret_cast<const float4*>(bias + c + j));
+            v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < n) v[j] += __ldg(bias + c + j);
+    }
+}
+
+template <bool GATED>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_q8_pair(const __grid_constant__ Maps maps, const __grid_constant__ Args a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    float* rings = reinterpret_cast<float*>(smem + kStages * kStageBytes);  // [kSlots][kSlotFloats]
+    __shared__ uint64_t full[kStages], empty[kStages], s_full[kSlots], s_empty[kSlots], acc_full[2], acc_empty[2], drain, met[4];
+    __shared__ uint32_t tmem_holder;
+    __shared__ volatile int abort_flag;
+    __shared__ float tops[2][128];
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int me = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    int* const status = a.t.status;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&acc_full[b], 1);
+            mbar_init(&acc_empty[b], 16);  // eight warps of either CTA
+        }
+        for (int q = 0; q < 4; ++q) mbar_init(&met[q], 2);
+        for (int s = 0; s < kSlots; ++s) {
+            mbar_init(&s_full[s], 64);
+            mbar_init(&s_empty[s], 8);
+        }
+        mbar_init(&drain, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc2(&tmem_holder, 512);
+        tmem_relinquish2();
+    }
+    pdl_wait();  // nothing above reads global memory
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // barriers and TMEM of both CTAs are there
+    tc_fence_after();
+    const uint32_t tmem = tmem_holder;
+
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int i = 0, t; ok && (t = tile_of(a, me, pairs, i)) >= 0; ++i) {
+                const Place pl = place(a, t);
+                const Product& p = a.prod[pl.prod];
+                const int row0 = pl.mt * 256 + (int)rank * 128;
+                const int col0 = GATED ? pl.nt * 128 : pl.nt * 256 + (int)rank * 128;
+                for (int k = 0; k < p.t.nk; ++k) {
+                    if (!mbar_wait(&empty[s], phase ^ 1u, &abort_flag, status)) { ok = false; break; }
+                    if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * kStageBytes);
+                    const uint32_t bar = map_rank(smem_u32(&full[s]), 0);
+                    const int second = k >= p.t.nk0;  // of a sum
+                    const int kc = (second ? k - p.t.nk0 : k) * kQBlock;
+                    uint8_t* sp = smem + (size_t)s * kStageBytes;
+                    tma_load_pair(sp, &maps.map[p.pm + second], bar, kc, row0);
+                    tma_load_pair(sp + kHalfBytes, &maps.map[p.qm + (GATED ? (int)rank : second)], bar, kc, col0);
+                    if (++s == kStages) { s = 0; phase ^= 1u; }
+                }
+            }
+            // every stage filled has been read before the CTA retires; after a failure, time for the copies to land
+            for (int i = 0; i < kStages && ok; ++i) {
+                ok = mbar_wait(&empty[s], phase ^ 1u, &abort_flag, status);
+                if (++s == kStages) { s = 0; phase ^= 1u; }
+            }
+            if (!ok) {
+                const unsigned long long t0 = globaltimer();
+                while (globaltimer() - t0 < 10000000ull) {}
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            int s = 0, buf = 0;
+            uint32_t phase = 0, bphase = 0;
+            bool ok = true;
+            for (int i = 0, t; ok && (t = tile_of(a, me, pairs, i)) >= 0; ++i) {
+                const int nk = a.prod[place(a, t).prod].t.nk;
+                for (int k = 0; k < nk; ++k) {
+                    if (!mbar_wait_warp(&acc_empty[buf], bphase ^ 1u, &abort_flag, status) ||
+                        !mbar_wait_warp(&full[s], phase, &abort_flag, status)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t st = smem_u32(smem + (size_t)s * kStageBytes);
+                    const uint64_t pd = sdesc_kmajor_sw128(st), qd = sdesc_kmajor_sw128(st + kHalfBytes);
+                    const uint32_t d = tmem + (uint32_t)buf * 256u;
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) mma_f8_pair_elect(d, pd + kk * 2, qd + kk * 2, a.idesc, kk != 0);
+                    commit_pair_elect(&empty[s]);
+                    commit_pair_elect(&acc_full[buf]);
+                    if (++s == kStages) { s = 0; phase ^= 1u; }
+                    if (++buf == 2) { buf = 0; bphase ^= 1u; }
+                }
+            }
+            commit_own_elect(&drain);
+            if (lane == 0) {
+                const unsigned long long t0 = globaltimer();
+                while (!mbar_try_wait(&drain, 0) && globaltimer() - t0 < kWaitLimitNs) {}
+            }
+        }
+        __syncwarp();
+    } else {
+        // warp 2: rows, warp 3: columns; blocks go into the ring in turn
+        Ring ring = {rings, s_full, s_empty, &abort_flag, status, 0, 0};
+        bool ok = true;
+        for (int i = 0, t; ok && (t = tile_of(a, me, pairs, i)) >= 0; ++i) {
+            const Place pl = place(a, t);
+            const Product& p = a.prod[pl.prod];
+            for (int second = 0; ok && second <= p.sum; ++second) {
+                const int k0 = second ? p.t.nk0 : 0, k1 = second || !p.sum ? p.t.nk : p.t.nk0;
+                if (warp == 2) {
+                    const long long r0 = (long long)pl.mt * 256 + rank * 128 + lane;
+                    ok = ring.fill<4>(k0, k1, p.t.nk, lane * 4, 128, 1, [&](int j, const Scales*& c, long long& r) {
+                        c = &p.ps[second];
+                        r = r0 + j * 32;
+                    });
+                } else if (p.vec) {  // gated: 128 columns of g, then of u
+                    const long long r0 = (long long)pl.nt * (GATED ? 128 : 256) + lane;
+                    ok = ring.fill<8>(k0, k1, p.t.nk, kColumns + lane, 32, 256, [&](int j, const Scales*& c, long long& r) {
+                        c = &p.qs[GATED ? j >> 2 : second];
+                        r = r0 + (GATED ? j & 3 : j) * 32;
+                    });
+                } else {  // lane 0: the first 128 columns' (g's), lane 1: the others' (u's)
+                    ok = ring.fill<1>(k0, k1, p.t.nk, kColumns + lane * 4, 0, 1, [&](int, const Scales*& c, long long& r) {
+                        c = &p.qs[GATED ? lane & 1 : second];
+                        r = (long long)pl.nt * (GATED ? 128 : 256) + (GATED ? 0 : (lane & 1) * 128);
+                    });
+                }
+            }
+        }
+        cp_async_wait_all();
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
+        const int q = warp & 3, part = (warp - 4) >> 2;
+        const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
+        const uint32_t freed = map_rank(smem_u32(&acc_empty[0]), 0);
+        int buf = 0;
+        uint32_t bphase = 0, mphase = 0;
+        bool ok = true;
+        int t = tile_of(a, me, pairs, 0);
+        Place pl = place(a, t < 0 ? 0 : t);
+        int slot_at = 0;
+        uint32_t sphase = 0;
+        for (int i = 0; t >= 0; ++i) {
+            const Product& p = a.prod[pl.prod];
+            const int nk = p.t.nk, vec = p.vec;
+            float acc[128];
+#pragma unroll
+            for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+            // the accumulator's columns of the thread's c-th 16
+            auto column = [&](int c) { return GATED ? (c >> 2) * 128 + part * 64 + (c & 3) * 16 : part * 128 + c * 16; };
+            float4 rows = {}, cols = {}, cols2 = {};  // the scales of the next four blocks
+            for (int k = 0; k < nk; ++k) {
+                const float* slot = rings + slot_at * kSlotFloats;
+                if ((k & 3) == 0) {
+                    ok = mbar_wait_warp(&s_full[slot_at], sphase, &abort_flag, status);
+                    if (!ok) break;
+                    rows = *reinterpret_cast<const float4*>(slot + (q * 32 + lane) * 4);
+                    cols = *reinterpret_cast<const float4*>(slot + kColumns + (GATED ? 0 : part * 4));
+                    if (GATED) cols2 = *reinterpret_cast<const float4*>(slot + kColumns + 4);
+                }
+                const float sp = rows.x, f0 = sp * cols.x, f1 = GATED ? sp * cols2.x : f0;
+                rows = make_float4(rows.y, rows.z, rows.w, 0.0f);
+                cols = make_float4(cols.y, cols.z, cols.w, 0.0f);
+                cols2 = make_float4(cols2.y, cols2.z, cols2.w, 0.0f);
+                ok = mbar_wait_warp(&acc_full[buf], bphase, &abort_flag, status);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t from = taddr + (uint32_t)buf * 256u;
+                auto freed_now = [&]() {  // the accumulator has been read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_either(freed + (uint32_t)buf * 8u);
+                };
+                if (vec) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t r[16];
+                        tmem_ld_32x32b_x16(from + column(c), r);
+                        float f[16];
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 v = *reinterpret_cast<const float4*>(slot + kColumns + (k & 3) * 256 + column(c) + j);
+                            f[j] = sp * v.x, f[j + 1] = sp * v.y, f[j + 2] = sp * v.z, f[j + 3] = sp * v.w;
+                        }
+                        tmem_ld_wait();
+                        if (c == 7) freed_now();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fmaf(__uint_as_float(r[j]), f[j], acc[c * 16 + j]);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t r[16];
+                        tmem_ld_32x32b_x16(from + column(c), r);
+                        tmem_ld_wait();
+                        if (c == 7) freed_now();
+                        const float f = c < 4 ? f0 : f1;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fmaf(__uint_as_float(r[j]), f, acc[c * 16 + j]);
+                    }
+                }
+                if ((k & 3) == 3 || k + 1 == nk) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_empty[slot_at]);
+                    if (++slot_at == kSlots) { slot_at = 0; sphase ^= 1u; }
+                }
+                if (++buf == 2) { buf = 0; bphase ^= 1u; }
+            }
+            if (!ok) break;
+            const Place done = pl;
+            t = tile_of(a, me, pairs, i + 1);
+            if (t >= 0) pl = place(a, t);
+            const long long row = (long long)done.mt * 256 + rank * 128 + q * 32 + lane;
+            const long long col0 = GATED ? (long long)done.nt * 128 + part * 64 : (long long)done.nt * 256 + part * 128;
+            const bool in = row < p.t.m;
+            float top = 0.0f;
+            // 16 (32) columns at a time in one loop, the sums moving up: unrolled, its instructions came
+            // from memory every time (11 us a tile with GELU).  A gated pair's outputs take g's place until their scale is
+            // known.
+            constexpr int D = GATED ? 1 : 2;
+            with_act(a.t.act, [&](auto tag) {
+#pragma unroll 1
+                for (int c = 0; c < (GATED ? 4 : 8); c += D) {
+#pragma unroll
+                    for (int d = 0; d < D; ++d) {
+                        const long long col = col0 + (c + d) * 16;
+                        float v[16], w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] = acc[d * 16 + j], w[j] = GATED ? acc[64 + j] : 0.0f;
+                        add_bias16(a.t.bias, col, p.t.n, v);
+                        if (GATED) add_bias16(a.t.bias2, col, p.t.n, w);
+                        if (in && col < p.t.n) {
+                            if (GATED && a.t.u.p) store16(a.t.u, row, col, p.t.n, w, status);
+                            if (a.t.z.p) store16(a.t.z, row, col, p.t.n, v, status);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            v[j] = act_f32<decltype(tag)::value>(v[j]);
+                            if (GATED) v[j] *= w[j];
+                        }
+                        if (GATED && a.y8.q) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                if (col + j < p.t.n) top = fmaxf(top, q8_size(v[j]));
+                                acc[j] = v[j];
+                            }
+                        } else if (in && col < p.t.n) {
+                            if (a.t.res.p) add16(a.t.res, row, col, p.t.n, v, status);
+                            store16(p.t.y, row, col, p.t.n, v, status);
+                        }
+                    }
+                    if (GATED) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float done_ = acc[j];
+                            acc[j] = acc[j + 16], acc[j + 16] = acc[j + 32], acc[j + 32] = acc[j + 48], acc[j + 48] = done_;
+                            acc[j + 64] = acc[j + 80], acc[j + 80] = acc[j + 96], acc[j + 96] = acc[j + 112];
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 96; ++j) acc[j] = acc[j + 32];
+                    }
+                }
+            });
+            if (GATED && a.y8.q) {
+                // the other half's largest of the row's 128 units, from the warp that has them
+                tops[part][q * 32 + lane] = top;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&met[q]);
+                ok = mbar_wait_warp(&met[q], mphase, &abort_flag, status);
+                mphase ^= 1u;
+                if (!ok) break;
+                const Q8Scale k = q8_scale(fmaxf(top, tops[part ^ 1][q * 32 + lane]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&met[q]);  // read: the next tile's may be written
+                ok = mbar_wait_warp(&met[q], mphase, &abort_flag, status);
+                mphase ^= 1u;
+                if (!ok) break;
+                if (in && dbg_in(row, p.t.m, status)) {
+                    if (part == 0) a.y8.s[row * a.y8.s_row + (long long)done.nt * a.y8.s_block] = k.s;
+                    uint8_t* out = static_cast<uint8_t*>(a.y8.q) + row * a.y8.ld + col0;
+                    const int live = (int)max(0ll, min(64ll, p.t.n - col0));
+                    const bool wide = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float* v = acc + c * 16 + j * 4;
+                            w[j] = q8_four(q8_quotient(v[0], k), q8_quotient(v[1], k), q8_quotient(v[2], k),
+                                           q8_quotient(v[3], k));
+                        }
+                        if (wide && live >= c * 16 + 16) {
+                            reinterpret_cast<uint4*>(out)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                        } else {
+                            store_bytes8(out + c * 16, live - c * 16, w[0], w[1]);
+                            store_bytes8(out + c * 16 + 8, live - c * 16 - 8, w[2], w[3]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // neither CTA's barriers nor TMEM are in use any more
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc2(tmem, 512);
+    }
+}
+
+// -------------------------------------------------------------------- host --
+
+bool encode8(CUtensorMap* map, const Q8Operand& o)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode_fn();
+    if (!enc) return false;
+    memset(map, 0, sizeof(*map));
+    const cuuint64_t gdim[2] = {(cuuint64_t)o.k, (cuuint64_t)o.rows};
+    const cuuint64_t gstride[1] = {(cuuint64_t)o.ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kQBlock, 128u};
+    const cuuint32_t estride[2] = {1u, 1u};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(o.p), gdim, gstride, box, estride,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+Scales scales_of(const Q8Operand& o) { return {o.s, o.s_row, o.s_block, o.rows, o.shift}; }
+
+template <bool GATED>
+sadmm_status run(const Maps& maps, const Args& a, int ctas, cudaStream_t s)
+{
+    static bool configured[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
+    constexpr int smem = kStages * (int)kStageBytes + kSlots * kSlotFloats * 4 + 1024;
+    auto kern = k_q8_pair<GATED>;
+    if (!configured[dev]) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+            return SADMM_ECUDA;
+        configured[dev] = true;
+    }
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, maps, a) == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+}
+
+long long blocks_of(const Q8Problem& t)
+{
+    return (t.a[0].k + kQBlock - 1) / kQBlock + (t.mode == kTgSum ? (t.a[1].k + kQBlock - 1) / kQBlock : 0);
+}
+
+}  // namespace
+
+sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s)
+{
+    // the longest contractions first
+    const Q8Problem* t[kProducts];
+    for (int i = 0; i < count; ++i) {
+        int j = i;
+        for (; j > 0 && blocks_of(*t[j - 1]) < blocks_of(problems[i]); --j) t[j] = t[j - 1];
+        t[j] = &problems[i];
+    }
+    Args a;
+    Maps maps;
+    memset(&a, 0, sizeof(a));
+    const bool gated = t[0]->mode == kTgGated;
+    long long tiles = 0;
+    int next = 0;
+    for (int i = 0; i < count; ++i) {
+        Product& p = a.prod[i];
+        const Q8Problem& q = *t[i];
+        const int cols = gated ? 128 : 256;
+        p.t.m = q.m;
+        p.t.n = q.n;
+        if (q.y.p) p.t.y = make_out(q.y, q.m, q.n);
+        p.t.p_tiles = (int)((q.m + 255) / 256);
+        p.t.q_tiles = (int)((q.n + cols - 1) / cols);
+        p.t.first = (int)tiles;
+        tiles += (long long)p.t.p_tiles * p.t.q_tiles;
+        if (tiles > 0x0fffffffll) return SADMM_EUNSUPPORTED;
+        p.sum = q.mode == kTgSum;
+        p.t.nk0 = (int)((q.a[0].k + kQBlock - 1) / kQBlock);
+        p.t.nk = (int)blocks_of(q);
+        const int na = p.sum ? 2 : 1, nb = p.sum || gated ? 2 : 1;
+        p.pm = next;
+        for (int j = 0; j < na; ++j)
+            if (next >= 8 || !encode8(&maps.map[next++], q.a[j])) return SADMM_ECUDA;
+        p.qm = next;
+        for (int j = 0; j < nb; ++j)
+            if (next >= 8 || !encode8(&maps.map[next++], q.b[j])) return SADMM_ECUDA;
+        for (int j = 0; j < 2; ++j) {
+            p.ps[j] = scales_of(q.a[na == 2 ? j : 0]);
+            p.qs[j] = scales_of(q.b[nb == 2 ? j : 0]);
+            if (p.qs[j].shift == 0) p.vec = 1;
+        }
+    }
+    a.t.products = count;
+    a.t.tiles = (int)tiles;
+    const Q8Problem& f = *t[0];
+    a.t.bias = f.bias;
+    a.t.bias2 = f.bias2;
+    a.t.act = act_for(f.act, f.y.p && f.y.dt == SADMM_BF16);
+    if (f.residual.p) a.t.res = make_out(f.residual, f.m, f.n);
+    if (f.z.p) a.t.z = make_out(f.z, f.m, f.n);
+    if (f.u.p) a.t.u = make_out(f.u, f.m, f.n);
+    a.t.status = device_status_ptr();
+    a.y8 = f.y8;
+    a.idesc = (1u << 4) | (256u >> 3) << 17 | (256u >> 4) << 24;  // e4m3 operands, fp32 sums, 256 x 256
+    const long long pairs = device_sm_count() / 2;
+    const int ctas = 2 * (int)(tiles < pairs ? tiles : pairs);
+    return gated ? run<true>(maps, a, ctas, s) : run<false>(maps, a, ctas, s);
+}
+
+}  // namespace sadmm
