@@ -133,14 +133,27 @@ bool zero(void* p, long long ld, int dt, long long rows, long long cols, cudaStr
 }
 bool zero(float* p, long long n, cudaStream_t s) { return !p || cudaMemsetAsync(p, 0, (size_t)n * 4, s) == cudaSuccess; }
 
-// Products of one call, by CTA pairs in one launch, or one after the other by single tiles.
+// Whether the columns' operand (of a summand) has scales of single rows.
+bool row_scales(const Q8Problem& t) { return t.b[0].shift == 0 || (t.mode != kTgSingle && t.b[1].shift == 0); }
+
+// Whether CTA pairs take a product.
+bool by_pairs(const Q8Problem& t) { return t.m > 128; }
+
+// Products of one call: by CTA pairs, neighbours of one kind in one launch, or by
+// single tiles.
 sadmm_status launch_q8_products(const Q8Problem* t, int n, cudaStream_t s)
 {
-    bool pairs = true;
-    for (int i = 0; i < n; ++i) pairs = pairs && t[i].m > 128;
-    if (pairs) return launch_q8_pair(t, n, s);
     sadmm_status st = SADMM_OK;
-    for (int i = 0; i < n && st == SADMM_OK; ++i) st = launch_q8_product(t[i], s);
+    for (int i = 0; i < n && st == SADMM_OK;) {
+        int m = i;
+        while (m < n && by_pairs(t[m]) && row_scales(t[m]) == row_scales(t[i])) ++m;
+        if (m > i) {
+            st = launch_q8_pair(t + i, m - i, s);
+            i = m;
+        } else {
+            st = launch_q8_product(t[i++], s);
+        }
+    }
     return st;
 }
 

@@ -23,8 +23,11 @@ namespace {
 
 constexpr int kThreads = 384;
 // Registers of a thread: 168 at launch (384 of them fill an SM), then these.
-constexpr int kFewRegs = 88, kManyRegs = 208;
-static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "more registers than the block was launched with");
+template <bool VEC>
+struct Regs {
+    static constexpr int few = VEC ? 56 : 40, many = VEC ? 224 : 232;
+    static_assert(128 * few + 256 * many <= 384 * 168, "more registers than the block was launched with");
+};
 constexpr int kStages = 6;
 constexpr uint32_t kHalfBytes = 128 * kQBlock;        // 128 rows of one block
 constexpr uint32_t kStageBytes = 2 * kHalfBytes;
@@ -43,7 +46,6 @@ struct Product {
     TgProduct t;           // y, m, n, first, p_tiles, q_tiles, nk0, nk are used
     Scales ps[2], qs[2];   // of both summands; gated: qs of Wg and Wu
     int sum;
-    int vec;               // the columns' scales are single rows'
     int pm, qm;            // maps; the second summand's (gated: Wu's) follow
 };
 
@@ -114,6 +116,11 @@ SADMM_DEV void cp_async4(float* dst, const float* src, bool in)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
 }
+// 16 bytes, of which `bytes` are there and the others zero.
+SADMM_DEV void cp_async16(float* dst, const float* src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
+}
 // Arrives on the barrier once this thread's copies so far have landed.
 SADMM_DEV void cp_async_arrive(uint64_t* bar)
 {
@@ -160,33 +167,76 @@ struct Ring {
     int* status;
     int s;
     uint32_t phase;
-    // N scales a lane of each of the blocks k0 .. k1-1 of a tile's nk; which(j, scales, row) says whose.  They lie `apart`
-    // places apart from `at` on, `next` places further for the next of a place's four blocks.
-    template <int N, typename F>
-    SADMM_DEV bool fill(int k0, int k1, int nk, int at, int apart, int next, F which)
+    SADMM_DEV bool wait(int k) { return (k & 3) != 0 || mbar_wait_warp(&empty[s], phase ^ 1u, abort_flag, status); }
+    SADMM_DEV float* slot(int k, int next) { return slots + s * kSlotFloats + (k & 3) * next; }
+    SADMM_DEV void done(int k, int nk)
     {
-        const float* from[N];
-        long long step[(N + 3) / 4];
+        if ((k & 3) != 3 && k + 1 != nk) return;
+        cp_async_arrive(&full[s]);
+        if (++s == kSlots) { s = 0; phase ^= 1u; }
+    }
+    // N scales a lane of each of the blocks k0 .. k1-1 of a tile's nk: those of the rows r0, r0 + 32, ... of c (r0 a
+    // multiple of 32 and the lane).  They lie `apart` places apart from `at` on, `next` places further for the next of a
+    // place's four blocks.
+    template <int N>
+    SADMM_DEV bool fill(int k0, int k1, int nk, int at, int apart, int next, const Scales& c, long long r0)
+    {
         uint32_t in = 0;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const Scales* c;
-            long long r;
-            which(j, c, r);
-            const bool there = r < c->rows;
-            in |= (there ? 1u : 0u) << j;
-            from[j] = c->s + ((there ? r : 0) >> c->shift) * c->s_row;
-            if (j % 4 == 0) step[j / 4] = c->s_block;
-        }
+        for (int j = 0; j < N; ++j) in |= (r0 + j * 32 < c.rows ? 1u : 0u) << j;
+        const float* from = c.s + ((in & 1u ? r0 : 0) >> c.shift) * c.s_row;
+        const long long more = c.s_row * (c.shift ? 1 : 32);  // a scale further
+        const long long step = c.s_block;
+        const int same = c.shift ? 2 : 0;                     // 1 << same places of 32 rows share one
         for (int k = k0; k < k1; ++k) {
-            if ((k & 3) == 0 && !mbar_wait_warp(&empty[s], phase ^ 1u, abort_flag, status)) return false;
-            float* slot = slots + s * kSlotFloats + at + (k & 3) * next;
+            if (!wait(k)) return false;
+            float* to = slot(k, next) + at;
             if (N > 1 || (threadIdx.x & 31) < 2) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    cp_async4(slot + j * apart, from[j], in >> j & 1u);
-                    from[j] += step[j / 4];
-                }
+                for (int j = 0; j < N; ++j)
+                    cp_async4(to + j * apart, in >> j & 1u ? from + (j >> same) * more : from, in >> j & 1u);
+            }
+            from += step;
+            done(k, nk);
+        }
+        return true;
+    }
+    // The same for 256 neighbouring scales from row r0 on, which start on 16-byte boundaries: four a lane, twice.
+    SADMM_DEV bool fill_wide(int k0, int k1, int nk, const Scales& c, long long r0)
+    {
+        const int lane = threadIdx.x & 31;
+        const long long left = c.rows - r0 - lane * 4;
+        const int b0 = (int)max(0ll, min(4ll, left)) * 4, b1 = (int)max(0ll, min(4ll, left - 128)) * 4;
+        const float* from = c.s + (b0 ? r0 + lane * 4 : 0);
+        for (int k = k0; k < k1; ++k) {
+            if (!wait(k)) return false;
+            float* to = slot(k, 256) + kColumns + lane * 4;
+            cp_async16(to, from, b0);
+            cp_async16(to + 128, b1 ? from + 128 : from, b1);
+            from += c.s_block;
+            done(k, nk);
+        }
+        return true;
+    }
+    // The 128 columns of either weight of a gated pair, from r0 on.
+    SADMM_DEV bool fill2(int k0, int k1, int nk, int at, const Scales (&c)[2], long long r0)
+    {
+        const float* from[2];
+        uint32_t in = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) in |= (r0 + j * 32 < c[0].rows ? 1u : 0u) << j;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) from[h] = c[h].s + ((in & 1u ? r0 : 0) >> c[h].shift) * c[h].s_row;
+        for (int k = k0; k < k1; ++k) {
+            if ((k & 3) == 0 && !mbar_wait_warp(&empty[s], phase ^ 1u, abort_flag, status)) return false;
+            float* slot = slots + s * kSlotFloats + at + (k & 3) * 256;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const long long more = c[h].shift ? 0 : c[h].s_row * 32;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    cp_async4(slot + h * 128 + j * 32, from[h] + (in >> j & 1u ? j * more : 0), in >> j & 1u);
+                from[h] += c[h].s_block;
             }
             if ((k & 3) == 3 || k + 1 == nk) {
                 cp_async_arrive(&full[s]);
@@ -214,7 +264,7 @@ SADMM_DEV void add_bias16(const float* bias, long long c, long long n, float (&v
     }
 }
 
-template <bool GATED>
+template <bool GATED, bool VEC>
 __global__ void __launch_bounds__(kThreads, 1)
     k_q8_pair(const __grid_constant__ Maps maps, const __grid_constant__ Args a)
 {
@@ -260,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = tmem_holder;
 
     if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Regs<VEC>::few));
     if (warp == 0) {
         if (lane == 0) {
             int s = 0;
@@ -335,30 +385,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Product& p = a.prod[pl.prod];
             for (int second = 0; ok && second <= p.sum; ++second) {
                 const int k0 = second ? p.t.nk0 : 0, k1 = second || !p.sum ? p.t.nk : p.t.nk0;
+                const int nt = pl.nt, mt = pl.mt;
                 if (warp == 2) {
-                    const long long r0 = (long long)pl.mt * 256 + rank * 128 + lane;
-                    ok = ring.fill<4>(k0, k1, p.t.nk, lane * 4, 128, 1, [&](int j, const Scales*& c, long long& r) {
-                        c = &p.ps[second];
-                        r = r0 + j * 32;
-                    });
-                } else if (p.vec) {  // gated: 128 columns of g, then of u
-                    const long long r0 = (long long)pl.nt * (GATED ? 128 : 256) + lane;
-                    ok = ring.fill<8>(k0, k1, p.t.nk, kColumns + lane, 32, 256, [&](int j, const Scales*& c, long long& r) {
-                        c = &p.qs[GATED ? j >> 2 : second];
-                        r = r0 + (GATED ? j & 3 : j) * 32;
-                    });
+                    ok = ring.fill<4>(k0, k1, p.t.nk, lane * 4, 128, 1, p.ps[second], (long long)mt * 256 + rank * 128 + lane);
+                } else if (VEC && !GATED && p.qs[second].shift == 0 && p.qs[second].s_row == 1 && (p.qs[second].s_block & 3) == 0 &&
+                           (reinterpret_cast<uintptr_t>(p.qs[second].s) & 15) == 0) {
+                    ok = ring.fill_wide(k0, k1, p.t.nk, p.qs[second], (long long)nt * 256);
+                } else if (VEC && !GATED) {
+                    ok = ring.fill<8>(k0, k1, p.t.nk, kColumns + lane, 32, 256, p.qs[second], (long long)nt * 256 + lane);
+                } else if (VEC) {
+                    ok = ring.fill2(k0, k1, p.t.nk, kColumns + lane, p.qs, (long long)nt * 128 + lane);
                 } else {  // lane 0: the first 128 columns' (g's), lane 1: the others' (u's)
-                    ok = ring.fill<1>(k0, k1, p.t.nk, kColumns + lane * 4, 0, 1, [&](int, const Scales*& c, long long& r) {
-                        c = &p.qs[GATED ? lane & 1 : second];
-                        r = (long long)pl.nt * (GATED ? 128 : 256) + (GATED ? 0 : (lane & 1) * 128);
-                    });
+                    ok = ring.fill<1>(k0, k1, p.t.nk, kColumns + lane * 4, 0, 1, p.qs[GATED ? lane & 1 : second],
+                                      (long long)nt * (GATED ? 128 : 256) + (GATED ? 0 : (lane & 1) * 128));
                 }
             }
         }
         cp_async_wait_all();
     }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Regs<VEC>::many));
         const int q = warp & 3, part = (warp - 4) >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
         const uint32_t freed = map_rank(smem_u32(&acc_empty[0]), 0);
@@ -371,12 +417,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t sphase = 0;
         for (int i = 0; t >= 0; ++i) {
             const Product& p = a.prod[pl.prod];
-            const int nk = p.t.nk, vec = p.vec;
+            const int nk = p.t.nk;
             float acc[128];
 #pragma unroll
             for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
-            // the accumulator's columns of the thread's c-th 16
-            auto column = [&](int c) { return GATED ? (c >> 2) * 128 + part * 64 + (c & 3) * 16 : part * 128 + c * 16; };
+            // the accumulator's columns of the thread's c-th 32
+            auto column = [&](int c) { return GATED ? (c >> 1) * 128 + part * 64 + (c & 1) * 32 : part * 128 + c * 32; };
             float4 rows = {}, cols = {}, cols2 = {};  // the scales of the next four blocks
             for (int k = 0; k < nk; ++k) {
                 const float* slot = rings + slot_at * kSlotFloats;
@@ -387,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     cols = *reinterpret_cast<const float4*>(slot + kColumns + (GATED ? 0 : part * 4));
                     if (GATED) cols2 = *reinterpret_cast<const float4*>(slot + kColumns + 4);
                 }
-                const float sp = rows.x, f0 = sp * cols.x, f1 = GATED ? sp * cols2.x : f0;
+                const float sp = rows.x, f0 = VEC ? 0.0f : sp * cols.x, f1 = GATED && !VEC ? sp * cols2.x : f0;
                 rows = make_float4(rows.y, rows.z, rows.w, 0.0f);
                 cols = make_float4(cols.y, cols.z, cols.w, 0.0f);
                 cols2 = make_float4(cols2.y, cols2.z, cols2.w, 0.0f);
@@ -395,37 +441,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t from = taddr + (uint32_t)buf * 256u;
-                auto freed_now = [&]() {  // the accumulator has been read
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_either(freed + (uint32_t)buf * 8u);
-                };
-                if (vec) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t r[16];
-                        tmem_ld_32x32b_x16(from + column(c), r);
-                        float f[16];
-#pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
-                            const float4 v = *reinterpret_cast<const float4*>(slot + kColumns + (k & 3) * 256 + column(c) + j);
-                            f[j] = sp * v.x, f[j + 1] = sp * v.y, f[j + 2] = sp * v.z, f[j + 3] = sp * v.w;
-                        }
-                        tmem_ld_wait();
-                        if (c == 7) freed_now();
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fmaf(__uint_as_float(r[j]), f[j], acc[c * 16 + j]);
+                for (int c = 0; c < 4; ++c) {
+                    // (32 columns a load: of 16, their latencies take a fifth longer)
+                    uint32_t r[32];
+                    tmem_ld_32x32b_x32(from + column(c), r);
+                    tmem_ld_wait();
+                    if (c == 3) {  // the accumulator has been read
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_either(freed + (uint32_t)buf * 8u);
                     }
-                } else {
+                    if (VEC) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t r[16];
-                        tmem_ld_32x32b_x16(from + column(c), r);
-                        tmem_ld_wait();
-                        if (c == 7) freed_now();
-                        const float f = c < 4 ? f0 : f1;
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 f = *reinterpret_cast<const float4*>(slot + kColumns + (k & 3) * 256 + column(c) + j);
+                            acc[c * 32 + j] = fmaf(__uint_as_float(r[j]), sp * f.x, acc[c * 32 + j]);
+                            acc[c * 32 + j + 1] = fmaf(__uint_as_float(r[j + 1]), sp * f.y, acc[c * 32 + j + 1]);
+                            acc[c * 32 + j + 2] = fmaf(__uint_as_float(r[j + 2]), sp * f.z, acc[c * 32 + j + 2]);
+                            acc[c * 32 + j + 3] = fmaf(__uint_as_float(r[j + 3]), sp * f.w, acc[c * 32 + j + 3]);
+                        }
+                    } else {
+                        const float f = c < 2 ? f0 : f1;
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fmaf(__uint_as_float(r[j]), f, acc[c * 16 + j]);
+                        for (int j = 0; j < 32; ++j) acc[c * 32 + j] = fmaf(__uint_as_float(r[j]), f, acc[c * 32 + j]);
                     }
                 }
                 if ((k & 3) == 3 || k + 1 == nk) {
@@ -557,14 +596,14 @@ bool encode8(CUtensorMap* map, const Q8Operand& o)
 
 Scales scales_of(const Q8Operand& o) { return {o.s, o.s_row, o.s_block, o.rows, o.shift}; }
 
-template <bool GATED>
+template <bool GATED, bool VEC>
 sadmm_status run(const Maps& maps, const Args& a, int ctas, cudaStream_t s)
 {
     static bool configured[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
     constexpr int smem = kStages * (int)kStageBytes + kSlots * kSlotFloats * 4 + 1024;
-    auto kern = k_q8_pair<GATED>;
+    auto kern = k_q8_pair<GATED, VEC>;
     if (!configured[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
             return SADMM_ECUDA;
@@ -607,6 +646,7 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     Maps maps;
     memset(&a, 0, sizeof(a));
     const bool gated = t[0]->mode == kTgGated;
+    bool vec = false;  // a product's columns have scales of single rows
     long long tiles = 0;
     int next = 0;
     for (int i = 0; i < count; ++i) {
@@ -634,7 +674,7 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
         for (int j = 0; j < 2; ++j) {
             p.ps[j] = scales_of(q.a[na == 2 ? j : 0]);
             p.qs[j] = scales_of(q.b[nb == 2 ? j : 0]);
-            if (p.qs[j].shift == 0) p.vec = 1;
+            vec = vec || p.qs[j].shift == 0;
         }
     }
     a.t.products = count;
@@ -651,7 +691,8 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     a.idesc = (1u << 4) | (256u >> 3) << 17 | (256u >> 4) << 24;  // e4m3 operands, fp32 sums, 256 x 256
     const long long pairs = device_sm_count() / 2;
     const int ctas = 2 * (int)(tiles < pairs ? tiles : pairs);
-    return gated ? run<true>(maps, a, ctas, s) : run<false>(maps, a, ctas, s);
+    if (gated) return vec ? run<true, true>(maps, a, ctas, s) : run<true, false>(maps, a, ctas, s);
+    return vec ? run<false, true>(maps, a, ctas, s) : run<false, false>(maps, a, ctas, s);
 }
 
 }  // namespace sadmm
