@@ -146,6 +146,65 @@ SADMM_DEV uint4 load16(const uint8_t* p, int n, const Span& m)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// The 16-byte words that hold eight neighbours of ES bytes each: all of a group's are
+// asked for before the first is used.
+// AL: the matrix's rows start on 16-byte boundaries; else whether they do is said at run time.
+template <int ES, bool AL = false>
+struct Raw8 {
+    static constexpr int n = ES / 2 + !AL;
+    uint4 w[n];           // the last one off 16-byte boundaries only
+    bool apart;           // not inside the matrix: to be read one by one
+};
+// `in`: at least one of the eight at p is wanted; aligned: p is on a 16-byte boundary (the same for the whole matrix).
+template <int ES, bool AL>
+SADMM_DEV void ask8(const uint8_t* p, bool in, bool aligned, const Span& m, Raw8<ES, AL>& r)
+{
+    aligned = AL || aligned;
+    const uint8_t* b = AL ? p : p - (reinterpret_cast<uintptr_t>(p) & 15);
+    const bool ok = in && b >= m.lo && b + (ES / 2 + !aligned) * 16 <= m.hi;
+    r.apart = in && !ok;
+#pragma unroll
+    for (int k = 0; k < r.n; ++k) {
+        r.w[k] = make_uint4(0, 0, 0, 0);
+        if (ok && (k < ES / 2 || !aligned)) r.w[k] = *reinterpret_cast<const uint4*>(b + 16 * k);
+    }
+}
+SADMM_DEV void load8(const void* p, int dt, int n, const Span& m, float (&v)[8]);
+// Their values, zeros after the n-th.
+template <int ES, bool AL>
+SADMM_DEV void take8(const uint8_t* p, int n, bool aligned, const Span& m, const Raw8<ES, AL>& r, float (&v)[8])
+{
+    if (r.apart) {
+        load8(p, ES == 2 ? SADMM_BF16 : SADMM_FP32, n, m, v);
+        return;
+    }
+    constexpr int W = 2 * ES;  // 32-bit words of the eight
+    uint32_t w[W + 4];
+#pragma unroll
+    for (int k = 0; k < r.n; ++k) w[4 * k] = r.w[k].x, w[4 * k + 1] = r.w[k].y, w[4 * k + 2] = r.w[k].z, w[4 * k + 3] = r.w[k].w;
+    if (!AL && !aligned) {
+        const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < W + 3; ++i) w[i] = w[i + 1];
+        }
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < W + 2; ++i) w[i] = w[i + 2];
+        }
+        if (ES == 2 && (off & 2)) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float x = ES == 4 ? __uint_as_float(w[ES == 4 ? j : 0])
+                                : __uint_as_float((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+        v[j] = j < n ? x : 0.0f;
+    }
+}
+
 // Eight neighbours of a bf16 (dt SADMM_BF16) or fp32 matrix at element p, `n` of
 // them wanted (at least one); zeros after those.
 SADMM_DEV void load8(const void* p, int dt, int n, const Span& m, float (&v)[8])

@@ -17,6 +17,7 @@ struct Args {
     sadmm_q8_out out[2], out_t[2];
     float* part[2];         // [row tiles][cols] column sums of a tile's rows; NULL: not wanted
     long long row_tiles, col_tiles;
+    int x_aligned, z_aligned, u_aligned;  // rows start on 16-byte boundaries
     int* status;
 };
 
@@ -41,36 +42,60 @@ SADMM_DEV Spans spans_of(const Args& a)
     return s;
 }
 
-// Columns c .. c+7 of row r of the source (which: dg or du); zeros outside the matrix.
-template <int PRO>
-SADMM_DEV void load_source(const Args& a, const Spans& s, int which, long long r, long long c, float (&v)[8])
-{
-    const int n = (int)min(8ll, a.cols - c);
-    if (r >= a.rows || n <= 0 || !dbg_in(r, a.rows, a.status) || !dbg_run(c, n, a.cols, a.status)) {
+// Columns c .. c+7 of N rows from r on (with `step` between them): the words first, then the values.
+template <int ES, int N, bool AL>
+struct Rows8 {
+    Raw8<ES, AL> raw[N];
+    SADMM_DEV void ask(const void* p, long long ld, bool aligned, const Span& m, const Args& a, long long r, long long step,
+                       long long c)
+    {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-        return;
+        for (int i = 0; i < N; ++i) {
+            const long long row = r + i * step;
+            const bool in = row < a.rows && c < a.cols && dbg_in(row, a.rows, a.status) && dbg_in(c, a.cols, a.status);
+            ask8(static_cast<const uint8_t*>(p) + (in ? (row * ld + c) * ES : 0), in, aligned, m, raw[i]);
+        }
     }
-    load8(static_cast<const uint8_t*>(a.x) + (r * a.ldx + c) * (a.xdt == SADMM_BF16 ? 2 : 4), a.xdt, n, s.x, v);
-    if (PRO == kPlain || (PRO == kSlope && a.act == SADMM_ACT_NONE)) return;
-    float z[8], u[8];
-    load8(static_cast<const __nv_bfloat16*>(a.z) + r * a.ldz + c, SADMM_BF16, n, s.z, z);
-    if (PRO == kGate && which == 0) load8(static_cast<const __nv_bfloat16*>(a.u) + r * a.ldu + c, SADMM_BF16, n, s.u, u);
-    with_act(a.act, [&](auto tag) {
+    SADMM_DEV void take(const void* p, long long ld, bool aligned, const Span& m, const Args& a, long long r, long long step,
+                        long long c, int i, float (&v)[8]) const
+    {
+        take8(static_cast<const uint8_t*>(p) + ((r + i * step) * ld + c) * ES, (int)min(8ll, a.cols - c), aligned, m, raw[i], v);
+    }
+};
+
+// The source's values in the same places, zeros outside the matrix (which: dg or du).
+template <int PRO, int ACT, int ES, int N, bool AL>
+SADMM_DEV void load_source(const Args& a, const Spans& s, int which, long long r, long long step, long long c, float (*v)[8])
+{
+    constexpr bool Z = PRO == kGate || (PRO == kSlope && ACT != SADMM_ACT_NONE);
+    Rows8<ES, N, AL> x;
+    Rows8<2, Z ? N : 1, AL> z;
+    Rows8<2, PRO == kGate ? N : 1, AL> u;
+    x.ask(a.x, a.ldx, a.x_aligned, s.x, a, r, step, c);
+    if (Z) z.ask(a.z, a.ldz, a.z_aligned, s.z, a, r, step, c);
+    if (PRO == kGate && which == 0) u.ask(a.u, a.ldu, a.u_aligned, s.u, a, r, step, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (r + i * step >= a.rows || c >= a.cols) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+            continue;
+        }
+        x.take(a.x, a.ldx, a.x_aligned, s.x, a, r, step, c, i, v[i]);
+        if (!Z) continue;
+        float zv[8], uv[8];
+        z.take(a.z, a.ldz, a.z_aligned, s.z, a, r, step, c, Z ? i : 0, zv);
+        if (PRO == kGate && which == 0) u.take(a.u, a.ldu, a.u_aligned, s.u, a, r, step, c, PRO == kGate ? i : 0, uv);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float f, slope;
-            act_slope_f32<decltype(tag)::value>(z[j], f, slope);
+            act_slope_f32<ACT>(zv[j], f, slope);
             if (PRO == kGate)
-                v[j] = which ? v[j] * f : v[j] * u[j] * slope;
+                v[i][j] = which ? v[i][j] * f : v[i][j] * uv[j] * slope;
             else
-                v[j] *= slope;
+                v[i][j] *= slope;
+            if (c + j >= a.cols) v[i][j] = 0.0f;  // (the slope there may be 0 times an infinity)
         }
-    });
-    if (n < 8) {  // (act(0) may be 0 times an infinity)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j >= n) v[j] = 0.0f;
     }
 }
 
@@ -80,6 +105,7 @@ constexpr int kRowSteps = 4;  // column blocks of a half warp
 
 // Blocks of one row, the matrix alone: a half warp takes four neighbouring blocks
 // of a row, a lane 8 values of each.
+template <int ES>
 __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
 {
     pdl_wait();
@@ -90,8 +116,17 @@ __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
     const int lane = threadIdx.x & 15;
     const Spans s = spans_of<kPlain>(a);
     float v[kRowSteps][8];
+    Raw8<ES> raw[kRowSteps];
+    auto at = [&](int i) { return (cg * kRowSteps + i) * kQBlock + lane * 8; };
 #pragma unroll
-    for (int i = 0; i < kRowSteps; ++i) load_source<kPlain>(a, s, 0, r, (cg * kRowSteps + i) * kQBlock + lane * 8, v[i]);
+    for (int i = 0; i < kRowSteps; ++i) {
+        const bool in = r < a.rows && at(i) < a.cols && dbg_in(r, a.rows, a.status) && dbg_in(at(i), a.cols, a.status);
+        ask8(static_cast<const uint8_t*>(a.x) + (in ? (r * a.ldx + at(i)) * ES : 0), in, a.x_aligned, s.x, raw[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kRowSteps; ++i)
+        take8(static_cast<const uint8_t*>(a.x) + (r * a.ldx + at(i)) * ES, (int)min(8ll, a.cols - at(i)), a.x_aligned, s.x,
+              raw[i], v[i]);
 #pragma unroll
     for (int i = 0; i < kRowSteps; ++i) {
         const long long b = cg * kRowSteps + i, c = b * kQBlock + lane * 8;
@@ -112,8 +147,8 @@ __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
 // columns of them, so that it holds 8 x 8 values.  The transpose goes through shared
 // memory in 8-byte words of 8 rows of a column, at word (row / 8) ^ (column / 8) of the
 // column's 16, so that neither side meets a bank twice.
-template <int PRO>
-__global__ void __launch_bounds__(256) k_q8_tile(const Args a)
+template <int PRO, int ACT, int ES, bool AL>
+__global__ void __launch_bounds__(256, 2) k_q8_tile(const Args a)
 {
     __shared__ __align__(16) uint2 turned[kQBlock][16];
     __shared__ float red[8][kQBlock], col_top[kQBlock], sums[8][kQBlock];
@@ -127,8 +162,10 @@ __global__ void __launch_bounds__(256) k_q8_tile(const Args a)
     for (int which = 0; which < (PRO == kGate ? 2 : 1); ++which) {
         const sadmm_q8_out &o = a.out[which], &ot = a.out_t[which];
         float v[8][8];
+        constexpr int N = PRO == kPlain ? 8 : PRO == kSlope ? 4 : 2;  // rows whose loads are in flight together
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load_source<PRO>(a, s, which, r0 + row0 + i, c0 + col, v[i]);
+        for (int i = 0; i < 8; i += N)
+            load_source<PRO, ACT, ES, N, AL>(a, s, which, r0 + row0 + i, 1, c0 + col, v + i);
         float top[8];  // of the lane's columns
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -258,6 +295,19 @@ __global__ void __launch_bounds__(1024) k_q8_sums(const float* __restrict__ part
     if (lane == 0 && at < cols) out[at] = v;
 }
 
+using TileKernel = void (*)(const Args);
+
+template <int PRO, int ES>
+TileKernel tile_kernel(int act, bool al)
+{
+    switch (act) {
+    case SADMM_ACT_RELU: return al ? k_q8_tile<PRO, SADMM_ACT_RELU, ES, true> : k_q8_tile<PRO, SADMM_ACT_RELU, ES, false>;
+    case SADMM_ACT_GELU: return al ? k_q8_tile<PRO, SADMM_ACT_GELU, ES, true> : k_q8_tile<PRO, SADMM_ACT_GELU, ES, false>;
+    case SADMM_ACT_SILU: return al ? k_q8_tile<PRO, SADMM_ACT_SILU, ES, true> : k_q8_tile<PRO, SADMM_ACT_SILU, ES, false>;
+    default: return al ? k_q8_tile<PRO, SADMM_ACT_NONE, ES, true> : k_q8_tile<PRO, SADMM_ACT_NONE, ES, false>;
+    }
+}
+
 }  // namespace
 
 size_t q8_source_bytes(const Q8Source& a)
@@ -285,15 +335,30 @@ sadmm_status launch_q8_source(const Q8Source& q, void* ws, cudaStream_t s)
             at += round_up((size_t)a.row_tiles * (size_t)q.cols * 4, 256);
         }
     }
+    auto aligned = [](const void* p, long long ld, int es) {
+        return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * es)) & 15) == 0;
+    };
+    const bool fp32 = q.xdt == SADMM_FP32;
+    a.x_aligned = aligned(a.x, a.ldx, fp32 ? 4 : 2);
+    a.z_aligned = !a.z || aligned(a.z, a.ldz, 2);
+    a.u_aligned = !a.u || aligned(a.u, a.ldu, 2);
+    const bool al = a.x_aligned && a.z_aligned && a.u_aligned;
     cudaError_t err;
     if (!a.z && !q.tile && !q.out_t[0].q && !q.sums[0]) {
         const long long grid = (q.rows + 15) / 16 * ((a.col_tiles + kRowSteps - 1) / kRowSteps);
         if (grid > 0x7fffffffll) return SADMM_EUNSUPPORTED;
-        err = launch_pdl(k_q8_rows, dim3((unsigned)grid), dim3(256), 0, s, a);
+        err = launch_pdl(fp32 ? k_q8_rows<4> : k_q8_rows<2>, dim3((unsigned)grid), dim3(256), 0, s, a);
     } else {
         const long long grid = a.row_tiles * a.col_tiles;
         if (grid > 0x7fffffffll) return SADMM_EUNSUPPORTED;
-        auto kern = q.u ? k_q8_tile<kGate> : a.z || q.sums[0] ? k_q8_tile<kSlope> : k_q8_tile<kPlain>;
+        TileKernel kern;
+        if (q.u)
+            kern = tile_kernel<kGate, 2>(a.act, al);
+        else if (a.z || q.sums[0])
+            kern = fp32 ? tile_kernel<kSlope, 4>(a.z ? a.act : SADMM_ACT_NONE, al) : tile_kernel<kSlope, 2>(a.z ? a.act : SADMM_ACT_NONE, al);
+        else
+            kern = fp32 ? (al ? k_q8_tile<kPlain, SADMM_ACT_NONE, 4, true> : k_q8_tile<kPlain, SADMM_ACT_NONE, 4, false>)
+                        : (al ? k_q8_tile<kPlain, SADMM_ACT_NONE, 2, true> : k_q8_tile<kPlain, SADMM_ACT_NONE, 2, false>);
         err = launch_pdl(kern, dim3((unsigned)grid), dim3(256), 0, s, a);
     }
     if (err == cudaSuccess && (q.sums[0] || q.sums[1]))

@@ -50,6 +50,24 @@ struct Rows {
     const void* p;
     long long ld, rows;
     int dt, cols;
+    int aligned;  // rows start on 16-byte boundaries
+    template <int ES>
+    SADMM_DEV const uint8_t* at(long long r, int c) const
+    {
+        return static_cast<const uint8_t*>(p) + (r * ld + c) * ES;
+    }
+    // Columns c .. c+7 of row r, in two steps.
+    template <int ES, bool AL>
+    SADMM_DEV void ask(long long r, int c, const Span& m, Raw8<ES, AL>& raw, int* status) const
+    {
+        const bool in = r < rows && c < cols && dbg_in(r, rows, status) && dbg_in(c, cols, status);
+        ask8(at<ES>(in ? r : 0, in ? c : 0), in, aligned, m, raw);
+    }
+    template <int ES, bool AL>
+    SADMM_DEV void take(long long r, int c, const Span& m, const Raw8<ES, AL>& raw, float (&v)[8]) const
+    {
+        take8(at<ES>(r, c), cols - c, aligned, m, raw, v);
+    }
     SADMM_DEV int size() const { return dt == SADMM_BF16 ? 2 : 4; }
     SADMM_DEV Span span() const
     {
@@ -133,37 +151,64 @@ SADMM_DEV void finish8(const FwdArgs& a, long long r, int c, float rstd, float (
                  q8_four(v[4], v[5], v[6], v[7]));
 }
 
-// A row over a group of threads, a warp or a block, E times 8 neighbours each,
-// kept in registers between the sum and the output.
-template <bool BLOCK, int E>
-__global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rms_fwd(const FwdArgs a)
+// A row over a group of threads, a warp or a block, E times 8 neighbours each, kept in
+// registers between the sum and the output; the next row's words are asked for
+// before this one's are added up.  XS, RS: bytes of an element of x and of the
+// residual (RS 0: none).
+template <int XS, int RS, bool BLOCK, int E>
+__global__ void __launch_bounds__(BLOCK ? 1024 : 256, BLOCK ? 1 : 3) k_rms_fwd(const FwdArgs a)
 {
+    constexpr int RW = RS ? RS : 2;
     __shared__ RowSums red;
     const int G = BLOCK ? blockDim.x : 32, t = BLOCK ? threadIdx.x : threadIdx.x & 31;
-    const long long r = BLOCK ? (long long)blockIdx.x : (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long step = (long long)gridDim.x * (BLOCK ? 1 : 8);
+    long long r = BLOCK ? (long long)blockIdx.x : (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (BLOCK) {
         clear(red);
         __syncthreads();
     }
     pdl_wait();
     pdl_trigger();
-    if (r >= a.rows) return;
-    const Span mx = a.x.span(), mr = a.res.p ? a.res.span() : mx;
-    float v[E][8], sum = 0.0f;
+    const Span mx = a.x.span(), mr = RS ? a.res.span() : mx;
+    Raw8<XS> nx[E];
+    Raw8<RW> nr[RS ? E : 1];
+    auto ask = [&](long long row) {
 #pragma unroll
-    for (int k = 0; k < E; ++k) load_h(a, r, (k * G + t) * 8, mx, mr, v[k]);
+        for (int k = 0; k < E; ++k) {
+            a.x.ask(row, (k * G + t) * 8, mx, nx[k], a.status);
+            if (RS) a.res.ask(row, (k * G + t) * 8, mr, nr[RS ? k : 0], a.status);
+        }
+    };
+    ask(r);
+    int slot = 0;
+    for (; r < a.rows; r += step) {
+        float v[E][8], sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < E; ++k) {
-        if (a.h.p) a.h.store(r, (k * G + t) * 8, v[k], a.status);
-        float p = 0.0f;
+        for (int k = 0; k < E; ++k) {
+            const int c = (k * G + t) * 8;
+            a.x.take(r, c, mx, nx[k], v[k]);
+            if (RS) {
+                float e[8];
+                a.res.take(r, c, mr, nr[RS ? k : 0], e);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p += v[k][j] * v[k][j];
-        sum += p;
+                for (int j = 0; j < 8; ++j) v[k][j] = RS == 2 ? round_to(v[k][j] + e[j], SADMM_BF16) : v[k][j] + e[j];
+            }
+        }
+        ask(r + step);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            if (RS && a.h.p) a.h.store(r, (k * G + t) * 8, v[k], a.status);
+            float p = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p += v[k][j] * v[k][j];
+            sum += p;
+        }
+        const float rstd = rsqrtf(row_sum<BLOCK>(sum, red, slot) / a.n + a.eps);
+        slot ^= 1;
+        if (t == 0 && a.rstd) a.rstd[r] = rstd;
+#pragma unroll
+        for (int k = 0; k < E; ++k) finish8(a, r, (k * G + t) * 8, rstd, v[k]);
     }
-    const float rstd = rsqrtf(row_sum<BLOCK>(sum, red, 0) / a.n + a.eps);
-    if (t == 0 && a.rstd) a.rstd[r] = rstd;
-#pragma unroll
-    for (int k = 0; k < E; ++k) finish8(a, r, (k * G + t) * 8, rstd, v[k]);
 }
 
 // Rows of any length: a block a row, read twice (the sum from h where it is written,
@@ -217,65 +262,65 @@ SADMM_DEV void load_gamma(const BwdArgs& a, int c, float (&g)[8])
     for (int j = 0; j < 8; ++j) g[j] = !a.gamma ? 1.0f : c + j < a.cols ? a.gamma[c + j] : 0.0f;
 }
 
-// A block takes rows blockIdx.x, + gridDim.x, ...: its threads own columns, add up
-// their shares of dgamma in registers and leave one partial sum a block.
-template <int E>
-__global__ void __launch_bounds__(512) k_rms_bwd(const BwdArgs a)
+// A block takes rows blockIdx.x, + gridDim.x, ...: its threads own eight columns, add up
+// their shares of dgamma in registers and leave one partial sum a block.  The next
+// row's words are asked for before this one's are added up.  HS, YS: bytes of an
+// element of h and of dy; AL: rows start on 16-byte boundaries.
+template <int HS, int YS, bool AL>
+__global__ void __launch_bounds__(1024, 1) k_rms_bwd(const BwdArgs a)
 {
     __shared__ RowSums red;
     clear(red);
     __syncthreads();
     pdl_wait();
     pdl_trigger();
-    const int G = blockDim.x, t = threadIdx.x;
+    const int c = threadIdx.x * 8;
     const Span mh = a.h.span(), my = a.dy.span(), md = a.dres.p ? a.dres.span() : mh;
-    float g[E][8], dg[E][8];
+    float g[8], dg[8];
+    load_gamma(a, c, g);
 #pragma unroll
-    for (int k = 0; k < E; ++k) {
-        load_gamma(a, (k * G + t) * 8, g[k]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dg[k][j] = 0.0f;
-    }
+    for (int j = 0; j < 8; ++j) dg[j] = 0.0f;
+    Raw8<HS, AL> nh, nd;
+    Raw8<YS, AL> ny;
+    float next = 0.0f;
+    auto ask = [&](long long r) {
+        a.h.ask(r, c, mh, nh, a.status);
+        a.dy.ask(r, c, my, ny, a.status);
+        if (a.dres.p) a.dres.ask(r, c, md, nd, a.status);
+        if (r < a.rows) next = a.rstd[r];
+    };
+    ask(blockIdx.x);
     int slot = 0;
     for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const float rstd = a.rstd[r];
-        float hv[E][8], dv[E][8], s = 0.0f;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            a.h.load(r, (k * G + t) * 8, mh, hv[k], a.status);
-            a.dy.load(r, (k * G + t) * 8, my, dv[k], a.status);
-        }
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                hv[k][j] *= rstd;
-                dg[k][j] += dv[k][j] * hv[k][j];
-                dv[k][j] *= g[k][j];
-                s += dv[k][j] * hv[k][j];
-            }
-        const float m = row_sum<true>(s, red, slot) * a.inv_n;
-        slot ^= 1;
-        if (!a.dx.p) continue;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            float e[8];
+        const float rstd = next;
+        float hv[8], dv[8], e[8], s = 0.0f;
+        a.h.take(r, c, mh, nh, hv);
+        a.dy.take(r, c, my, ny, dv);
+        if (a.dres.p) {
+            a.dres.take(r, c, md, nd, e);
+        } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) e[j] = 0.0f;
-            if (a.dres.p) a.dres.load(r, (k * G + t) * 8, md, e, a.status);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = rstd * (dv[k][j] - hv[k][j] * m) + e[j];
-            a.dx.store(r, (k * G + t) * 8, e, a.status);
         }
+        ask(r + gridDim.x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            hv[j] *= rstd;
+            dg[j] += dv[j] * hv[j];
+            dv[j] *= g[j];
+            s += dv[j] * hv[j];
+        }
+        if (!a.dx.p) continue;
+        const float m = row_sum<true>(s, red, slot) * a.inv_n;
+        slot ^= 1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = rstd * (dv[j] - hv[j] * m) + e[j];
+        a.dx.store(r, c, e, a.status);
     }
     if (!a.part) return;
 #pragma unroll
-    for (int k = 0; k < E; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = (k * G + t) * 8 + j;
-            if (c < a.cols) a.part[(long long)blockIdx.x * a.cols + c] = dg[k][j];
-        }
+    for (int j = 0; j < 8; ++j)
+        if (c + j < a.cols) a.part[(long long)blockIdx.x * a.cols + c + j] = dg[j];
 }
 
 // Rows of any length: dx, a block a row, read twice.
@@ -360,23 +405,40 @@ __global__ void __launch_bounds__(1024) k_rms_sums(const float* __restrict__ par
 
 constexpr int kWarpCols = 512;          // up to here a warp takes a row
 constexpr int kFwdCols = 32768;         // up to here a row stays in registers (1024 threads of 32)
-constexpr int kBwdCols = 8192;          // backward: 512 threads of 16
+constexpr int kBwdCols = 8192;          // backward: 1024 threads of 8
 
 int row_threads(int cols, int e) { return (int)round_up((cols + 8 * e - 1) / (8 * e), 32); }
 
-int bwd_blocks(long long rows)
+// Blocks of n threads of 64 registers an SM holds.
+int per_sm(int n) { return n > 512 ? 1 : 1024 / n < 8 ? 1024 / n : 8; }
+
+int bwd_blocks(long long rows, int cols)
 {
-    const long long most = 2ll * device_sm_count();
+    const long long most = (long long)per_sm(cols <= kBwdCols ? row_threads(cols, 1) : 512) * device_sm_count();
     return (int)(rows < most ? rows : most);
 }
 
-Rows rows_of(const void* p, long long ld, int dt, long long rows, int cols) { return {p, ld, rows, dt, cols}; }
+Rows rows_of(const void* p, long long ld, int dt, long long rows, int cols)
+{
+    const long long es = dt == SADMM_BF16 ? 2 : 4;
+    return {p, ld, rows, dt, cols, ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * es)) & 15) == 0};
+}
 
-template <bool BLOCK, int E>
+template <int XS, int RS, bool BLOCK, int E>
 cudaError_t fwd(const FwdArgs& a, cudaStream_t s)
 {
-    const long long grid = BLOCK ? a.rows : (a.rows + 7) / 8;
-    return launch_pdl(k_rms_fwd<BLOCK, E>, dim3((unsigned)grid), dim3(BLOCK ? row_threads(a.cols, E) : 256), 0, s, a);
+    const int threads = BLOCK ? row_threads(a.cols, E) : 256;
+    const long long want = BLOCK ? a.rows : (a.rows + 7) / 8, most = (long long)per_sm(threads) * device_sm_count();
+    return launch_pdl(k_rms_fwd<XS, RS, BLOCK, E>, dim3((unsigned)(want < most ? want : most)), dim3(threads), 0, s, a);
+}
+
+template <int XS, int RS>
+cudaError_t fwd(const FwdArgs& a, cudaStream_t s)
+{
+    if (a.cols <= 256) return fwd<XS, RS, false, 1>(a, s);
+    if (a.cols <= kWarpCols) return fwd<XS, RS, false, 2>(a, s);
+    if (a.cols <= 8192) return fwd<XS, RS, true, 1>(a, s);
+    return fwd<XS, RS, true, 4>(a, s);
 }
 
 }  // namespace
@@ -397,23 +459,20 @@ sadmm_status launch_rmsnorm_fwd(const sadmm_rmsnorm_fwd_args& a, cudaStream_t s)
     f.eps = a.eps;
     f.n = (float)a.cols;
     f.status = device_status_ptr();
+    const int xs = a.xdt == SADMM_BF16 ? 2 : 4, rs = !a.residual ? 0 : a.rdt == SADMM_BF16 ? 2 : 4;
     cudaError_t err;
-    if (a.cols <= 256)
-        err = fwd<false, 1>(f, s);
-    else if (a.cols <= kWarpCols)
-        err = fwd<false, 2>(f, s);
-    else if (a.cols <= 8192)
-        err = fwd<true, 2>(f, s);
-    else if (a.cols <= kFwdCols)
-        err = fwd<true, 4>(f, s);
-    else
+    if (a.cols > kFwdCols)
         err = launch_pdl(k_rms_fwd_long, dim3((unsigned)a.rows), dim3(1024), 0, s, f);
+    else if (xs == 2)
+        err = rs == 0 ? fwd<2, 0>(f, s) : rs == 2 ? fwd<2, 2>(f, s) : fwd<2, 4>(f, s);
+    else
+        err = rs == 0 ? fwd<4, 0>(f, s) : rs == 2 ? fwd<4, 2>(f, s) : fwd<4, 4>(f, s);
     return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
 }
 
 size_t rmsnorm_bwd_bytes(const sadmm_rmsnorm_bwd_args& a)
 {
-    return a.dgamma ? (size_t)bwd_blocks(a.rows) * (size_t)a.cols * 4 : 0;
+    return a.dgamma ? (size_t)bwd_blocks(a.rows, a.cols) * (size_t)a.cols * 4 : 0;
 }
 
 sadmm_status launch_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args& a, void* ws, cudaStream_t s)
@@ -434,12 +493,16 @@ sadmm_status launch_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args& a, void* ws, cudaS
     b.cols = a.cols;
     b.inv_n = (float)(1.0 / a.cols);
     b.status = device_status_ptr();
-    const int blocks = bwd_blocks(a.rows);
+    const int blocks = bwd_blocks(a.rows, a.cols);
     cudaError_t err = cudaSuccess;
-    if (a.cols <= 2048) {
-        err = launch_pdl(k_rms_bwd<1>, dim3(blocks), dim3(row_threads(a.cols, 1)), 0, s, b);
-    } else if (a.cols <= kBwdCols) {
-        err = launch_pdl(k_rms_bwd<2>, dim3(blocks), dim3(row_threads(a.cols, 2)), 0, s, b);
+    if (a.cols <= kBwdCols) {
+        const int hs = a.hdt == SADMM_BF16 ? 2 : 4, ys = a.dydt == SADMM_BF16 ? 2 : 4;
+        const bool al = b.h.aligned && b.dy.aligned && (!b.dres.p || b.dres.aligned);
+        auto kern = al ? (hs == 2 ? (ys == 2 ? k_rms_bwd<2, 2, true> : k_rms_bwd<2, 4, true>)
+                                  : (ys == 2 ? k_rms_bwd<4, 2, true> : k_rms_bwd<4, 4, true>))
+                       : (hs == 2 ? (ys == 2 ? k_rms_bwd<2, 2, false> : k_rms_bwd<2, 4, false>)
+                                  : (ys == 2 ? k_rms_bwd<4, 2, false> : k_rms_bwd<4, 4, false>));
+        err = launch_pdl(kern, dim3(blocks), dim3(row_threads(a.cols, 1)), 0, s, b);
     } else {
         if (a.dx) err = launch_pdl(k_rms_bwd_long, dim3((unsigned)a.rows), dim3(1024), 0, s, b);
         if (err == cudaSuccess && b.part)
