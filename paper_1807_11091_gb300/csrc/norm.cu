@@ -1,5 +1,6 @@
 // norm.cu -- layer norm over the rows of a matrix, forward and backward, with
-// the gradients of its weight and bias.
+// the gradients of its weight and bias; and the backward pass of the
+// root-mean-square norm (rms.cu), which is the same without the mean.
 //
 //   y = gamma xhat + beta,  xhat = (x - mean) rstd,  rstd = (var + eps)^-1/2
 //   d = gamma dy,  dx = rstd (d - avg(d) - xhat avg(d xhat)) [+ dres]
@@ -425,9 +426,9 @@ struct BwdArgs {
     const void* dres;
     void* dx;
     const float* gamma;
-    const float* mean;
+    const float* mean;  // NULL: a root-mean-square norm, whose xhat is x rstd and whose dx has no avg(d)
     const float* rstd;
-    float* part_g;  // [blocks][cols] partial dgamma, dbeta; NULL: not wanted
+    float* part_g;  // [blocks][cols] partial dgamma, dbeta; NULL: not wanted (of an RMS norm, no dbeta)
     float* part_b;
     long long rows, ldx, lddy, lddres, lddx;
     int cols;
@@ -492,10 +493,10 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 
     int slot = 0, s = 0, last = 0;
     uint32_t phase = 0;
     float next_mean = 0.0f, next_rstd = 0.0f;
-    if (first < a.rows) next_mean = a.mean[first], next_rstd = a.rstd[first];
+    if (first < a.rows) next_mean = a.mean ? a.mean[first] : 0.0f, next_rstd = a.rstd[first];
     for (long long r = first; r < a.rows; r += step) {
         const float mean = next_mean, rstd = next_rstd;
-        if (r + step < a.rows) next_mean = a.mean[r + step], next_rstd = a.rstd[r + step];
+        if (r + step < a.rows) next_mean = a.mean ? a.mean[r + step] : 0.0f, next_rstd = a.rstd[r + step];
         const uint8_t* row = nullptr;
         if (a.stages) {
             mbar_wait(&bar[s], phase, &abort_flag, a.status);
@@ -526,7 +527,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 
         // the whole group is done with the row before: its place takes the one `stages` rows on
         if (a.stages && c.t == 0 && r != first) fetch(r + (a.stages - 1) * step, last);
         if (a.dx) {
-            const float c1 = sum.x * a.inv_n, c2 = sum.y * a.inv_n;
+            const float c1 = a.mean ? sum.x * a.inv_n : 0.0f, c2 = sum.y * a.inv_n;
             const unsigned long long m1 = pair(-c1, -c1), m2 = pair(-c2, -c2);
             X* dx = static_cast<X*>(a.dx) + r * a.lddx;
 #pragma unroll
@@ -560,7 +561,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 
             for (int j = 0; j < 8; ++j)
                 if (c.at(k, j) < a.cols) {
                     pg[c.at(k, j)] = (j & 1) ? high(dg[k][j / 2]) : low(dg[k][j / 2]);
-                    pb[c.at(k, j)] = (j & 1) ? high(db[k][j / 2]) : low(db[k][j / 2]);
+                    if (a.part_b) pb[c.at(k, j)] = (j & 1) ? high(db[k][j / 2]) : low(db[k][j / 2]);
                 }
     } else {
         // the warps' sums added up in warp order, thread (j, lane) for element j of lane's eight
@@ -568,6 +569,7 @@ __global__ void __launch_bounds__(CAP ? CAP : 256, CAP == 512 ? 1 : CAP && E == 
         for (int k = 0; k < E; ++k)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
+                if (half && !a.part_b) break;
                 __syncthreads();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -595,7 +597,7 @@ __global__ void __launch_bounds__(1024) k_ln_bwd_long(const BwdArgs a)
     const long long r = blockIdx.x;
     const X* x = static_cast<const X*>(a.x) + r * a.ldx;
     const Y* dy = static_cast<const Y*>(a.dy) + r * a.lddy;
-    const float mean = a.mean[r], rstd = a.rstd[r];
+    const float mean = a.mean ? a.mean[r] : 0.0f, rstd = a.rstd[r];
     float2 s = make_float2(0.0f, 0.0f);
     for (int c = threadIdx.x; c < a.cols; c += 1024) {
         const float d = to_f32(dy[c]) * (a.gamma ? a.gamma[c] : 1.0f);
@@ -603,7 +605,7 @@ __global__ void __launch_bounds__(1024) k_ln_bwd_long(const BwdArgs a)
         s.y += d * (to_f32(x[c]) - mean) * rstd;
     }
     s = row_sum2<true>(s.x, s.y, red, 0);
-    const float c1 = s.x * a.inv_n, c2 = s.y * a.inv_n;
+    const float c1 = a.mean ? s.x * a.inv_n : 0.0f, c2 = s.y * a.inv_n;
     const X* dres = a.dres ? static_cast<const X*>(a.dres) + r * a.lddres : nullptr;
     X* dx = static_cast<X*>(a.dx) + r * a.lddx;
     for (int c = threadIdx.x; c < a.cols; c += 1024) {
@@ -625,11 +627,11 @@ __global__ void __launch_bounds__(256) k_ln_cols_long(const BwdArgs a)
     float g = 0.0f, b = 0.0f;
     for (long long r = blockIdx.y; r < a.rows; r += gridDim.y) {
         const float dy = to_f32(static_cast<const Y*>(a.dy)[r * a.lddy + c]);
-        g += dy * (to_f32(static_cast<const X*>(a.x)[r * a.ldx + c]) - a.mean[r]) * a.rstd[r];
+        g += dy * (to_f32(static_cast<const X*>(a.x)[r * a.ldx + c]) - (a.mean ? a.mean[r] : 0.0f)) * a.rstd[r];
         b += dy;
     }
     a.part_g[(long long)blockIdx.y * a.cols + c] = g;
-    a.part_b[(long long)blockIdx.y * a.cols + c] = b;
+    if (a.part_b) a.part_b[(long long)blockIdx.y * a.cols + c] = b;
 }
 
 // out[c] = the sum of part[0 .. parts-1][c], 32 groups of parts at a time, then
@@ -788,6 +790,24 @@ sadmm_status bwd(const BwdArgs& a, cudaStream_t s)
     return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
 }
 
+sadmm_status run_bwd(const BwdArgs& b, int xdt, int dydt, cudaStream_t s)
+{
+    const bool vec = rows16(b.x, b.ldx, xdt) && rows16(b.dy, b.lddy, dydt) && rows16(b.dres, b.lddres, xdt) &&
+                     rows16(b.dx, b.lddx, xdt) && rows16(b.gamma, 0, SADMM_FP32);
+    sadmm_status st;
+    if (xdt == SADMM_BF16) {
+        if (dydt == SADMM_BF16)
+            st = vec ? bwd<bf16, bf16, true>(b, s) : bwd<bf16, bf16, false>(b, s);
+        else
+            st = vec ? bwd<bf16, float, true>(b, s) : bwd<bf16, float, false>(b, s);
+    } else if (dydt == SADMM_BF16) {
+        st = vec ? bwd<float, bf16, true>(b, s) : bwd<float, bf16, false>(b, s);
+    } else {
+        st = vec ? bwd<float, float, true>(b, s) : bwd<float, float, false>(b, s);
+    }
+    return st;
+}
+
 }  // namespace
 
 size_t layernorm_bwd_bytes(const sadmm_layernorm_bwd_args& a)
@@ -824,22 +844,30 @@ sadmm_status launch_layernorm_bwd(const sadmm_layernorm_bwd_args& a, void* ws, c
     float* pb = cols ? pg + (size_t)blocks * (size_t)round_up(a.cols, 64) : nullptr;
     const BwdArgs b = {a.x, a.dy, a.dres, a.dx, a.gamma, a.mean, a.rstd, pg, pb, a.rows, a.ldx, a.lddy, a.lddres,
                        a.lddx, a.cols, 0, (float)(1.0 / a.cols), device_status_ptr()};
-    const bool vec = rows16(a.x, a.ldx, a.xdt) && rows16(a.dy, a.lddy, a.dydt) && rows16(a.dres, a.lddres, a.xdt) &&
-                     rows16(a.dx, a.lddx, a.xdt) && rows16(a.gamma, 0, SADMM_FP32);
-    sadmm_status st;
-    if (a.xdt == SADMM_BF16) {
-        if (a.dydt == SADMM_BF16)
-            st = vec ? bwd<bf16, bf16, true>(b, s) : bwd<bf16, bf16, false>(b, s);
-        else
-            st = vec ? bwd<bf16, float, true>(b, s) : bwd<bf16, float, false>(b, s);
-    } else if (a.dydt == SADMM_BF16) {
-        st = vec ? bwd<float, bf16, true>(b, s) : bwd<float, bf16, false>(b, s);
-    } else {
-        st = vec ? bwd<float, float, true>(b, s) : bwd<float, float, false>(b, s);
-    }
+    const sadmm_status st = run_bwd(b, a.xdt, a.dydt, s);
     if (st != SADMM_OK || !cols) return st;
     return launch_pdl(k_ln_sums, dim3((unsigned)((a.cols + 31) / 32), 2), dim3(1024), 0, s, pg, pb, a.dgamma, a.dbeta,
                       a.cols, blocks) == cudaSuccess
+               ? SADMM_OK
+               : SADMM_ECUDA;
+}
+
+size_t rmsnorm_bwd_bytes(const sadmm_rmsnorm_bwd_args& a)
+{
+    return a.dgamma ? (size_t)bwd_blocks(a.rows, a.cols) * (size_t)round_up(a.cols, 64) * 4 : 0;
+}
+
+sadmm_status launch_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args& a, void* ws, cudaStream_t s)
+{
+    if (a.rows == 0)
+        return a.dgamma && cudaMemsetAsync(a.dgamma, 0, (size_t)a.cols * 4, s) != cudaSuccess ? SADMM_ECUDA : SADMM_OK;
+    float* pg = a.dgamma ? static_cast<float*>(ws) : nullptr;
+    const BwdArgs b = {a.h, a.dy, a.dres, a.dx, a.gamma, nullptr, a.rstd, pg, nullptr, a.rows, a.ldh, a.lddy, a.lddres,
+                       a.lddx, a.cols, 0, (float)(1.0 / a.cols), device_status_ptr()};
+    const sadmm_status st = run_bwd(b, a.hdt, a.dydt, s);
+    if (st != SADMM_OK || !pg) return st;
+    return launch_pdl(k_ln_sums, dim3((unsigned)((a.cols + 31) / 32), 1), dim3(1024), 0, s, pg, nullptr, a.dgamma, nullptr,
+                      a.cols, bwd_blocks(a.rows, a.cols)) == cudaSuccess
                ? SADMM_OK
                : SADMM_ECUDA;
 }

@@ -143,64 +143,91 @@ __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
     }
 }
 
-// A tile of 128 x 128 a CTA: warp w's half h takes rows 16 w + 8 h ... + 7, a lane 8
-// columns of them, so that it holds 8 x 8 values.  The transpose goes through shared
-// memory in 8-byte words of 8 rows of a column, at word (row / 8) ^ (column / 8) of the
-// column's 16, so that neither side meets a bank twice.
+// A tile of 128 x 128 a CTA.  A half warp takes a row (a lane 8 columns), so that a
+// row's block is quantised as it comes (with `tile` after the whole tile has); the values
+// also go to shared memory, where the transpose's blocks are read: a thread a column, 16
+// rows at a time.  Loops of few rows: unrolled over the
+// tile, the instructions came from memory (no instruction to issue for a third of the time).
 template <int PRO, int ACT, int ES, bool AL>
-__global__ void __launch_bounds__(256, 2) k_q8_tile(const Args a)
+__global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
 {
-    __shared__ __align__(16) uint2 turned[kQBlock][16];
-    __shared__ float red[8][kQBlock], col_top[kQBlock], sums[8][kQBlock];
+    constexpr int U = PRO == kGate ? 2 : 4;  // rows whose loads are in flight together
+    extern __shared__ __align__(16) float vals[];  // [128][128]
+    __shared__ float red[8][kQBlock], sums[PRO == kPlain ? 1 : 8][PRO == kPlain ? 1 : kQBlock], top_s[kQBlock];
     pdl_wait();
     pdl_trigger();
-    const int warp = threadIdx.x >> 5, half = (threadIdx.x >> 4) & 1, lane = threadIdx.x & 15;
+    const int hw = threadIdx.x >> 4, lane = threadIdx.x & 15, col = lane * 8;
     const long long rt = blockIdx.x / a.col_tiles, ct = blockIdx.x - rt * a.col_tiles;
     const long long r0 = rt * kQBlock, c0 = ct * kQBlock;
-    const int row0 = warp * 16 + half * 8, col = lane * 8;
     const Spans s = spans_of<PRO>(a);
+    const int live = (int)max(0ll, min(8ll, a.cols - c0 - col));  // the lane's columns inside the matrix
+    auto put_row = [&](const sadmm_q8_out& o, int row, const Q8Scale& k, const float (&v)[8]) {
+        const long long r = r0 + row;
+        if (r >= a.rows || live == 0 || !dbg_in(r, a.rows, a.status) || !dbg_run(c0 + col, live, a.cols, a.status)) return;
+        if (!a.tile && lane == 0) store_scale(o, r, ct, k.s);
+        float q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = q8_quotient(v[j], k);
+        store_bytes8(static_cast<uint8_t*>(o.q) + r * o.ld + c0 + col, live, q8_four(q[0], q[1], q[2], q[3]),
+                     q8_four(q[4], q[5], q[6], q[7]));
+    };
     for (int which = 0; which < (PRO == kGate ? 2 : 1); ++which) {
         const sadmm_q8_out &o = a.out[which], &ot = a.out_t[which];
-        float v[8][8];
-        constexpr int N = PRO == kPlain ? 8 : PRO == kSlope ? 4 : 2;  // rows whose loads are in flight together
+        const bool keep = ot.q || a.tile;
+        float top[8], sum[8];
 #pragma unroll
-        for (int i = 0; i < 8; i += N)
-            load_source<PRO, ACT, ES, N, AL>(a, s, which, r0 + row0 + i, 1, c0 + col, v + i);
-        float top[8];  // of the lane's columns
+        for (int j = 0; j < 8; ++j) top[j] = sum[j] = 0.0f;
+#pragma unroll 1
+        for (int i = 0; i < 8; i += U) {
+            float v[U][8];
+            load_source<PRO, ACT, ES, U, AL>(a, s, which, r0 + i * 16 + hw, 16, c0 + col, v);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int row = (i + u) * 16 + hw;
+                float t = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = q8_size(v[u][j]);
+                    top[j] = fmaxf(top[j], x);
+                    t = fmaxf(t, x);
+                    if (PRO != kPlain) sum[j] += v[u][j];
+                }
+                if (!a.tile && o.q) put_row(o, row, q8_scale(max16(t)), v[u]);
+                if (keep) {
+                    float4* to = reinterpret_cast<float4*>(vals + row * kQBlock + col);
+                    to[0] = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
+                    to[1] = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
+                }
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            top[j] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top[j] = fmaxf(top[j], q8_size(v[i][j]));
+            top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
+            if (PRO != kPlain) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+            if (hw & 1) continue;
+            red[hw >> 1][col + j] = top[j];
+            if (PRO != kPlain) sums[PRO == kPlain ? 0 : hw >> 1][PRO == kPlain ? 0 : col + j] = sum[j];
         }
-        if (PRO != kPlain && a.part[which]) {
+        __syncthreads();
+        if (threadIdx.x < kQBlock) {
+            float t = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int w = 0; w < 8; ++w) t = fmaxf(t, red[w][threadIdx.x]);
+            top_s[threadIdx.x] = t;
+            if (PRO != kPlain && a.part[which] && c0 + threadIdx.x < a.cols) {
                 float p = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p += v[i][j];
-                p += __shfl_xor_sync(0xffffffffu, p, 16);
-                if (half == 0) sums[warp][col + j] = p;
+                for (int w = 0; w < 8; ++w) p += sums[PRO == kPlain ? 0 : w][PRO == kPlain ? 0 : threadIdx.x];
+                a.part[which][rt * a.cols + c0 + threadIdx.x] = p;
             }
         }
-        Q8Scale tile = {1.0f, 1.0f};
-        if (a.tile || ot.q) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float t = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
-                if (half == 0) red[warp][col + j] = t;
-            }
+        if (keep) {
             __syncthreads();
-            if (threadIdx.x < kQBlock) {
-                float t = 0.0f;
-#pragma unroll
-                for (int w = 0; w < 8; ++w) t = fmaxf(t, red[w][threadIdx.x]);
-                col_top[threadIdx.x] = t;
-            }
-            __syncthreads();
+            Q8Scale tile = {1.0f, 1.0f};
             if (a.tile) {
                 float t = 0.0f;
-                for (int j = 0; j < 4; ++j) t = fmaxf(t, col_top[(threadIdx.x & 31) * 4 + j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t = fmaxf(t, top_s[(threadIdx.x & 31) * 4 + j]);
 #pragma unroll
                 for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
                 tile = q8_scale(t);
@@ -208,59 +235,40 @@ __global__ void __launch_bounds__(256, 2) k_q8_tile(const Args a)
                     if (o.q) store_scale(o, rt, ct, tile.s);
                     if (ot.q) store_scale(ot, ct, rt, tile.s);
                 }
-            }
-        } else if (PRO != kPlain && a.part[which]) {
-            __syncthreads();
-        }
-        if (PRO != kPlain && a.part[which] && threadIdx.x < kQBlock && c0 + threadIdx.x < a.cols) {
-            float p = 0.0f;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) p += sums[w][threadIdx.x];
-            a.part[which][rt * a.cols + c0 + threadIdx.x] = p;
-        }
-        if (o.q) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const long long r = r0 + row0 + i;
-                Q8Scale k = tile;
-                if (!a.tile) {
-                    float t = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) t = fmaxf(t, q8_size(v[i][j]));
-                    k = q8_scale(max16(t));
+                if (o.q) {
+#pragma unroll 2
+                    for (int row = hw; row < kQBlock; row += 16) {
+                        const float4* from = reinterpret_cast<const float4*>(vals + row * kQBlock + col);
+                        const float4 x = from[0], y = from[1];
+                        const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                        put_row(o, row, tile, v);
+                    }
                 }
-                if (r >= a.rows || c0 + col >= a.cols || !dbg_in(r, a.rows, a.status) ||
-                    !dbg_in(c0 + col, a.cols, a.status))
-                    continue;
-                if (!a.tile && lane == 0) store_scale(o, r, ct, k.s);
-                float q[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = q8_quotient(v[i][j], k);
-                store_bytes8(static_cast<uint8_t*>(o.q) + r * o.ld + c0 + col, (int)min(8ll, a.cols - c0 - col),
-                             q8_four(q[0], q[1], q[2], q[3]), q8_four(q[4], q[5], q[6], q[7]));
             }
-        }
-        if (ot.q) {
+            if (ot.q) {
+                const int c = threadIdx.x & 127;
+                const Q8Scale k = a.tile ? tile : q8_scale(top_s[c]);
+                const bool in = c0 + c < a.cols && dbg_in(c0 + c, a.cols, a.status);
+                if (!a.tile && in && threadIdx.x < kQBlock) store_scale(ot, c0 + c, rt, k.s);
+                uint8_t* to = static_cast<uint8_t*>(ot.q) + (in ? (c0 + c) * ot.ld : 0) + r0;
+#pragma unroll 1
+                for (int row = (threadIdx.x >> 7) * 16; row < kQBlock; row += 32) {
+                    uint32_t w[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const Q8Scale k = a.tile ? tile : q8_scale(col_top[col + j]);
-                if (!a.tile && row0 == 0 && c0 + col + j < a.cols) store_scale(ot, c0 + col + j, rt, k.s);
-                float q[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) q[i] = q8_quotient(v[i][j], k);
-                turned[col + j][(warp * 2 + half) ^ lane] =
-                    make_uint2(q8_four(q[0], q[1], q[2], q[3]), q8_four(q[4], q[5], q[6], q[7]));
-            }
-            __syncthreads();
-            const int n = (int)min(8ll, a.rows - r0 - lane * 8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = (threadIdx.x >> 4) * 8 + i;
-                const uint2 w = turned[c][lane ^ (c >> 3)];
-                if (c0 + c >= a.cols || n <= 0 || !dbg_in(c0 + c, a.cols, a.status) ||
-                    !dbg_in(r0 + lane * 8, a.rows, a.status))
-                    continue;
-                store_bytes8(static_cast<uint8_t*>(ot.q) + (c0 + c) * ot.ld + r0 + lane * 8, n, w.x, w.y);
+                    for (int i = 0; i < 4; ++i) {
+                        const float* f = vals + (row + 4 * i) * kQBlock + c;
+                        w[i] = q8_four(q8_quotient(f[0], k), q8_quotient(f[kQBlock], k), q8_quotient(f[2 * kQBlock], k),
+                                       q8_quotient(f[3 * kQBlock], k));
+                    }
+                    const int n = (int)min(16ll, a.rows - r0 - row);
+                    if (!in || n <= 0 || !dbg_run(r0 + row, n, a.rows, a.status)) continue;
+                    if (n == 16 && (reinterpret_cast<uintptr_t>(to + row) & 15) == 0) {
+                        *reinterpret_cast<uint4*>(to + row) = make_uint4(w[0], w[1], w[2], w[3]);
+                    } else {
+                        store_bytes8(to + row, n, w[0], w[1]);
+                        store_bytes8(to + row + 8, n - 8, w[2], w[3]);
+                    }
+                }
             }
         }
         if (PRO == kGate) __syncthreads();  // shared memory is written again
@@ -295,16 +303,34 @@ __global__ void __launch_bounds__(1024) k_q8_sums(const float* __restrict__ part
     if (lane == 0 && at < cols) out[at] = v;
 }
 
-using TileKernel = void (*)(const Args);
-
+template <int PRO, int ACT, int ES, bool AL>
+cudaError_t launch_tiles(const Args& a, long long grid, cudaStream_t s)
+{
+    static bool configured[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    constexpr int smem = kQBlock * kQBlock * 4;
+    auto kern = k_q8_tile<PRO, ACT, ES, AL>;
+    if (!configured[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    return launch_pdl(kern, dim3((unsigned)grid), dim3(256), smem, s, a);
+}
+template <int PRO, int ACT, int ES>
+cudaError_t launch_tiles(const Args& a, bool al, long long grid, cudaStream_t s)
+{
+    return al ? launch_tiles<PRO, ACT, ES, true>(a, grid, s) : launch_tiles<PRO, ACT, ES, false>(a, grid, s);
+}
 template <int PRO, int ES>
-TileKernel tile_kernel(int act, bool al)
+cudaError_t launch_tiles(const Args& a, int act, bool al, long long grid, cudaStream_t s)
 {
     switch (act) {
-    case SADMM_ACT_RELU: return al ? k_q8_tile<PRO, SADMM_ACT_RELU, ES, true> : k_q8_tile<PRO, SADMM_ACT_RELU, ES, false>;
-    case SADMM_ACT_GELU: return al ? k_q8_tile<PRO, SADMM_ACT_GELU, ES, true> : k_q8_tile<PRO, SADMM_ACT_GELU, ES, false>;
-    case SADMM_ACT_SILU: return al ? k_q8_tile<PRO, SADMM_ACT_SILU, ES, true> : k_q8_tile<PRO, SADMM_ACT_SILU, ES, false>;
-    default: return al ? k_q8_tile<PRO, SADMM_ACT_NONE, ES, true> : k_q8_tile<PRO, SADMM_ACT_NONE, ES, false>;
+    case SADMM_ACT_RELU: return launch_tiles<PRO, SADMM_ACT_RELU, ES>(a, al, grid, s);
+    case SADMM_ACT_GELU: return launch_tiles<PRO, SADMM_ACT_GELU, ES>(a, al, grid, s);
+    case SADMM_ACT_SILU: return launch_tiles<PRO, SADMM_ACT_SILU, ES>(a, al, grid, s);
+    default: return launch_tiles<PRO, SADMM_ACT_NONE, ES>(a, al, grid, s);
     }
 }
 
@@ -351,15 +377,14 @@ sadmm_status launch_q8_source(const Q8Source& q, void* ws, cudaStream_t s)
     } else {
         const long long grid = a.row_tiles * a.col_tiles;
         if (grid > 0x7fffffffll) return SADMM_EUNSUPPORTED;
-        TileKernel kern;
+        const int act = a.z ? a.act : SADMM_ACT_NONE;
         if (q.u)
-            kern = tile_kernel<kGate, 2>(a.act, al);
+            err = launch_tiles<kGate, 2>(a, act, al, grid, s);
         else if (a.z || q.sums[0])
-            kern = fp32 ? tile_kernel<kSlope, 4>(a.z ? a.act : SADMM_ACT_NONE, al) : tile_kernel<kSlope, 2>(a.z ? a.act : SADMM_ACT_NONE, al);
+            err = fp32 ? launch_tiles<kSlope, 4>(a, act, al, grid, s) : launch_tiles<kSlope, 2>(a, act, al, grid, s);
         else
-            kern = fp32 ? (al ? k_q8_tile<kPlain, SADMM_ACT_NONE, 4, true> : k_q8_tile<kPlain, SADMM_ACT_NONE, 4, false>)
-                        : (al ? k_q8_tile<kPlain, SADMM_ACT_NONE, 2, true> : k_q8_tile<kPlain, SADMM_ACT_NONE, 2, false>);
-        err = launch_pdl(kern, dim3((unsigned)grid), dim3(256), 0, s, a);
+            err = fp32 ? launch_tiles<kPlain, SADMM_ACT_NONE, 4>(a, al, grid, s)
+                       : launch_tiles<kPlain, SADMM_ACT_NONE, 2>(a, al, grid, s);
     }
     if (err == cudaSuccess && (q.sums[0] || q.sums[1]))
         err = launch_pdl(k_q8_sums, dim3((unsigned)((q.cols + 31) / 32), 2), dim3(1024), 0, s, a.part[0], a.part[1],

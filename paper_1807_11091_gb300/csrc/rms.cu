@@ -1,10 +1,8 @@
 // rms.cu -- root-mean-square norm of rows, with the residual's addition before
-// it and its output in 8 bits where wanted, forward and backward.
+// it and its output in 8 bits where wanted (the backward pass: norm.cu).
 //
 //   h = x + residual (rounded to the residual's type),  y = gamma h rstd,
 //   rstd = (avg h^2 + eps)^-1/2
-//   d = gamma dy,  dx = rstd (d - hhat avg(d hhat)) [+ dres],  hhat = h rstd
-//   dgamma = sum over rows of dy hhat
 #include "q8.cuh"
 
 namespace sadmm {
@@ -154,11 +152,12 @@ SADMM_DEV void finish8(const FwdArgs& a, long long r, int c, float rstd, float (
 // A row over a group of threads, a warp or a block, E times 8 neighbours each, kept in
 // registers between the sum and the output; the next row's words are asked for
 // before this one's are added up.  XS, RS: bytes of an element of x and of the
-// residual (RS 0: none).
-template <int XS, int RS, bool BLOCK, int E>
-__global__ void __launch_bounds__(BLOCK ? 1024 : 256, BLOCK ? 1 : 3) k_rms_fwd(const FwdArgs a)
+// residual (RS 0: none); AL: rows start on 16-byte boundaries.
+template <int XS, int RS, bool BLOCK, int E, bool AL>
+__global__ void __launch_bounds__(!BLOCK ? 256 : E == 4 ? 1024 : 512, !BLOCK ? 3 : E == 4 ? 1 : 2) k_rms_fwd(const FwdArgs a)
 {
     constexpr int RW = RS ? RS : 2;
+    constexpr bool AHEAD = E < 4;  // (four times eight: no registers for the next row)
     __shared__ RowSums red;
     const int G = BLOCK ? blockDim.x : 32, t = BLOCK ? threadIdx.x : threadIdx.x & 31;
     const long long step = (long long)gridDim.x * (BLOCK ? 1 : 8);
@@ -170,8 +169,8 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256, BLOCK ? 1 : 3) k_rms_fwd(c
     pdl_wait();
     pdl_trigger();
     const Span mx = a.x.span(), mr = RS ? a.res.span() : mx;
-    Raw8<XS> nx[E];
-    Raw8<RW> nr[RS ? E : 1];
+    Raw8<XS, AL> nx[E];
+    Raw8<RW, AL> nr[RS ? E : 1];
     auto ask = [&](long long row) {
 #pragma unroll
         for (int k = 0; k < E; ++k) {
@@ -179,9 +178,10 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256, BLOCK ? 1 : 3) k_rms_fwd(c
             if (RS) a.res.ask(row, (k * G + t) * 8, mr, nr[RS ? k : 0], a.status);
         }
     };
-    ask(r);
+    if (AHEAD) ask(r);
     int slot = 0;
     for (; r < a.rows; r += step) {
+        if (!AHEAD) ask(r);
         float v[E][8], sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < E; ++k) {
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256, BLOCK ? 1 : 3) k_rms_fwd(c
                 for (int j = 0; j < 8; ++j) v[k][j] = RS == 2 ? round_to(v[k][j] + e[j], SADMM_BF16) : v[k][j] + e[j];
             }
         }
-        ask(r + step);
+        if (AHEAD) ask(r + step);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
             if (RS && a.h.p) a.h.store(r, (k * G + t) * 8, v[k], a.status);
@@ -245,178 +245,15 @@ __global__ void __launch_bounds__(1024) k_rms_fwd_long(const FwdArgs a)
     }
 }
 
-struct BwdArgs {
-    Rows h, dy, dres, dx;
-    const float* gamma;
-    const float* rstd;
-    float* part;          // [blocks][cols] partial dgamma; NULL: not wanted
-    long long rows;
-    int cols;
-    float inv_n;
-    int* status;
-};
-
-SADMM_DEV void load_gamma(const BwdArgs& a, int c, float (&g)[8])
-{
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = !a.gamma ? 1.0f : c + j < a.cols ? a.gamma[c + j] : 0.0f;
-}
-
-// A block takes rows blockIdx.x, + gridDim.x, ...: its threads own eight columns, add up
-// their shares of dgamma in registers and leave one partial sum a block.  The next
-// row's words are asked for before this one's are added up.  HS, YS: bytes of an
-// element of h and of dy; AL: rows start on 16-byte boundaries.
-template <int HS, int YS, bool AL>
-__global__ void __launch_bounds__(1024, 1) k_rms_bwd(const BwdArgs a)
-{
-    __shared__ RowSums red;
-    clear(red);
-    __syncthreads();
-    pdl_wait();
-    pdl_trigger();
-    const int c = threadIdx.x * 8;
-    const Span mh = a.h.span(), my = a.dy.span(), md = a.dres.p ? a.dres.span() : mh;
-    float g[8], dg[8];
-    load_gamma(a, c, g);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) dg[j] = 0.0f;
-    Raw8<HS, AL> nh, nd;
-    Raw8<YS, AL> ny;
-    float next = 0.0f;
-    auto ask = [&](long long r) {
-        a.h.ask(r, c, mh, nh, a.status);
-        a.dy.ask(r, c, my, ny, a.status);
-        if (a.dres.p) a.dres.ask(r, c, md, nd, a.status);
-        if (r < a.rows) next = a.rstd[r];
-    };
-    ask(blockIdx.x);
-    int slot = 0;
-    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const float rstd = next;
-        float hv[8], dv[8], e[8], s = 0.0f;
-        a.h.take(r, c, mh, nh, hv);
-        a.dy.take(r, c, my, ny, dv);
-        if (a.dres.p) {
-            a.dres.take(r, c, md, nd, e);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = 0.0f;
-        }
-        ask(r + gridDim.x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            hv[j] *= rstd;
-            dg[j] += dv[j] * hv[j];
-            dv[j] *= g[j];
-            s += dv[j] * hv[j];
-        }
-        if (!a.dx.p) continue;
-        const float m = row_sum<true>(s, red, slot) * a.inv_n;
-        slot ^= 1;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = rstd * (dv[j] - hv[j] * m) + e[j];
-        a.dx.store(r, c, e, a.status);
-    }
-    if (!a.part) return;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (c + j < a.cols) a.part[(long long)blockIdx.x * a.cols + c + j] = dg[j];
-}
-
-// Rows of any length: dx, a block a row, read twice.
-__global__ void __launch_bounds__(1024) k_rms_bwd_long(const BwdArgs a)
-{
-    __shared__ RowSums red;
-    clear(red);
-    __syncthreads();
-    pdl_wait();
-    pdl_trigger();
-    const long long r = blockIdx.x;
-    const Span mh = a.h.span(), my = a.dy.span(), md = a.dres.p ? a.dres.span() : mh;
-    const float rstd = a.rstd[r];
-    float s = 0.0f;
-    for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
-        float h[8], d[8], g[8];
-        a.h.load(r, c, mh, h, a.status);
-        a.dy.load(r, c, my, d, a.status);
-        load_gamma(a, c, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s += d[j] * g[j] * (h[j] * rstd);
-    }
-    const float m = row_sum<true>(s, red, 0) * a.inv_n;
-    for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
-        float h[8], d[8], g[8], e[8];
-        a.h.load(r, c, mh, h, a.status);
-        a.dy.load(r, c, my, d, a.status);
-        load_gamma(a, c, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = 0.0f;
-        if (a.dres.p) a.dres.load(r, c, md, e, a.status);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = rstd * (d[j] * g[j] - h[j] * rstd * m) + e[j];
-        a.dx.store(r, c, e, a.status);
-    }
-}
-
-// Rows of any length: partial dgamma of 2048 columns over the rows blockIdx.y,
-// blockIdx.y + gridDim.y, ...
-__global__ void __launch_bounds__(256) k_rms_cols_long(const BwdArgs a)
-{
-    pdl_wait();
-    pdl_trigger();
-    const Span mh = a.h.span(), my = a.dy.span();
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (c >= a.cols) return;
-    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (long long r = blockIdx.y; r < a.rows; r += gridDim.y) {
-        float h[8], d[8];
-        a.h.load(r, c, mh, h, a.status);
-        a.dy.load(r, c, my, d, a.status);
-        const float rstd = a.rstd[r];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] += d[j] * (h[j] * rstd);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (c + j < a.cols) a.part[(long long)blockIdx.y * a.cols + c + j] = s[j];
-}
-
-// out[c] = the sum of part[0 .. parts-1][c]: 32 groups of parts, then the groups in order.
-__global__ void __launch_bounds__(1024) k_rms_sums(const float* __restrict__ part, float* __restrict__ out, int cols,
-                                                   int parts)
-{
-    __shared__ float red[32][33];
-    pdl_wait();
-    pdl_trigger();
-    const int g = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c = blockIdx.x * 32 + lane;
-    float v = 0.0f;
-    if (c < cols) {
-#pragma unroll 16
-        for (int k = g; k < parts; k += 32) v += part[(size_t)k * cols + c];
-    }
-    red[g][lane] = v;
-    __syncthreads();
-    v = warp_sum(red[lane][g]);
-    if (lane == 0 && blockIdx.x * 32 + g < cols) out[blockIdx.x * 32 + g] = v;
-}
-
 // -------------------------------------------------------------------- host --
 
 constexpr int kWarpCols = 512;          // up to here a warp takes a row
 constexpr int kFwdCols = 32768;         // up to here a row stays in registers (1024 threads of 32)
-constexpr int kBwdCols = 8192;          // backward: 1024 threads of 8
 
 int row_threads(int cols, int e) { return (int)round_up((cols + 8 * e - 1) / (8 * e), 32); }
 
 // Blocks of n threads of 64 registers an SM holds.
 int per_sm(int n) { return n > 512 ? 1 : 1024 / n < 8 ? 1024 / n : 8; }
-
-int bwd_blocks(long long rows, int cols)
-{
-    const long long most = (long long)per_sm(cols <= kBwdCols ? row_threads(cols, 1) : 512) * device_sm_count();
-    return (int)(rows < most ? rows : most);
-}
 
 Rows rows_of(const void* p, long long ld, int dt, long long rows, int cols)
 {
@@ -424,21 +261,27 @@ Rows rows_of(const void* p, long long ld, int dt, long long rows, int cols)
     return {p, ld, rows, dt, cols, ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * es)) & 15) == 0};
 }
 
-template <int XS, int RS, bool BLOCK, int E>
+template <int XS, int RS, bool AL, bool BLOCK, int E>
 cudaError_t fwd(const FwdArgs& a, cudaStream_t s)
 {
     const int threads = BLOCK ? row_threads(a.cols, E) : 256;
     const long long want = BLOCK ? a.rows : (a.rows + 7) / 8, most = (long long)per_sm(threads) * device_sm_count();
-    return launch_pdl(k_rms_fwd<XS, RS, BLOCK, E>, dim3((unsigned)(want < most ? want : most)), dim3(threads), 0, s, a);
+    return launch_pdl(k_rms_fwd<XS, RS, BLOCK, E, AL>, dim3((unsigned)(want < most ? want : most)), dim3(threads), 0, s, a);
+}
+
+template <int XS, int RS, bool AL>
+cudaError_t fwd(const FwdArgs& a, cudaStream_t s)
+{
+    if (a.cols <= 256) return fwd<XS, RS, AL, false, 1>(a, s);
+    if (a.cols <= kWarpCols) return fwd<XS, RS, AL, false, 2>(a, s);
+    if (a.cols <= 8192) return fwd<XS, RS, AL, true, 2>(a, s);
+    return fwd<XS, RS, AL, true, 4>(a, s);
 }
 
 template <int XS, int RS>
 cudaError_t fwd(const FwdArgs& a, cudaStream_t s)
 {
-    if (a.cols <= 256) return fwd<XS, RS, false, 1>(a, s);
-    if (a.cols <= kWarpCols) return fwd<XS, RS, false, 2>(a, s);
-    if (a.cols <= 8192) return fwd<XS, RS, true, 1>(a, s);
-    return fwd<XS, RS, true, 4>(a, s);
+    return a.x.aligned && (!RS || a.res.aligned) ? fwd<XS, RS, true>(a, s) : fwd<XS, RS, false>(a, s);
 }
 
 }  // namespace
@@ -467,51 +310,6 @@ sadmm_status launch_rmsnorm_fwd(const sadmm_rmsnorm_fwd_args& a, cudaStream_t s)
         err = rs == 0 ? fwd<2, 0>(f, s) : rs == 2 ? fwd<2, 2>(f, s) : fwd<2, 4>(f, s);
     else
         err = rs == 0 ? fwd<4, 0>(f, s) : rs == 2 ? fwd<4, 2>(f, s) : fwd<4, 4>(f, s);
-    return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
-}
-
-size_t rmsnorm_bwd_bytes(const sadmm_rmsnorm_bwd_args& a)
-{
-    return a.dgamma ? (size_t)bwd_blocks(a.rows, a.cols) * (size_t)a.cols * 4 : 0;
-}
-
-sadmm_status launch_rmsnorm_bwd(const sadmm_rmsnorm_bwd_args& a, void* ws, cudaStream_t s)
-{
-    if (a.rows == 0) {
-        if (a.dgamma && cudaMemsetAsync(a.dgamma, 0, (size_t)a.cols * 4, s) != cudaSuccess) return SADMM_ECUDA;
-        return SADMM_OK;
-    }
-    BwdArgs b = {};
-    b.h = rows_of(a.h, a.ldh, a.hdt, a.rows, a.cols);
-    b.dy = rows_of(a.dy, a.lddy, a.dydt, a.rows, a.cols);
-    b.dres = rows_of(a.dres, a.lddres, a.hdt, a.rows, a.cols);
-    b.dx = rows_of(a.dx, a.lddx, a.hdt, a.rows, a.cols);
-    b.gamma = a.gamma;
-    b.rstd = a.rstd;
-    b.part = a.dgamma ? static_cast<float*>(ws) : nullptr;
-    b.rows = a.rows;
-    b.cols = a.cols;
-    b.inv_n = (float)(1.0 / a.cols);
-    b.status = device_status_ptr();
-    const int blocks = bwd_blocks(a.rows, a.cols);
-    cudaError_t err = cudaSuccess;
-    if (a.cols <= kBwdCols) {
-        const int hs = a.hdt == SADMM_BF16 ? 2 : 4, ys = a.dydt == SADMM_BF16 ? 2 : 4;
-        const bool al = b.h.aligned && b.dy.aligned && (!b.dres.p || b.dres.aligned);
-        auto kern = al ? (hs == 2 ? (ys == 2 ? k_rms_bwd<2, 2, true> : k_rms_bwd<2, 4, true>)
-                                  : (ys == 2 ? k_rms_bwd<4, 2, true> : k_rms_bwd<4, 4, true>))
-                       : (hs == 2 ? (ys == 2 ? k_rms_bwd<2, 2, false> : k_rms_bwd<2, 4, false>)
-                                  : (ys == 2 ? k_rms_bwd<4, 2, false> : k_rms_bwd<4, 4, false>));
-        err = launch_pdl(kern, dim3(blocks), dim3(row_threads(a.cols, 1)), 0, s, b);
-    } else {
-        if (a.dx) err = launch_pdl(k_rms_bwd_long, dim3((unsigned)a.rows), dim3(1024), 0, s, b);
-        if (err == cudaSuccess && b.part)
-            err = launch_pdl(k_rms_cols_long, dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)blocks), dim3(256), 0,
-                             s, b);
-    }
-    if (err == cudaSuccess && b.part)
-        err = launch_pdl(k_rms_sums, dim3((unsigned)((a.cols + 31) / 32)), dim3(1024), 0, s, b.part, a.dgamma, a.cols,
-                         blocks);
     return err == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
 }
 
