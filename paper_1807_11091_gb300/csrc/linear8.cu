@@ -136,8 +136,9 @@ bool zero(float* p, long long n, cudaStream_t s) { return !p || cudaMemsetAsync(
 // Whether the columns' operand (of a summand) has scales of single rows.
 bool row_scales(const Q8Problem& t) { return t.b[0].shift == 0 || (t.mode != kTgSingle && t.b[1].shift == 0); }
 
-// Whether CTA pairs take a product.
-bool by_pairs(const Q8Problem& t) { return t.m > 128; }
+// Whether CTA pairs take a product: where they are expected to be faster (8192 -> 2048 of 512 tokens:
+// 32 us by pairs, 25 by single tiles; 4096 -> 16384 of 129: 21 and 47).
+bool by_pairs(const Q8Problem& t) { return time_q8_pair(t) < time_q8_product(t); }
 
 // Products of one call: by CTA pairs, neighbours of one kind in one launch, or by
 // single tiles.

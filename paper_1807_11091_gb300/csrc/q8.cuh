@@ -42,8 +42,12 @@ inline bool q8_aligned(const void* p, long long ld)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 15) == 0;
 }
 
-sadmm_status launch_q8_product(const Q8Problem& t, cudaStream_t s);                  // q8gemm.cu
-sadmm_status launch_q8_pair(const Q8Problem* t, int count, cudaStream_t s);          // q8pair.cu
+// One tile a CTA (q8gemm.cu), or up to three products by CTA pairs (q8pair.cu), and the times
+// they are expected to take.
+sadmm_status launch_q8_product(const Q8Problem& t, cudaStream_t s);
+long long time_q8_product(const Q8Problem& t);
+sadmm_status launch_q8_pair(const Q8Problem* t, int count, cudaStream_t s);
+long long time_q8_pair(const Q8Problem& t);
 
 // Matrices in 8 bits (quant.cu).  What is made 8-bit: x; dy act'(z) (z given); or
 // the gated pair's dg and du (u given), whose outputs are [0] and [1].  sums: column

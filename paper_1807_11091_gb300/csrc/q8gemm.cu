@@ -122,7 +122,9 @@ SADMM_DEV void finish4(const Args& a, long long r, long long c, float (&v)[4], f
     }
 }
 
-template <bool GATED, int BN>
+// PROWS: P's scales are single rows'; else one for the tile, which then goes into the other
+// side's and saves a product an element.
+template <bool GATED, int BN, bool PROWS>
 __global__ void __launch_bounds__(kThreads, 1) k_q8_tiles(const __grid_constant__ Maps maps, const __grid_constant__ Args a)
 {
     constexpr int H = GATED ? 2 : 1;
@@ -133,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_q8_tiles(const __grid_constant_
     __shared__ uint64_t full[kMostStages], empty[kMostStages], acc_full[NB], acc_empty[NB];
     __shared__ uint32_t tmem_holder;
     __shared__ volatile int abort_flag;
-    __shared__ __align__(16) float s_q[4][BN];  // a warp's own copy of the rows' scales
+    __shared__ __align__(16) float s_q[4][PROWS ? 1 : H][BN];  // a warp's own copy of the rows' scales
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)a.splits);
     const long long tile = blockIdx.x / (unsigned)a.splits;
@@ -211,38 +213,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_q8_tiles(const __grid_constant_
         const int q = warp & 3;
         const uint32_t taddr = tmem + ((uint32_t)(q * 32) << 16);
         const long long prow = p0 + q * 32 + lane;
-        float* sq = s_q[warp - 2];
+        float (&sq)[PROWS ? 1 : H][BN] = s_q[warp - 2];
         float acc[H][BN];
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int j = 0; j < BN; ++j) acc[h][j] = 0.0f;
-        constexpr int SQ = (BN + 31) / 32;
-        float nq[SQ], np[H];
-        auto fetch = [&](int k) {
+        // the scales of the next blocks are on their way in registers, AHEAD of them (with one, each block waited for
+        // its own: 1.2 us a block)
+        constexpr int SQ = (BN + 31) / 32, AHEAD = 4;
+        float nq[AHEAD][SQ], np[AHEAD][H];
+        auto fetch = [&](int k, float (&q)[SQ], float (&p)[H]) {
+            if (k >= k1) return;
             const int second = a.sum && k >= a.nk0;
             const int b = second ? k - a.nk0 : k;
 #pragma unroll
             for (int i = 0; i < SQ; ++i) {
                 const int j = i * 32 + lane;
-                nq[i] = j < BN ? a.qs[second].at(q0 + j, b) : 0.0f;
+                q[i] = j < BN ? a.qs[second].at(q0 + j, b) : 0.0f;
             }
 #pragma unroll
-            for (int h = 0; h < H; ++h) np[h] = a.ps[GATED ? h : second].at(prow, b);
+            for (int h = 0; h < H; ++h) p[h] = a.ps[GATED ? h : second].at(PROWS ? prow : p0, b);
         };
-        if (k0 < k1) fetch(k0);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch(k0 + i, nq[i], np[i]);
         int buf = 0;
         uint32_t bphase = 0;
         for (int k = k0; k < k1; ++k) {
             __syncwarp();  // the last block's scales have been read
 #pragma unroll
             for (int i = 0; i < SQ; ++i)
-                if (i * 32 + lane < BN) sq[i * 32 + lane] = nq[i];
+                if (i * 32 + lane < BN) {
+#pragma unroll
+                    for (int h = 0; h < (PROWS ? 1 : H); ++h) sq[h][i * 32 + lane] = PROWS ? nq[0][i] : nq[0][i] * np[0][h];
+                }
             float sp[H];
 #pragma unroll
-            for (int h = 0; h < H; ++h) sp[h] = np[h];
+            for (int h = 0; h < H; ++h) sp[h] = np[0][h];
             __syncwarp();
-            if (k + 1 < k1) fetch(k + 1);
+#pragma unroll
+            for (int d = 0; d + 1 < AHEAD; ++d) {
+#pragma unroll
+                for (int i = 0; i < SQ; ++i) nq[d][i] = nq[d + 1][i];
+#pragma unroll
+                for (int h = 0; h < H; ++h) np[d][h] = np[d + 1][h];
+            }
+            fetch(k + AHEAD, nq[AHEAD - 1], np[AHEAD - 1]);
             if (!mbar_wait_warp(&acc_full[buf], bphase, &abort_flag, a.status)) break;
             tc_fence_after();
 #pragma unroll
@@ -258,11 +274,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_q8_tiles(const __grid_constant_
                     tmem_ld_wait();
 #pragma unroll
                     for (int j = 0; j < CH; j += 4) {
-                        const float4 f = *reinterpret_cast<const float4*>(sq + c + j);
-                        acc[h][c + j] = fmaf(__uint_as_float(r[j]), sp[h] * f.x, acc[h][c + j]);
-                        acc[h][c + j + 1] = fmaf(__uint_as_float(r[j + 1]), sp[h] * f.y, acc[h][c + j + 1]);
-                        acc[h][c + j + 2] = fmaf(__uint_as_float(r[j + 2]), sp[h] * f.z, acc[h][c + j + 2]);
-                        acc[h][c + j + 3] = fmaf(__uint_as_float(r[j + 3]), sp[h] * f.w, acc[h][c + j + 3]);
+                        float4 f = *reinterpret_cast<const float4*>(sq[PROWS ? 0 : h] + c + j);
+                        if (PROWS) f.x *= sp[h], f.y *= sp[h], f.z *= sp[h], f.w *= sp[h];
+                        acc[h][c + j] = fmaf(__uint_as_float(r[j]), f.x, acc[h][c + j]);
+                        acc[h][c + j + 1] = fmaf(__uint_as_float(r[j + 1]), f.y, acc[h][c + j + 1]);
+                        acc[h][c + j + 2] = fmaf(__uint_as_float(r[j + 2]), f.z, acc[h][c + j + 2]);
+                        acc[h][c + j + 3] = fmaf(__uint_as_float(r[j + 3]), f.w, acc[h][c + j + 3]);
                     }
                 }
             }
@@ -284,18 +301,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_q8_tiles(const __grid_constant_
     // the cluster's CTAs finish the tile's rows in turn
     const int rows = (int)min((long long)BN, a.m - q0);
     for (int j = rank * (kThreads / 32) + warp; j < rows; j += a.splits * (kThreads / 32)) {
-        float v[2][4];
+        float v[2][4], e[H][8][4];
+        // all of them on their way before the first is added
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const uint32_t at = smem_u32(smem) + (uint32_t)((h * BN + j) * kPRows + lane * 4) * 4u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < a.splits) ld_cluster<4>(map_rank(at, (uint32_t)i), e[h][i]);
+        }
 #pragma unroll
         for (int h = 0; h < H; ++h) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[h][i] = 0.0f;
-            const uint32_t at = smem_u32(smem) + (uint32_t)((h * BN + j) * kPRows + lane * 4) * 4u;
-            for (int i = 0; i < a.splits; ++i) {
-                float e[4];
-                ld_cluster<4>(map_rank(at, (uint32_t)i), e);
+            for (int l = 0; l < 4; ++l) v[h][l] = e[h][0][l];
 #pragma unroll
-                for (int l = 0; l < 4; ++l) v[h][l] += e[l];
-            }
+            for (int i = 1; i < 8; ++i)
+                if (i < a.splits) {
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) v[h][l] += e[h][i][l];
+                }
         }
         finish4<GATED>(a, q0 + j, p0 + lane * 4, v[0], v[1]);
     }
@@ -322,7 +346,58 @@ bool encode8(CUtensorMap* map, const Q8Operand& o, int box_rows)
 
 Scales scales_of(const Q8Operand& o) { return {o.s, o.s_row, o.s_block, o.rows, o.shift}; }
 
-template <bool GATED, int BN>
+// Clusters of n CTAs of this kernel's kind that the device holds at once, one CTA an SM (a GPC's SMs
+// are no multiple of eight: of 128 CTAs in clusters of eight the last ones waited, 11.7 us where
+// clusters of four take 7.8).
+int clusters_at_once(int n)
+{
+    static int known[64][9];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (!known[dev][n]) {
+        auto kern = k_q8_tiles<false, 128, false>;
+        constexpr int smem = kStageSmem + 1024;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)n;
+        attr.val.clusterDim.y = 1;
+        attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)n);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int most = 0;
+        if (cudaOccupancyMaxActiveClusters(&most, kern, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            most = device_sm_count() / (2 * n);
+        }
+        known[dev][n] = most > 0 ? most : 1;
+    }
+    return known[dev][n];
+}
+
+// CTAs that share a tile's contraction: as many as run at once (eight at most), none
+// of them without a block.
+int split_of(long long tiles, int nk)
+{
+    int n = nk < 8 ? nk : 8;
+    while (n > 1 && tiles > clusters_at_once(n)) --n;
+    const int steps = (nk + n - 1) / n;
+    return (nk + steps - 1) / steps;
+}
+
+// Output rows of a tile.
+int rows_of_tile(const Q8Problem& t)
+{
+    if (t.m <= 16) return 16;
+    if (t.m <= 32) return 32;
+    return t.m <= 64 || t.mode == kTgGated ? 64 : 128;
+}
+
+template <bool GATED, int BN, bool PROWS>
 sadmm_status run(const Q8Problem& t, Args a, cudaStream_t s)
 {
     constexpr int H = GATED ? 2 : 1;
@@ -330,7 +405,7 @@ sadmm_status run(const Q8Problem& t, Args a, cudaStream_t s)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
     constexpr int smem = kStageSmem + 1024;
-    auto kern = k_q8_tiles<GATED, BN>;
+    auto kern = k_q8_tiles<GATED, BN, PROWS>;
     if (!configured[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
             return SADMM_ECUDA;
@@ -352,8 +427,7 @@ sadmm_status run(const Q8Problem& t, Args a, cudaStream_t s)
     a.idesc = idesc_e4m3(kPRows, BN);
     a.p_tiles = (int)((t.n + kPRows - 1) / kPRows);
     const long long tiles = a.p_tiles * ((t.m + BN - 1) / BN);
-    a.splits = 1;
-    while (a.splits < 8 && tiles * a.splits * 2 <= device_sm_count() && a.splits * 2 <= a.nk) a.splits *= 2;
+    a.splits = split_of(tiles, a.nk);
     a.steps = (a.nk + a.splits - 1) / a.splits;
     if (tiles * a.splits > 0x7fffffffll) return SADMM_EUNSUPPORTED;
     cudaLaunchAttribute attr[2];
@@ -371,6 +445,13 @@ sadmm_status run(const Q8Problem& t, Args a, cudaStream_t s)
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kern, maps, a) == cudaSuccess ? SADMM_OK : SADMM_ECUDA;
+}
+
+template <bool GATED, int BN>
+sadmm_status run(const Q8Problem& t, const Args& a, cudaStream_t s)
+{
+    const bool rows = t.b[0].shift == 0 || (t.mode != kTgSingle && t.b[1].shift == 0);
+    return rows ? run<GATED, BN, true>(t, a, s) : run<GATED, BN, false>(t, a, s);
 }
 
 }  // namespace
@@ -393,15 +474,29 @@ sadmm_status launch_q8_product(const Q8Problem& t, cudaStream_t s)
     a.bias2 = t.bias2;
     a.act = act_for(t.act, t.y.p && t.y.dt == SADMM_BF16);
     a.status = device_status_ptr();
+    const int bn = rows_of_tile(t);
     if (t.mode == kTgGated) {
-        if (t.m <= 16) return run<true, 16>(t, a, s);
-        if (t.m <= 32) return run<true, 32>(t, a, s);
-        return run<true, 64>(t, a, s);
+        if (bn == 16) return run<true, 16>(t, a, s);
+        return bn == 32 ? run<true, 32>(t, a, s) : run<true, 64>(t, a, s);
     }
-    if (t.m <= 16) return run<false, 16>(t, a, s);
-    if (t.m <= 32) return run<false, 32>(t, a, s);
-    if (t.m <= 64) return run<false, 64>(t, a, s);
-    return run<false, 128>(t, a, s);
+    if (bn == 16) return run<false, 16>(t, a, s);
+    if (bn == 32) return run<false, 32>(t, a, s);
+    return bn == 64 ? run<false, 64>(t, a, s) : run<false, 128>(t, a, s);
+}
+
+// Expected time, ns.  Measured: a block takes 0.20 us on tiles of 16 rows, 0.25 on 32, 0.33 on
+// 64, 0.56 on 128 (the gated pair's 0.27, 0.45, 0.70); a round of tiles 3.5 beside its blocks,
+// a launch 4, the join of a split contraction 2.
+long long time_q8_product(const Q8Problem& t)
+{
+    const bool gated = t.mode == kTgGated;
+    const int bn = rows_of_tile(t);
+    const int nk = (int)((t.a[0].k + kQBlock - 1) / kQBlock) + (t.mode == kTgSum ? (int)((t.a[1].k + kQBlock - 1) / kQBlock) : 0);
+    const long long tiles = (t.n + kPRows - 1) / kPRows * ((t.m + bn - 1) / bn);
+    const int splits = split_of(tiles, nk), steps = (nk + splits - 1) / splits;
+    const long long rounds = (tiles * splits + device_sm_count() - 1) / device_sm_count();
+    const long long block = bn == 16 ? (gated ? 270 : 200) : bn == 32 ? (gated ? 450 : 250) : bn == 64 ? (gated ? 700 : 330) : 560;
+    return rounds * (steps * block + 3500) + 4000 + (splits > 1 ? 2000 : 0);
 }
 
 }  // namespace sadmm
