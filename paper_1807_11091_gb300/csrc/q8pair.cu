@@ -30,10 +30,11 @@ struct Regs {
     static constexpr int few = VEC ? 56 : 40, many = VEC ? 224 : 232;
     static_assert(128 * few + 256 * many <= 384 * 168, "more registers than the block was launched with");
 };
-constexpr int kStages = 6;
+constexpr int kStages = 4;
 constexpr uint32_t kHalfBytes = 128 * kQBlock;        // 128 rows of one block
 constexpr uint32_t kStageBytes = 2 * kHalfBytes;
 constexpr int kProducts = 3;
+constexpr int kBoxBytes = 4096;                       // 32 output rows of 128 bytes on their way out; two a warp
 constexpr int kSlots = 3;                             // places of the ring of scales, four blocks each:
 constexpr int kColumns = 4 * 128;                     // [row][block], then [block][column], or where all columns of a
 constexpr int kSlotFloats = kColumns + 4 * 256;       // half (of a weight) have one scale [half][block]
@@ -49,16 +50,18 @@ struct Product {
     Scales ps[2], qs[2];   // of both summands; gated: qs of Wg and Wu
     int sum;
     int pm, qm;            // maps; the second summand's (gated: Wu's) follow
+    int ym;                // map of y, -1: its rows do not start on 16-byte boundaries
 };
 
 struct Maps {
-    CUtensorMap map[8];
+    CUtensorMap map[8 + kProducts + 2];
 };
 
 struct Args {
     Product prod[kProducts];
     TgArgs t;              // products, tiles, res, z, u, bias, bias2, act, status are used
     sadmm_q8_out y8;
+    int zm, um;            // maps of z and u, as ym
     uint32_t idesc;
 };
 
@@ -249,6 +252,57 @@ struct Ring {
     }
 };
 
+// A warp's two boxes of 32 rows x 128 bytes (64 bf16 or 32 fp32 columns) in shared memory, from
+// which the tensor-memory accelerator writes them out while the next tile is added up, and
+// leaves out what lies past the matrix.  (Stored by the threads themselves, 32 rows of 32
+// bytes at a time, a tile's output took 4.4 us.)
+struct Boxes {
+    uint8_t* mem;
+    int lane;
+    // Whether box b may be written again: all stores but the last `left` have been read.
+    template <int LEFT>
+    SADMM_DEV void free()
+    {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory");
+        __syncwarp();
+    }
+    // The lane's row: 16 values to the piece-th of four (bf16) or two (fp32) pieces of the box.
+    SADMM_DEV void put(int b, int piece, bool bf16, const float (&v)[16])
+    {
+        uint8_t* row = mem + b * kBoxBytes + lane * 128;
+        if (bf16) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<uint4*>(row + (((piece * 2 + h) ^ (lane & 7)) << 4)) =
+                    make_uint4(pack_bf16(v[8 * h], v[8 * h + 1]), pack_bf16(v[8 * h + 2], v[8 * h + 3]),
+                               pack_bf16(v[8 * h + 4], v[8 * h + 5]), pack_bf16(v[8 * h + 6], v[8 * h + 7]));
+        } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                *reinterpret_cast<float4*>(row + (((piece * 4 + h) ^ (lane & 7)) << 4)) =
+                    make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+        }
+    }
+    // Box b to columns c on, rows r on of the m x n matrix behind the map.
+    SADMM_DEV void send(int b, const CUtensorMap* map, long long c, long long r, long long n, long long m)
+    {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            if (c < n && r < m)
+                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map),
+                             "r"(smem_u32(mem + b * kBoxBytes)), "r"((int)c), "r"((int)r)
+                             : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
+    SADMM_DEV void finish()
+    {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
+};
+
 // v += bias of columns c .. c+15, the same for the whole warp.
 SADMM_DEV void add_bias16(const float* bias, long long c, long long n, float (&v)[16])
 {
@@ -266,7 +320,56 @@ SADMM_DEV void add_bias16(const float* bias, long long c, long long n, float (&v
     }
 }
 
-template <bool GATED, bool VEC>
+// The same in few instructions, where a group of a 16-byte word is inside the row or outside.
+SADMM_DEV void add_bias16_whole(const float* bias, long long c, long long n, float (&v)[16])
+{
+    if (!bias) return;
+#pragma unroll
+    for (int j = 0; j < 16; j += 4)
+        if (c + j < n) {
+            const float4 b = __ldg(reinterpret_cast<const float4*>(bias + c + j));
+            v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+        }
+}
+SADMM_DEV void add16_whole(const Out& o, long long r, long long c, long long n, float (&v)[16])
+{
+    if (o.bf16) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(o.p) + r * o.ld + c;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (c + 8 * h < n) {
+                const uint4 q = reinterpret_cast<const uint4*>(p)[h];
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[8 * h + 2 * j] += __uint_as_float(w[j] << 16);
+                    v[8 * h + 2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u);
+                }
+            }
+    } else {
+        const float* p = static_cast<const float*>(o.p) + r * o.ld + c;
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+            if (c + j < n) {
+                const float4 q = *reinterpret_cast<const float4*>(p + j);
+                v[j] += q.x; v[j + 1] += q.y; v[j + 2] += q.z; v[j + 3] += q.w;
+            }
+    }
+}
+SADMM_DEV void store16_whole(const Out& o, long long r, long long c, long long n, const float (&v)[16])
+{
+    uint4* p = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(o.p) + r * o.ld + c);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (c + 8 * h < n)
+            p[h] = make_uint4(pack_bf16(v[8 * h], v[8 * h + 1]), pack_bf16(v[8 * h + 2], v[8 * h + 3]),
+                              pack_bf16(v[8 * h + 4], v[8 * h + 5]), pack_bf16(v[8 * h + 6], v[8 * h + 7]));
+}
+
+// WHOLE: every output goes out by boxes or whole 16-byte words, bias and residual come by such.  The
+// general forms' instructions, most of them jumped over, do not stay in the SM: a tile's
+// output took 4.4 us with them and with GELU 9.
+template <bool GATED, bool VEC, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 1)
     k_q8_pair(const __grid_constant__ Maps maps, const __grid_constant__ Args a)
 {
@@ -417,6 +520,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         Place pl = place(a, t < 0 ? 0 : t);
         int slot_at = 0;
         uint32_t sphase = 0;
+        Boxes box = {smem + kStages * kStageBytes + kSlots * kSlotFloats * 4 + (warp - 4) * 2 * kBoxBytes, lane};
+        int turn = 0;
         for (int i = 0; t >= 0; ++i) {
             const Product& p = a.prod[pl.prod];
             const int nk = p.t.nk;
@@ -483,6 +588,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const long long row = (long long)done.mt * 256 + rank * 128 + q * 32 + lane;
             const long long col0 = GATED ? (long long)done.nt * 128 + part * 64 : (long long)done.nt * 256 + part * 128;
             const bool in = row < p.t.m;
+            const long long row0 = row - lane;
+            const bool y_bf16 = p.t.y.bf16, two = a.zm >= 0 || a.um >= 0;  // boxes that are filled together
             float top = 0.0f;
             // 16 (32) columns at a time in one loop, the sums moving up: unrolled, its instructions came
             // from memory every time (11 us a tile with GELU).  A gated pair's outputs take g's place until their scale is
@@ -497,11 +604,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                         float v[16], w[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] = acc[d * 16 + j], w[j] = GATED ? acc[64 + j] : 0.0f;
-                        add_bias16(a.t.bias, col, p.t.n, v);
-                        if (GATED) add_bias16(a.t.bias2, col, p.t.n, w);
-                        if (in && col < p.t.n) {
-                            if (GATED && a.t.u.p) store16(a.t.u, row, col, p.t.n, w, status);
-                            if (a.t.z.p) store16(a.t.z, row, col, p.t.n, v, status);
+                        if (WHOLE) {
+                            add_bias16_whole(a.t.bias, col, p.t.n, v);
+                            if (GATED) add_bias16_whole(a.t.bias2, col, p.t.n, w);
+                        } else {
+                            add_bias16(a.t.bias, col, p.t.n, v);
+                            if (GATED) add_bias16(a.t.bias2, col, p.t.n, w);
+                        }
+                        const int piece = (c + d) & 3;
+                        if (two && piece == 0) box.free<0>();
+                        if (GATED && a.um >= 0) {
+                            box.put(1, piece, true, w);
+                            if (piece == 3) box.send(1, &maps.map[a.um], col - 48, row0, p.t.n, p.t.m);
+                        } else if (!WHOLE && GATED && a.t.u.p && in && col < p.t.n) {
+                            store16(a.t.u, row, col, p.t.n, w, status);
+                        }
+                        if (a.zm >= 0) {
+                            box.put(0, piece, true, v);
+                            if (piece == 3) box.send(0, &maps.map[a.zm], col - 48, row0, p.t.n, p.t.m);
+                        } else if (!WHOLE && a.t.z.p && in && col < p.t.n) {
+                            store16(a.t.z, row, col, p.t.n, v, status);
                         }
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
@@ -514,9 +636,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 if (col + j < p.t.n) top = fmaxf(top, q8_size(v[j]));
                                 acc[j] = v[j];
                             }
-                        } else if (in && col < p.t.n) {
-                            if (a.t.res.p) add16(a.t.res, row, col, p.t.n, v, status);
-                            store16(p.t.y, row, col, p.t.n, v, status);
+                        } else {
+                            if (a.t.res.p && in && col < p.t.n) {
+                                if (WHOLE)
+                                    add16_whole(a.t.res, row, col, p.t.n, v);
+                                else
+                                    add16(a.t.res, row, col, p.t.n, v, status);
+                            }
+                            if (!GATED && (WHOLE || p.ym >= 0)) {
+                                const int last = y_bf16 ? 3 : 1, at = piece & last;
+                                if (at == 0) {
+                                    turn = two ? 1 : turn ^ 1;
+                                    if (!two) box.free<1>();
+                                    else if (piece) box.free<0>();
+                                }
+                                box.put(turn, at, y_bf16, v);
+                                if (at == last) box.send(turn, &maps.map[p.ym], col - 16 * last, row0, p.t.n, p.t.m);
+                            } else if (in && col < p.t.n) {
+                                if (WHOLE)
+                                    store16_whole(p.t.y, row, col, p.t.n, v);
+                                else
+                                    store16(p.t.y, row, col, p.t.n, v, status);
+                            }
                         }
                     }
                     if (GATED) {
@@ -560,8 +701,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                             w[j] = q8_four(q8_quotient(v[0], k), q8_quotient(v[1], k), q8_quotient(v[2], k),
                                            q8_quotient(v[3], k));
                         }
-                        if (wide && live >= c * 16 + 16) {
+                        if ((WHOLE || wide) && live >= c * 16 + 16) {
                             reinterpret_cast<uint4*>(out)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                        } else if (WHOLE) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                if (c * 16 + j < live) out[c * 16 + j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
                         } else {
                             store_bytes8(out + c * 16, live - c * 16, w[0], w[1]);
                             store_bytes8(out + c * 16 + 8, live - c * 16 - 8, w[2], w[3]);
@@ -570,6 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
+        box.finish();
     }
     tc_fence_before();
     __syncthreads();
@@ -596,16 +742,32 @@ bool encode8(CUtensorMap* map, const Q8Operand& o)
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// An output's map, of boxes of 128 bytes x 32 rows; false: it is stored by the threads.
+bool encode_out(CUtensorMap* map, const TgMatrix& t, long long m, long long n)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode_fn();
+    if (!t.p || !enc || !make_out(t, m, n).vec) return false;
+    const bool bf16 = t.dt == SADMM_BF16;
+    memset(map, 0, sizeof(*map));
+    const cuuint64_t gdim[2] = {(cuuint64_t)n, (cuuint64_t)m};
+    const cuuint64_t gstride[1] = {(cuuint64_t)t.ld * (bf16 ? 2 : 4)};
+    const cuuint32_t box[2] = {bf16 ? 64u : 32u, 32u};
+    const cuuint32_t estride[2] = {1u, 1u};
+    return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, t.p, gdim, gstride, box,
+               estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 Scales scales_of(const Q8Operand& o) { return {o.s, o.s_row, o.s_block, o.rows, o.shift}; }
 
-template <bool GATED, bool VEC>
+template <bool GATED, bool VEC, bool WHOLE>
 sadmm_status run(const Maps& maps, const Args& a, int ctas, cudaStream_t s)
 {
     static bool configured[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
-    constexpr int smem = kStages * (int)kStageBytes + kSlots * kSlotFloats * 4 + 1024;
-    auto kern = k_q8_pair<GATED, VEC>;
+    constexpr int smem = kStages * (int)kStageBytes + kSlots * kSlotFloats * 4 + 16 * kBoxBytes + 1024;
+    auto kern = k_q8_pair<GATED, VEC, WHOLE>;
     if (!configured[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
             return SADMM_ECUDA;
@@ -673,6 +835,7 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
         p.qm = next;
         for (int j = 0; j < nb; ++j)
             if (next >= 8 || !encode8(&maps.map[next++], q.b[j])) return SADMM_ECUDA;
+        p.ym = encode_out(&maps.map[8 + i], q.y, q.m, q.n) ? 8 + i : -1;
         for (int j = 0; j < 2; ++j) {
             p.ps[j] = scales_of(q.a[na == 2 ? j : 0]);
             p.qs[j] = scales_of(q.b[nb == 2 ? j : 0]);
@@ -688,13 +851,30 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     if (f.residual.p) a.t.res = make_out(f.residual, f.m, f.n);
     if (f.z.p) a.t.z = make_out(f.z, f.m, f.n);
     if (f.u.p) a.t.u = make_out(f.u, f.m, f.n);
+    a.zm = encode_out(&maps.map[8 + kProducts], f.z, f.m, f.n) ? 8 + kProducts : -1;
+    a.um = encode_out(&maps.map[9 + kProducts], f.u, f.m, f.n) ? 9 + kProducts : -1;
     a.t.status = device_status_ptr();
     a.y8 = f.y8;
     a.idesc = (1u << 4) | (256u >> 3) << 17 | (256u >> 4) << 24;  // e4m3 operands, fp32 sums, 256 x 256
     const long long pairs = device_sm_count() / 2;
     const int ctas = 2 * (int)(tiles < pairs ? tiles : pairs);
-    if (gated) return vec ? run<true, true>(maps, a, ctas, s) : run<true, false>(maps, a, ctas, s);
-    return vec ? run<false, true>(maps, a, ctas, s) : run<false, false>(maps, a, ctas, s);
+    const Out& y = a.prod[0].t.y;
+    const long long n = f.n;
+    auto words = [](const float* b) { return (reinterpret_cast<uintptr_t>(b) & 15) == 0; };
+    bool whole = (!a.t.z.p || a.zm >= 0) && (!a.t.u.p || a.um >= 0) && words(a.t.bias) && words(a.t.bias2);
+    if (a.t.bias || a.t.bias2) whole = whole && n % 4 == 0;
+    if (a.t.res.p) whole = whole && a.t.res.vec && n % (a.t.res.bf16 ? 8 : 4) == 0;
+    if (gated) whole = whole && (a.y8.q ? q8_aligned(a.y8.q, a.y8.ld) : y.vec && n % 8 == 0);
+    for (int i = 0; i < count && !gated; ++i) whole = whole && a.prod[i].ym >= 0;
+#ifdef SADMM_DEBUG
+    whole = false;  // the general forms check their indexes
+#endif
+    if (gated) {
+        if (whole) return vec ? run<true, true, true>(maps, a, ctas, s) : run<true, false, true>(maps, a, ctas, s);
+        return vec ? run<true, true, false>(maps, a, ctas, s) : run<true, false, false>(maps, a, ctas, s);
+    }
+    if (whole) return vec ? run<false, true, true>(maps, a, ctas, s) : run<false, false, true>(maps, a, ctas, s);
+    return vec ? run<false, true, false>(maps, a, ctas, s) : run<false, false, false>(maps, a, ctas, s);
 }
 
 // Expected time of a product by itself, ns.  Measured: a block takes 0.41 us, 0.86 where the
