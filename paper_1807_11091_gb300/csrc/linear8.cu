@@ -138,7 +138,10 @@ bool row_scales(const Q8Problem& t) { return t.b[0].shift == 0 || (t.mode != kTg
 
 // Whether CTA pairs take a product: where they are expected to be faster (8192 -> 2048 of 512 tokens:
 // 32 us by pairs, 25 by single tiles; 4096 -> 16384 of 129: 21 and 47).
-bool by_pairs(const Q8Problem& t) { return time_q8_pair(t) < time_q8_product(t); }
+bool by_pairs(const Q8Problem& t)
+{
+    return !(t.mode == kTgGated && row_scales(t)) && time_q8_pair(t) < time_q8_product(t);
+}
 
 // Products of one call: by CTA pairs, neighbours of one kind in one launch, or by
 // single tiles.

@@ -94,11 +94,23 @@ SADMM_DEV float q8_quotient(float x, const Q8Scale& k)
     const float q = __fmul_rn(x, k.r);
     return __fmaf_rn(__fmaf_rn(-q, k.s, x), k.r, q);
 }
-// What x counts for in its block's largest magnitude.
-SADMM_DEV float q8_size(float x)
+// The largest finite magnitude of N values (0: none), of which infinities become NaN, as
+// which they end anyway: the largest passes over a NaN by itself.
+template <int N>
+SADMM_DEV float q8_top(float (&v)[N])
 {
-    const float a = fabsf(x);
-    return a < __int_as_float(0x7f800000) ? a : 0.0f;
+    float t = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) t = fmaxf(t, fabsf(v[j]));
+    if (t == __int_as_float(0x7f800000)) {
+        t = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (fabsf(v[j]) == __int_as_float(0x7f800000)) v[j] = __int_as_float(0x7fffffff);
+            t = fmaxf(t, fabsf(v[j]));
+        }
+    }
+    return t;
 }
 SADMM_DEV uint32_t q8_two(float lo, float hi)
 {

@@ -69,6 +69,29 @@ constexpr uint32_t idesc_e4m3(int m, int n)
     return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+// Four neighbouring 8-bit columns; a warp has the 128 of a block.
+SADMM_DEV void put4(const Args& a, long long r, long long c, float (&v)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j >= a.n) v[j] = 0.0f;
+    float top = q8_top(v);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const Q8Scale k = q8_scale(top);
+    if (c >= a.n || !dbg_in(c, a.n, a.status) || !dbg_in(r, a.m, a.status)) return;
+    if ((threadIdx.x & 31) == 0) a.y8.s[r * a.y8.s_row + c / kQBlock * a.y8.s_block] = k.s;
+    const uint32_t q = q8_four(q8_quotient(v[0], k), q8_quotient(v[1], k), q8_quotient(v[2], k), q8_quotient(v[3], k));
+    uint8_t* p = static_cast<uint8_t*>(a.y8.q) + r * a.y8.ld + c;
+    if (c + 4 <= a.n && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
+        *reinterpret_cast<uint32_t*>(p) = q;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < a.n) p[j] = (uint8_t)(q >> (8 * j));
+    }
+}
+
 // Four neighbouring columns c .. c+3 of output row r; all lanes of a warp call it, a
 // warp one row's 128 columns.  v (and w, the pair's u) are the sums.
 template <bool GATED>
@@ -100,26 +123,7 @@ SADMM_DEV void finish4(const Args& a, long long r, long long c, float (&v)[4], f
         store_n<4>(a.y, r, c, a.n, v, a.status);
         return;
     }
-    float top = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (c + j >= a.n) v[j] = 0.0f;
-        top = fmaxf(top, q8_size(v[j]));
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const Q8Scale k = q8_scale(top);
-    if (c >= a.n || !dbg_in(c, a.n, a.status) || !dbg_in(r, a.m, a.status)) return;
-    if ((threadIdx.x & 31) == 0) a.y8.s[r * a.y8.s_row + c / kQBlock * a.y8.s_block] = k.s;
-    const uint32_t q = q8_four(q8_quotient(v[0], k), q8_quotient(v[1], k), q8_quotient(v[2], k), q8_quotient(v[3], k));
-    uint8_t* p = static_cast<uint8_t*>(a.y8.q) + r * a.y8.ld + c;
-    if (c + 4 <= a.n && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
-        *reinterpret_cast<uint32_t*>(p) = q;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < a.n) p[j] = (uint8_t)(q >> (8 * j));
-    }
+    if constexpr (GATED) put4(a, r, c, v);
 }
 
 // PROWS: P's scales are single rows'; else one for the tile, which then goes into the other

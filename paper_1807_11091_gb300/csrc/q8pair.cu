@@ -32,12 +32,21 @@ struct Regs {
 };
 constexpr int kStages = 4;
 constexpr uint32_t kHalfBytes = 128 * kQBlock;        // 128 rows of one block
-constexpr uint32_t kStageBytes = 2 * kHalfBytes;
+// A tile is 256 rows by 256 columns; with VEC (the columns' scales are single rows') 512 by 128, so
+// that a thread has two rows and a column's scale is read half as often.
+template <bool VEC>
+struct Tile {
+    static constexpr int rows = VEC ? 512 : 256, cols = VEC ? 128 : 256;
+    static constexpr uint32_t p_bytes = (VEC ? 2 : 1) * kHalfBytes;            // a CTA's part of a stage: of the rows,
+    static constexpr uint32_t bytes = p_bytes + (VEC ? kHalfBytes / 2 : kHalfBytes);  // and of the columns too
+    static constexpr int boxes = VEC ? 1 : 2;                                  // of a warp
+    // the ring of scales: [block][row of the CTA], then [block][column], or where 128 columns have one [half][block]
+    static constexpr int own = VEC ? 256 : 128, columns = 4 * own;
+};
 constexpr int kProducts = 3;
-constexpr int kBoxBytes = 4096;                       // 32 output rows of 128 bytes on their way out; two a warp
-constexpr int kSlots = 3;                             // places of the ring of scales, four blocks each:
-constexpr int kColumns = 4 * 128;                     // [row][block], then [block][column], or where all columns of a
-constexpr int kSlotFloats = kColumns + 4 * 256;       // half (of a weight) have one scale [half][block]
+constexpr int kBoxBytes = 4096;                       // 32 output rows of 128 bytes on their way out
+constexpr int kSlots = 3;                             // places of the ring of scales, four blocks each
+constexpr int kSlotFloats = 4 * 384;
 
 struct Scales {
     const float* s;
@@ -186,9 +195,11 @@ struct Ring {
     template <int N>
     SADMM_DEV bool fill(int k0, int k1, int nk, int at, int apart, int next, const Scales& c, long long r0)
     {
+        // (eight: the second four are 256 rows on)
+        auto row = [&](int j) { return j * 32 + (N == 8 && j >= 4 ? 128 : 0); };
         uint32_t in = 0;
 #pragma unroll
-        for (int j = 0; j < N; ++j) in |= (r0 + j * 32 < c.rows ? 1u : 0u) << j;
+        for (int j = 0; j < N; ++j) in |= (r0 + row(j) < c.rows ? 1u : 0u) << j;
         const float* from = c.s + ((in & 1u ? r0 : 0) >> c.shift) * c.s_row;
         const long long more = c.s_row * (c.shift ? 1 : 32);  // a scale further
         const long long step = c.s_block;
@@ -199,54 +210,36 @@ struct Ring {
             if (N > 1 || (threadIdx.x & 31) < 2) {
 #pragma unroll
                 for (int j = 0; j < N; ++j)
-                    cp_async4(to + j * apart, in >> j & 1u ? from + (j >> same) * more : from, in >> j & 1u);
+                    cp_async4(to + j * apart, in >> j & 1u ? from + (row(j) / 32 >> same) * more : from, in >> j & 1u);
             }
             from += step;
             done(k, nk);
         }
         return true;
     }
-    // The same for 256 neighbouring scales from row r0 on, which start on 16-byte boundaries: four a lane, twice.
-    SADMM_DEV bool fill_wide(int k0, int k1, int nk, const Scales& c, long long r0)
+    // Whether 128 scales from a multiple of 128 on are neighbours and start on a 16-byte boundary.
+    static SADMM_DEV bool wide(const Scales& c)
+    {
+        return c.shift == 0 && c.s_row == 1 && (c.s_block & 3) == 0 && (reinterpret_cast<uintptr_t>(c.s) & 15) == 0;
+    }
+    // The same for N times 128 such, 256 rows apart, from row r0 on: four a lane.  (One by one, two warps could not
+    // fetch the 384 of a block while its products run: 0.86 us a block.)
+    template <int N>
+    SADMM_DEV bool fill_wide(int k0, int k1, int nk, int at, int next, const Scales& c, long long r0)
     {
         const int lane = threadIdx.x & 31;
-        const long long left = c.rows - r0 - lane * 4;
-        const int b0 = (int)max(0ll, min(4ll, left)) * 4, b1 = (int)max(0ll, min(4ll, left - 128)) * 4;
-        const float* from = c.s + (b0 ? r0 + lane * 4 : 0);
+        int bytes[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) bytes[j] = (int)max(0ll, min(4ll, c.rows - r0 - j * 256 - lane * 4)) * 4;
+        const float* from = c.s + (bytes[0] ? r0 + lane * 4 : 0);
+        const long long step = c.s_block;
         for (int k = k0; k < k1; ++k) {
             if (!wait(k)) return false;
-            float* to = slot(k, 256) + kColumns + lane * 4;
-            cp_async16(to, from, b0);
-            cp_async16(to + 128, b1 ? from + 128 : from, b1);
-            from += c.s_block;
+            float* to = slot(k, next) + at + lane * 4;
+#pragma unroll
+            for (int j = 0; j < N; ++j) cp_async16(to + j * 128, bytes[j] ? from + j * 256 : from, bytes[j]);
+            from += step;
             done(k, nk);
-        }
-        return true;
-    }
-    // The 128 columns of either weight of a gated pair, from r0 on.
-    SADMM_DEV bool fill2(int k0, int k1, int nk, int at, const Scales (&c)[2], long long r0)
-    {
-        const float* from[2];
-        uint32_t in = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) in |= (r0 + j * 32 < c[0].rows ? 1u : 0u) << j;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) from[h] = c[h].s + ((in & 1u ? r0 : 0) >> c[h].shift) * c[h].s_row;
-        for (int k = k0; k < k1; ++k) {
-            if ((k & 3) == 0 && !mbar_wait_warp(&empty[s], phase ^ 1u, abort_flag, status)) return false;
-            float* slot = slots + s * kSlotFloats + at + (k & 3) * 256;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const long long more = c[h].shift ? 0 : c[h].s_row * 32;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    cp_async4(slot + h * 128 + j * 32, from[h] + (in >> j & 1u ? j * more : 0), in >> j & 1u);
-                from[h] += c[h].s_block;
-            }
-            if ((k & 3) == 3 || k + 1 == nk) {
-                cp_async_arrive(&full[s]);
-                if (++s == kSlots) { s = 0; phase ^= 1u; }
-            }
         }
         return true;
     }
@@ -375,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    constexpr uint32_t kStageBytes = Tile<VEC>::bytes;
     float* rings = reinterpret_cast<float*>(smem + kStages * kStageBytes);  // [kSlots][kSlotFloats]
     __shared__ uint64_t full[kStages], empty[kStages], s_full[kSlots], s_empty[kSlots], acc_full[2], acc_empty[2], drain, met[4];
     __shared__ uint32_t tmem_holder;
@@ -424,8 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0, t; ok && (t = tile_of(a, me, pairs, i)) >= 0; ++i) {
                 const Place pl = place(a, t);
                 const Product& p = a.prod[pl.prod];
-                const int row0 = pl.mt * 256 + (int)rank * 128;
-                const int col0 = GATED ? pl.nt * 128 : pl.nt * 256 + (int)rank * 128;
+                const int row0 = pl.mt * Tile<VEC>::rows + (int)rank * 128;
+                const int col0 = GATED ? pl.nt * 128 : pl.nt * Tile<VEC>::cols + (int)rank * (Tile<VEC>::cols / 2);
                 for (int k = 0; k < p.t.nk; ++k) {
                     if (!mbar_wait(&empty[s], phase ^ 1u, &abort_flag, status)) { ok = false; break; }
                     if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * kStageBytes);
@@ -434,7 +428,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int kc = (second ? k - p.t.nk0 : k) * kQBlock;
                     uint8_t* sp = smem + (size_t)s * kStageBytes;
                     tma_load_pair(sp, &maps.map[p.pm + second], bar, kc, row0);
-                    tma_load_pair(sp + kHalfBytes, &maps.map[p.qm + (GATED ? (int)rank : second)], bar, kc, col0);
+                    if (VEC) tma_load_pair(sp + kHalfBytes, &maps.map[p.pm + second], bar, kc, row0 + 256);
+                    tma_load_pair(sp + Tile<VEC>::p_bytes, &maps.map[p.qm + (GATED ? (int)rank : second)], bar, kc, col0);
                     if (++s == kStages) { s = 0; phase ^= 1u; }
                 }
             }
@@ -464,10 +459,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tc_fence_after();
                     const uint32_t st = smem_u32(smem + (size_t)s * kStageBytes);
-                    const uint64_t pd = sdesc_kmajor_sw128(st), qd = sdesc_kmajor_sw128(st + kHalfBytes);
-                    const uint32_t d = tmem + (uint32_t)buf * 256u;
+                    const uint64_t qd = sdesc_kmajor_sw128(st + Tile<VEC>::p_bytes);
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) mma_f8_pair_elect(d, pd + kk * 2, qd + kk * 2, a.idesc, kk != 0);
+                    for (int b = 0; b < (VEC ? 2 : 1); ++b) {
+                        const uint64_t pd = sdesc_kmajor_sw128(st + b * kHalfBytes);
+                        const uint32_t d = tmem + (uint32_t)(buf * 256 + b * 128);
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) mma_f8_pair_elect(d, pd + kk * 2, qd + kk * 2, a.idesc, kk != 0);
+                    }
                     commit_pair_elect(&empty[s]);
                     commit_pair_elect(&acc_full[buf]);
                     if (++s == kStages) { s = 0; phase ^= 1u; }
@@ -491,17 +490,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int second = 0; ok && second <= p.sum; ++second) {
                 const int k0 = second ? p.t.nk0 : 0, k1 = second || !p.sum ? p.t.nk : p.t.nk0;
                 const int nt = pl.nt, mt = pl.mt;
+                const Scales& cs = p.qs[second];
+                constexpr int own = Tile<VEC>::own;
                 if (warp == 2) {
-                    ok = ring.fill<4>(k0, k1, p.t.nk, lane * 4, 128, 1, p.ps[second], (long long)mt * 256 + rank * 128 + lane);
-                } else if (VEC && !GATED && p.qs[second].shift == 0 && p.qs[second].s_row == 1 && (p.qs[second].s_block & 3) == 0 &&
-                           (reinterpret_cast<uintptr_t>(p.qs[second].s) & 15) == 0) {
-                    ok = ring.fill_wide(k0, k1, p.t.nk, p.qs[second], (long long)nt * 256);
-                } else if (VEC && !GATED) {
-                    ok = ring.fill<8>(k0, k1, p.t.nk, kColumns + lane, 32, 256, p.qs[second], (long long)nt * 256 + lane);
+                    const Scales& rs = p.ps[second];
+                    const long long r0 = (long long)mt * Tile<VEC>::rows + rank * 128;
+                    ok = Ring::wide(rs) ? ring.fill_wide<own / 128>(k0, k1, p.t.nk, 0, own, rs, r0)
+                                        : ring.fill<own / 32>(k0, k1, p.t.nk, lane, 32, own, rs, r0 + lane);
                 } else if (VEC) {
-                    ok = ring.fill2(k0, k1, p.t.nk, kColumns + lane, p.qs, (long long)nt * 128 + lane);
+                    ok = Ring::wide(cs) ? ring.fill_wide<1>(k0, k1, p.t.nk, Tile<VEC>::columns, 128, cs, (long long)nt * 128)
+                                        : ring.fill<4>(k0, k1, p.t.nk, Tile<VEC>::columns + lane, 32, 128, cs,
+                                                       (long long)nt * 128 + lane);
                 } else {  // lane 0: the first 128 columns' (g's), lane 1: the others' (u's)
-                    ok = ring.fill<1>(k0, k1, p.t.nk, kColumns + lane * 4, 0, 1, p.qs[GATED ? lane & 1 : second],
+                    ok = ring.fill<1>(k0, k1, p.t.nk, Tile<VEC>::columns + lane * 4, 0, 1, p.qs[GATED ? lane & 1 : second],
                                       (long long)nt * (GATED ? 128 : 256) + (GATED ? 0 : (lane & 1) * 128));
                 }
             }
@@ -520,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         Place pl = place(a, t < 0 ? 0 : t);
         int slot_at = 0;
         uint32_t sphase = 0;
-        Boxes box = {smem + kStages * kStageBytes + kSlots * kSlotFloats * 4 + (warp - 4) * 2 * kBoxBytes, lane};
+        Boxes box = {smem + kStages * kStageBytes + kSlots * kSlotFloats * 4 + (warp - 4) * Tile<VEC>::boxes * kBoxBytes, lane};
         int turn = 0;
         for (int i = 0; t >= 0; ++i) {
             const Product& p = a.prod[pl.prod];
@@ -530,45 +531,60 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
             // the accumulator's columns of the thread's c-th 32
             auto column = [&](int c) { return GATED ? (c >> 1) * 128 + part * 64 + (c & 1) * 32 : part * 128 + c * 32; };
-            float4 rows = {}, cols = {}, cols2 = {};  // the scales of the next four blocks
             for (int k = 0; k < nk; ++k) {
                 const float* slot = rings + slot_at * kSlotFloats;
                 if ((k & 3) == 0) {
                     ok = mbar_wait_warp(&s_full[slot_at], sphase, &abort_flag, status);
                     if (!ok) break;
-                    rows = *reinterpret_cast<const float4*>(slot + (q * 32 + lane) * 4);
-                    cols = *reinterpret_cast<const float4*>(slot + kColumns + (GATED ? 0 : part * 4));
-                    if (GATED) cols2 = *reinterpret_cast<const float4*>(slot + kColumns + 4);
                 }
-                const float sp = rows.x, f0 = VEC ? 0.0f : sp * cols.x, f1 = GATED && !VEC ? sp * cols2.x : f0;
-                rows = make_float4(rows.y, rows.z, rows.w, 0.0f);
-                cols = make_float4(cols.y, cols.z, cols.w, 0.0f);
-                cols2 = make_float4(cols2.y, cols2.z, cols2.w, 0.0f);
+                // the scales of the thread's rows, and of the tile's columns
+                constexpr int R = VEC ? 2 : 1;
+                float sp[R], f0 = 0.0f, f1 = 0.0f;
+#pragma unroll
+                for (int b = 0; b < R; ++b) sp[b] = slot[(k & 3) * Tile<VEC>::own + b * 128 + q * 32 + lane];
+                if (!VEC) {
+                    f0 = sp[0] * slot[Tile<VEC>::columns + (GATED ? 0 : part * 4) + (k & 3)];
+                    f1 = GATED ? sp[0] * slot[Tile<VEC>::columns + 4 + (k & 3)] : f0;
+                }
                 ok = mbar_wait_warp(&acc_full[buf], bphase, &abort_flag, status);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t from = taddr + (uint32_t)buf * 256u;
+                auto read = [&]() {  // the accumulator has been read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_either(freed + (uint32_t)buf * 8u);
+                };
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    // (32 columns a load: of 16, their latencies take a fifth longer)
-                    uint32_t r[32];
-                    tmem_ld_32x32b_x32(from + column(c), r);
-                    tmem_ld_wait();
-                    if (c == 3) {  // the accumulator has been read
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_either(freed + (uint32_t)buf * 8u);
-                    }
                     if (VEC) {
+                        // 16 columns of both rows.  (Every thread reads every column's scale: 128 bytes of shared memory a
+                        // cycle, the bound of this form; of one row each 1024 cycles a block, 0.86 us.)
+                        uint32_t r[2][16];
+                        tmem_ld_32x32b_x16(from + part * 64 + c * 16, r[0]);
+                        tmem_ld_32x32b_x16(from + 128 + part * 64 + c * 16, r[1]);
+                        const float* column_scales = slot + Tile<VEC>::columns + (k & 3) * 128 + part * 64 + c * 16;
+                        tmem_ld_wait();
+                        if (c == 3) read();
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const float4 f = *reinterpret_cast<const float4*>(slot + kColumns + (k & 3) * 256 + column(c) + j);
-                            acc[c * 32 + j] = fmaf(__uint_as_float(r[j]), sp * f.x, acc[c * 32 + j]);
-                            acc[c * 32 + j + 1] = fmaf(__uint_as_float(r[j + 1]), sp * f.y, acc[c * 32 + j + 1]);
-                            acc[c * 32 + j + 2] = fmaf(__uint_as_float(r[j + 2]), sp * f.z, acc[c * 32 + j + 2]);
-                            acc[c * 32 + j + 3] = fmaf(__uint_as_float(r[j + 3]), sp * f.w, acc[c * 32 + j + 3]);
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 f = *reinterpret_cast<const float4*>(column_scales + j);
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                float* v = acc + b * 64 + c * 16 + j;
+                                const float s_ = sp[VEC ? b : 0];
+                                v[0] = fmaf(__uint_as_float(r[b][j]), s_ * f.x, v[0]);
+                                v[1] = fmaf(__uint_as_float(r[b][j + 1]), s_ * f.y, v[1]);
+                                v[2] = fmaf(__uint_as_float(r[b][j + 2]), s_ * f.z, v[2]);
+                                v[3] = fmaf(__uint_as_float(r[b][j + 3]), s_ * f.w, v[3]);
+                            }
                         }
                     } else {
+                        // (32 columns a load: of 16, their latencies take a fifth longer)
+                        uint32_t r[32];
+                        tmem_ld_32x32b_x32(from + column(c), r);
+                        tmem_ld_wait();
+                        if (c == 3) read();
                         const float f = c < 2 ? f0 : f1;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) acc[c * 32 + j] = fmaf(__uint_as_float(r[j]), f, acc[c * 32 + j]);
@@ -585,10 +601,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Place done = pl;
             t = tile_of(a, me, pairs, i + 1);
             if (t >= 0) pl = place(a, t);
-            const long long row = (long long)done.mt * 256 + rank * 128 + q * 32 + lane;
-            const long long col0 = GATED ? (long long)done.nt * 128 + part * 64 : (long long)done.nt * 256 + part * 128;
-            const bool in = row < p.t.m;
-            const long long row0 = row - lane;
+            const long long row1 = (long long)done.mt * Tile<VEC>::rows + rank * 128 + q * 32 + lane;
+            const long long col0 = (long long)done.nt * (GATED ? 128 : Tile<VEC>::cols) + part * (GATED || VEC ? 64 : 128);
             const bool y_bf16 = p.t.y.bf16, two = a.zm >= 0 || a.um >= 0;  // boxes that are filled together
             float top = 0.0f;
             // 16 (32) columns at a time in one loop, the sums moving up: unrolled, its instructions came
@@ -600,7 +614,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = 0; c < (GATED ? 4 : 8); c += D) {
 #pragma unroll
                     for (int d = 0; d < D; ++d) {
-                        const long long col = col0 + (c + d) * 16;
+                        const long long row = VEC ? row1 + (c >> 2) * 256 : row1, row0 = row - lane;
+                        const long long col = col0 + (VEC ? (c + d) & 3 : c + d) * 16;
+                        const bool in = row < p.t.m;
                         float v[16], w[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] = acc[d * 16 + j], w[j] = GATED ? acc[64 + j] : 0.0f;
@@ -632,10 +648,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         if (GATED && a.y8.q) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                if (col + j < p.t.n) top = fmaxf(top, q8_size(v[j]));
-                                acc[j] = v[j];
-                            }
+                            for (int j = 0; j < 16; ++j)
+                                if (col + j >= p.t.n) v[j] = 0.0f;
+                            top = fmaxf(top, q8_top(v));
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[j] = v[j];
                         } else {
                             if (a.t.res.p && in && col < p.t.n) {
                                 if (WHOLE)
@@ -646,9 +663,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (!GATED && (WHOLE || p.ym >= 0)) {
                                 const int last = y_bf16 ? 3 : 1, at = piece & last;
                                 if (at == 0) {
-                                    turn = two ? 1 : turn ^ 1;
-                                    if (!two) box.free<1>();
-                                    else if (piece) box.free<0>();
+                                    turn = VEC ? 0 : two ? 1 : turn ^ 1;
+                                    if (VEC || (two && piece)) box.free<0>();
+                                    else if (!two) box.free<1>();
                                 }
                                 box.put(turn, at, y_bf16, v);
                                 if (at == last) box.send(turn, &maps.map[p.ym], col - 16 * last, row0, p.t.n, p.t.m);
@@ -687,7 +704,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = mbar_wait_warp(&met[q], mphase, &abort_flag, status);
                 mphase ^= 1u;
                 if (!ok) break;
-                if (in && dbg_in(row, p.t.m, status)) {
+                const long long row = row1;
+                if (row < p.t.m && dbg_in(row, p.t.m, status)) {
                     if (part == 0) a.y8.s[row * a.y8.s_row + (long long)done.nt * a.y8.s_block] = k.s;
                     uint8_t* out = static_cast<uint8_t*>(a.y8.q) + row * a.y8.ld + col0;
                     const int live = (int)max(0ll, min(64ll, p.t.n - col0));
@@ -728,14 +746,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // -------------------------------------------------------------------- host --
 
-bool encode8(CUtensorMap* map, const Q8Operand& o)
+bool encode8(CUtensorMap* map, const Q8Operand& o, int box_rows)
 {
     PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode_fn();
     if (!enc) return false;
     memset(map, 0, sizeof(*map));
     const cuuint64_t gdim[2] = {(cuuint64_t)o.k, (cuuint64_t)o.rows};
     const cuuint64_t gstride[1] = {(cuuint64_t)o.ld};
-    const cuuint32_t box[2] = {(cuuint32_t)kQBlock, 128u};
+    const cuuint32_t box[2] = {(cuuint32_t)kQBlock, (cuuint32_t)box_rows};
     const cuuint32_t estride[2] = {1u, 1u};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(o.p), gdim, gstride, box, estride,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -766,7 +784,7 @@ sadmm_status run(const Maps& maps, const Args& a, int ctas, cudaStream_t s)
     static bool configured[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SADMM_ECUDA;
-    constexpr int smem = kStages * (int)kStageBytes + kSlots * kSlotFloats * 4 + 16 * kBoxBytes + 1024;
+    constexpr int smem = kStages * (int)Tile<VEC>::bytes + kSlots * kSlotFloats * 4 + 8 * Tile<VEC>::boxes * kBoxBytes + 1024;
     auto kern = k_q8_pair<GATED, VEC, WHOLE>;
     if (!configured[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
@@ -811,16 +829,19 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     memset(&a, 0, sizeof(a));
     const bool gated = t[0]->mode == kTgGated;
     bool vec = false;  // a product's columns have scales of single rows
+    for (int i = 0; i < count; ++i)
+        for (int j = 0; j < (t[i]->mode == kTgSingle ? 1 : 2); ++j) vec = vec || t[i]->b[j].shift == 0;
+    if (gated && vec) return SADMM_EUNSUPPORTED;  // (single tiles take those)
     long long tiles = 0;
     int next = 0;
     for (int i = 0; i < count; ++i) {
         Product& p = a.prod[i];
         const Q8Problem& q = *t[i];
-        const int cols = gated ? 128 : 256;
+        const int cols = gated || vec ? 128 : 256, rows = vec ? 512 : 256;
         p.t.m = q.m;
         p.t.n = q.n;
         if (q.y.p) p.t.y = make_out(q.y, q.m, q.n);
-        p.t.p_tiles = (int)((q.m + 255) / 256);
+        p.t.p_tiles = (int)((q.m + rows - 1) / rows);
         p.t.q_tiles = (int)((q.n + cols - 1) / cols);
         p.t.first = (int)tiles;
         tiles += (long long)p.t.p_tiles * p.t.q_tiles;
@@ -831,15 +852,14 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
         const int na = p.sum ? 2 : 1, nb = p.sum || gated ? 2 : 1;
         p.pm = next;
         for (int j = 0; j < na; ++j)
-            if (next >= 8 || !encode8(&maps.map[next++], q.a[j])) return SADMM_ECUDA;
+            if (next >= 8 || !encode8(&maps.map[next++], q.a[j], 128)) return SADMM_ECUDA;
         p.qm = next;
         for (int j = 0; j < nb; ++j)
-            if (next >= 8 || !encode8(&maps.map[next++], q.b[j])) return SADMM_ECUDA;
+            if (next >= 8 || !encode8(&maps.map[next++], q.b[j], vec ? 64 : 128)) return SADMM_ECUDA;
         p.ym = encode_out(&maps.map[8 + i], q.y, q.m, q.n) ? 8 + i : -1;
         for (int j = 0; j < 2; ++j) {
             p.ps[j] = scales_of(q.a[na == 2 ? j : 0]);
             p.qs[j] = scales_of(q.b[nb == 2 ? j : 0]);
-            vec = vec || p.qs[j].shift == 0;
         }
     }
     a.t.products = count;
@@ -851,11 +871,11 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     if (f.residual.p) a.t.res = make_out(f.residual, f.m, f.n);
     if (f.z.p) a.t.z = make_out(f.z, f.m, f.n);
     if (f.u.p) a.t.u = make_out(f.u, f.m, f.n);
-    a.zm = encode_out(&maps.map[8 + kProducts], f.z, f.m, f.n) ? 8 + kProducts : -1;
+    a.zm = !vec && encode_out(&maps.map[8 + kProducts], f.z, f.m, f.n) ? 8 + kProducts : -1;
     a.um = encode_out(&maps.map[9 + kProducts], f.u, f.m, f.n) ? 9 + kProducts : -1;
     a.t.status = device_status_ptr();
     a.y8 = f.y8;
-    a.idesc = (1u << 4) | (256u >> 3) << 17 | (256u >> 4) << 24;  // e4m3 operands, fp32 sums, 256 x 256
+    a.idesc = (1u << 4) | (vec ? 128u >> 3 : 256u >> 3) << 17 | (256u >> 4) << 24;  // e4m3 operands, fp32 sums
     const long long pairs = device_sm_count() / 2;
     const int ctas = 2 * (int)(tiles < pairs ? tiles : pairs);
     const Out& y = a.prod[0].t.y;
@@ -869,26 +889,24 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
 #ifdef SADMM_DEBUG
     whole = false;  // the general forms check their indexes
 #endif
-    if (gated) {
-        if (whole) return vec ? run<true, true, true>(maps, a, ctas, s) : run<true, false, true>(maps, a, ctas, s);
-        return vec ? run<true, true, false>(maps, a, ctas, s) : run<true, false, false>(maps, a, ctas, s);
-    }
+    if (gated) return whole ? run<true, false, true>(maps, a, ctas, s) : run<true, false, false>(maps, a, ctas, s);
     if (whole) return vec ? run<false, true, true>(maps, a, ctas, s) : run<false, false, true>(maps, a, ctas, s);
     return vec ? run<false, true, false>(maps, a, ctas, s) : run<false, false, false>(maps, a, ctas, s);
 }
 
-// Expected time of a product by itself, ns.  Measured: a block takes 0.41 us, 0.86 where the
+// Expected time of a product by itself, ns.  Measured: a block takes 0.41 us, 0.75 where the
 // columns have scales of single rows; a round of tiles 3.5 beside its blocks (where
 // an output's rows do not start on 16-byte boundaries 25 more: its elements are stored one by one,
 // 32 rows a store), a launch 4.
 long long time_q8_pair(const Q8Problem& t)
 {
     const bool rows = t.b[0].shift == 0 || (t.mode != kTgSingle && t.b[1].shift == 0);
-    const long long tiles = (t.m + 255) / 256 * ((t.n + (t.mode == kTgGated ? 127 : 255)) / (t.mode == kTgGated ? 128 : 256));
+    const int tall = rows ? 512 : 256, wide = rows || t.mode == kTgGated ? 128 : 256;
+    const long long tiles = (t.m + tall - 1) / tall * ((t.n + wide - 1) / wide);
     const long long pairs = device_sm_count() / 2, rounds = (tiles + pairs - 1) / pairs;
     bool apart = false;
     for (const TgMatrix* m : {&t.y, &t.residual, &t.z, &t.u}) apart = apart || (m->p && !make_out(*m, t.m, t.n).vec);
-    return rounds * (blocks_of(t) * (rows ? 860 : 410) + 3500 + (apart ? 25000 : 0)) + 4000;
+    return rounds * (blocks_of(t) * (rows ? 750 : 410) + 3500 + (apart ? 25000 : 0)) + 4000;
 }
 
 }  // namespace sadmm

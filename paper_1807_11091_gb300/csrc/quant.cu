@@ -130,10 +130,7 @@ __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
 #pragma unroll
     for (int i = 0; i < kRowSteps; ++i) {
         const long long b = cg * kRowSteps + i, c = b * kQBlock + lane * 8;
-        float top = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, q8_size(v[i][j]));
-        const Q8Scale k = q8_scale(max16(top));
+        const Q8Scale k = q8_scale(max16(q8_top(v[i])));
         if (r >= a.rows || c >= a.cols || !dbg_in(r, a.rows, a.status) || !dbg_in(c, a.cols, a.status)) continue;
         if (lane == 0) store_scale(a.out[0], r, b, k.s);
 #pragma unroll
@@ -157,6 +154,7 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
     pdl_wait();
     pdl_trigger();
     const int hw = threadIdx.x >> 4, lane = threadIdx.x & 15, col = lane * 8;
+    const int late = lane >> 2 & 1;  // every other four lanes their second 16 bytes first: eight of them meet no bank twice
     const long long rt = blockIdx.x / a.col_tiles, ct = blockIdx.x - rt * a.col_tiles;
     const long long r0 = rt * kQBlock, c0 = ct * kQBlock;
     const Spans s = spans_of<PRO>(a);
@@ -184,19 +182,20 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int row = (i + u) * 16 + hw;
-                float t = 0.0f;
+                if (PRO != kPlain) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float x = q8_size(v[u][j]);
-                    top[j] = fmaxf(top[j], x);
-                    t = fmaxf(t, x);
-                    if (PRO != kPlain) sum[j] += v[u][j];
+                    for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
                 }
+                const float t = q8_top(v[u]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top[j] = fmaxf(top[j], fabsf(v[u][j]));
                 if (!a.tile && o.q) put_row(o, row, q8_scale(max16(t)), v[u]);
                 if (keep) {
                     float4* to = reinterpret_cast<float4*>(vals + row * kQBlock + col);
-                    to[0] = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
-                    to[1] = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
+                    const float4 x = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
+                    const float4 y = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
+                    to[late] = late ? y : x;
+                    to[late ^ 1] = late ? x : y;
                 }
             }
         }
@@ -239,7 +238,8 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
 #pragma unroll 2
                     for (int row = hw; row < kQBlock; row += 16) {
                         const float4* from = reinterpret_cast<const float4*>(vals + row * kQBlock + col);
-                        const float4 x = from[0], y = from[1];
+                        const float4 p = from[late], q = from[late ^ 1];
+                        const float4 x = late ? q : p, y = late ? p : q;
                         const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                         put_row(o, row, tile, v);
                     }

@@ -137,10 +137,7 @@ SADMM_DEV void finish8(const FwdArgs& a, long long r, int c, float rstd, float (
         a.y.store(r, c, v, a.status);
         return;
     }
-    float top = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, q8_size(v[j]));
-    const Q8Scale k = q8_scale(max16(top));
+    const Q8Scale k = q8_scale(max16(q8_top(v)));
     if (c >= a.cols || !dbg_in(c, a.cols, a.status) || !dbg_in(r, a.rows, a.status)) return;
     if ((threadIdx.x & 15) == 0) a.y8.s[r * a.y8.s_row + c / kQBlock * a.y8.s_block] = k.s;
 #pragma unroll
