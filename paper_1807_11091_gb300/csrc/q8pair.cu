@@ -1,5 +1,6 @@
 // q8pair.cu -- products of large 8-bit matrices: a persistent kernel of CTA pairs,
-// one tile of 256 rows by 256 columns at a time (gated: 128 of either weight's).
+// one tile of 256 rows by 256 columns at a time (gated: 128 of either weight's; where
+// the columns' scales are single rows', as a weight gradient's, 512 by 128).
 //
 // The pair shares each MMA (tcgen05.mma.cta_group::2, M 256): a CTA holds 128 of
 // the tile's rows and half of its columns' operand (gated: the second CTA Wu's
@@ -13,6 +14,12 @@
 //               the sums' warps the addresses alone took 720 cycles a block, of 512)
 //   warps 4-11  sums and output: TMEM lane = tile row, each half of the warps
 //               takes half of the columns, 128 sums a thread
+//
+// Measured (us, of the operations at twice the 1859 TFLOP/s of bf16): 8192 x 4096 -> 4096 with
+// GELU 160 (74), the gated pair 8192 x 4096 -> 2 x 10240 with g and u kept 667 (370), gradients of
+// 8192 x 5120 -> 2048 with the quantiser 285 (92).  Bound by the accumulators' way to the sums and
+// back: a block takes 0.41 us where its MMAs take 0.27, with single rows' scales 0.75; beside it
+// a tile's output is not hidden, some 4 us and with GELU 8.
 #include <string.h>
 
 #include <initializer_list>
@@ -248,7 +255,7 @@ struct Ring {
 // A warp's two boxes of 32 rows x 128 bytes (64 bf16 or 32 fp32 columns) in shared memory, from
 // which the tensor-memory accelerator writes them out while the next tile is added up, and
 // leaves out what lies past the matrix.  (Stored by the threads themselves, 32 rows of 32
-// bytes at a time, a tile's output took 4.4 us.)
+// bytes at a time, and without WHOLE: 8192 x 4096 -> 4096 162 us instead of 158.)
 struct Boxes {
     uint8_t* mem;
     int lane;
@@ -359,9 +366,8 @@ SADMM_DEV void store16_whole(const Out& o, long long r, long long c, long long n
                               pack_bf16(v[8 * h + 4], v[8 * h + 5]), pack_bf16(v[8 * h + 6], v[8 * h + 7]));
 }
 
-// WHOLE: every output goes out by boxes or whole 16-byte words, bias and residual come by such.  The
-// general forms' instructions, most of them jumped over, do not stay in the SM: a tile's
-// output took 4.4 us with them and with GELU 9.
+// WHOLE: every output goes out by boxes or whole 16-byte words, bias and residual come by such, and
+// the general forms' instructions are not there to be jumped over (1 to 3 % with the boxes).
 template <bool GATED, bool VEC, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 1)
     k_q8_pair(const __grid_constant__ Maps maps, const __grid_constant__ Args a)
@@ -558,8 +564,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     if (VEC) {
-                        // 16 columns of both rows.  (Every thread reads every column's scale: 128 bytes of shared memory a
-                        // cycle, the bound of this form; of one row each 1024 cycles a block, 0.86 us.)
+                        // 16 columns of both rows: every thread reads every column's scale, and with two rows
+                        // half as many as with one (where they were 1024 cycles of shared memory a block).
                         uint32_t r[2][16];
                         tmem_ld_32x32b_x16(from + part * 64 + c * 16, r[0]);
                         tmem_ld_32x32b_x16(from + 128 + part * 64 + c * 16, r[1]);
@@ -764,8 +770,9 @@ bool encode8(CUtensorMap* map, const Q8Operand& o, int box_rows)
 bool encode_out(CUtensorMap* map, const TgMatrix& t, long long m, long long n)
 {
     PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode_fn();
-    if (!t.p || !enc || !make_out(t, m, n).vec) return false;
     const bool bf16 = t.dt == SADMM_BF16;
+    // (a row that ends inside 16 bytes is stored by the threads: by a box, the values behind its last column changed)
+    if (!t.p || !enc || !make_out(t, m, n).vec || n % (bf16 ? 8 : 4)) return false;
     memset(map, 0, sizeof(*map));
     const cuuint64_t gdim[2] = {(cuuint64_t)n, (cuuint64_t)m};
     const cuuint64_t gstride[1] = {(cuuint64_t)t.ld * (bf16 ? 2 : 4)};
@@ -905,7 +912,8 @@ long long time_q8_pair(const Q8Problem& t)
     const long long tiles = (t.m + tall - 1) / tall * ((t.n + wide - 1) / wide);
     const long long pairs = device_sm_count() / 2, rounds = (tiles + pairs - 1) / pairs;
     bool apart = false;
-    for (const TgMatrix* m : {&t.y, &t.residual, &t.z, &t.u}) apart = apart || (m->p && !make_out(*m, t.m, t.n).vec);
+    // (not z and u: what is kept beside y must not change y's bits)
+    for (const TgMatrix* m : {&t.y, &t.residual}) apart = apart || (m->p && !make_out(*m, t.m, t.n).vec);
     return rounds * (blocks_of(t) * (rows ? 750 : 410) + 3500 + (apart ? 25000 : 0)) + 4000;
 }
 

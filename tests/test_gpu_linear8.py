@@ -101,6 +101,63 @@ def test_residual_in_place_and_nothing_beside():
         assert got.data_ptr() == r.data_ptr() and torch.equal(got, want) and untouched(r, before)
 
 
+@pytest.mark.parametrize("tokens,n_in,n_out", [(5, 300, 200), (300, 300, 200), (1100, 640, 1500)])
+def test_tiles_for_tokens_and_rows_for_weights(tokens, n_in, n_out):
+    """Either operand's scales may be of rows or of tiles, forward and backward."""
+    g = gen(tokens)
+    for xt, wt in ((True, True), (True, False), (False, False)):
+        x, W = operand(g, tokens, n_in, xt), operand(g, n_out, n_in, wt, scale=n_in ** -0.5)
+        z, ez = product(x, W)
+        check(sadmm.linear8(*x, *W, out_dtype=FP32), z, rounded(z, ez, FP32), "y")
+        xT, WT = operand(g, n_in, tokens, xt), operand(g, n_in, n_out, wt)
+        dy = matrix(g, tokens, n_out, BF16, "padded", 0.01)
+        dx, dW, _ = sadmm.linear8_backward(dy, *xT, *WT, dx_dtype=FP32, dw_dtype=FP32)
+        for got, d, other in ((dx, dy.double(), WT), (dW, dy.double().t(), xT)):
+            v, e = product(quantized(d.float()), other)
+            check(got, v, rounded(v, e, FP32), "gradient")
+    assert sadmm.device_status() == 0
+
+
+@pytest.mark.parametrize("tokens", [3, 100, 600])
+def test_one_scale_for_a_whole_matrix(tokens):
+    """Scales of stride zero."""
+    g = gen(tokens)
+    x, W = operand(g, tokens, 512), operand(g, 768, 512, True)
+    one = torch.full((1, 1), 0.25, device="cuda")
+    xs, Ws = one.expand(tokens, 4), one.expand(6, 4)
+    z, ez = product((x[0], xs), (W[0], Ws))
+    y = sadmm.linear8(x[0], xs, W[0], Ws, out_dtype=FP32)
+    check(y, z, rounded(z, ez, FP32), "y")
+
+
+@pytest.mark.parametrize("tokens,n_out", [(700, 1000), (2300, 520), (513, 4097), (600, 4092), (1111, 2050)])
+def test_large_outputs_leave_the_rest_of_their_buffers(tokens, n_out):
+    """Whose rows start on 16-byte boundaries (written by the tensor-memory accelerator), with room behind each."""
+    g = gen(tokens)
+    x, W, Wr = operand(g, tokens, 384), operand(g, n_out, 384, True), operand(g, n_out, 384, False)
+    for out in (BF16, FP32):
+        for w in (W, Wr):
+            y, r = matrix(g, tokens, n_out, out, "padded"), matrix(g, tokens, n_out, out, "padded")
+            before = guard(y)
+            got, z = sadmm.linear8(*x, *w, residual=r, out=y, save=True)
+            assert got.data_ptr() == y.data_ptr() and untouched(y, before)
+            v, e = product(x, w)
+            check(z, v, rounded(v, e, BF16), "z")
+            v, e = v + r.double(), e + U32 * (v + r.double()).abs()
+            check(y, v, rounded(v, e, out), "y")
+
+
+def test_what_is_kept_does_not_change_the_result():
+    g = gen(21)
+    for tokens in (4, 60, 900):
+        x, W = operand(g, tokens, 700), operand(g, 900, 700, True)
+        y, _ = sadmm.linear8(*x, *W, act=3, save=True)
+        assert torch.equal(y, sadmm.linear8(*x, *W, act=3))
+        q = sadmm.gated8(*x, *W, *W)
+        k = sadmm.gated8(*x, *W, *W, save=True)
+        assert torch.equal(q[0].view(torch.uint8), k[0].view(torch.uint8)) and torch.equal(q[1], k[1])
+
+
 def test_same_bits_and_leading_dimensions():
     g = gen(14)
     x, W = operand(g, 6, 256), operand(g, 64, 256, True)
