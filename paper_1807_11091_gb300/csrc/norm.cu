@@ -23,6 +23,7 @@
 // (in pairs, f32x2) and its reduction take as long as its bytes; backward of
 // 3001 x 1153 fp32 rows off 16-byte boundaries 14.5 (5.2), bound by loads and
 // stores of single elements.
+// The RMS norm's backward of 8192 x 5120 bf16 with a residual's gradient: 75.5 (49.4 at 6.79 TB/s).
 #include <string.h>
 
 #include "common.cuh"

@@ -8,6 +8,10 @@
 // add it to fp32 sums in registers, while the next block's products run into
 // another accumulator.  Few tiles share their contraction among the CTAs of
 // a cluster, which exchange their sums through shared memory in rank order.
+// Measured: one token, 5120 -> 4096, 6.9 us (3.1 of its 21 MB at 6.79 TB/s): bound by the latencies of
+// a launch, of the loads and of the join; the gated pair of 16 tokens, 4096 -> 2 x 5461, 13.0
+// (6.6 of its 45 MB), from 129 CTAs on 152 SMs; 777 dense rows, 2731 -> 1025, 20.4 with the copy of the
+// unaligned operands (1.7).
 // Per CTA, six warps:
 //   warp 0     TMA producer
 //   warp 1     TMEM allocator, issuer of the MMAs
