@@ -82,17 +82,33 @@ struct Q8Scale {
     float s, r;
 };
 constexpr float kE4m3Max = 448.0f;
-SADMM_DEV Q8Scale q8_scale(float top)
-{
-    Q8Scale q;
-    q.s = __fdiv_rn(fmaxf(top, 1.2621774483536189e-29f /* 2^-96 */), kE4m3Max);
-    q.r = __frcp_rn(q.s);
-    return q;
-}
 SADMM_DEV float q8_quotient(float x, const Q8Scale& k)
 {
     const float q = __fmul_rn(x, k.r);
     return __fmaf_rn(__fmaf_rn(-q, k.s, x), k.r, q);
+}
+SADMM_DEV Q8Scale q8_scale(float top)
+{
+    Q8Scale q;
+    q.s = q8_quotient(fmaxf(top, 1.2621774483536189e-29f /* 2^-96 */), {kE4m3Max, 1.0f / kE4m3Max});
+    q.r = __frcp_rn(q.s);
+    return q;
+}
+// Two at a time, in half the instructions.
+SADMM_DEV void q8_quotients(float& a, float& b, const Q8Scale& k)
+{
+    asm("{\n\t"
+        ".reg .b64 x, q, e, s, r;\n\t"
+        "mov.b64 x, {%0, %1};\n\t"
+        "mov.b64 s, {%2, %2};\n\t"
+        "mov.b64 r, {%3, %3};\n\t"
+        "mul.rn.f32x2 q, x, r;\n\t"
+        "fma.rn.f32x2 e, q, s, x;\n\t"
+        "fma.rn.f32x2 q, e, r, q;\n\t"
+        "mov.b64 {%0, %1}, q;\n\t"
+        "}"
+        : "+f"(a), "+f"(b)
+        : "f"(-k.s), "f"(k.r));
 }
 // The largest finite magnitude of N values (0: none), of which infinities become NaN, as
 // which they end anyway: the largest passes over a NaN by itself.
@@ -117,6 +133,13 @@ SADMM_DEV uint32_t q8_two(float lo, float hi)
     return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }
 SADMM_DEV uint32_t q8_four(float a, float b, float c, float d) { return q8_two(a, b) | q8_two(c, d) << 16; }
+// The same of four quotients.
+SADMM_DEV uint32_t q8_four(float a, float b, float c, float d, const Q8Scale& k)
+{
+    q8_quotients(a, b, k);
+    q8_quotients(c, d, k);
+    return q8_four(a, b, c, d);
+}
 
 // The largest of v over groups of 16 lanes.
 SADMM_DEV float max16(float v)
@@ -124,6 +147,33 @@ SADMM_DEV float max16(float v)
 #pragma unroll
     for (int o = 8; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
+}
+
+// The scales of N rows (2 or 4) from their lanes' largest, over groups of 16 lanes: a lane goes on with
+// one of the rows, so that a scale's arithmetic is done once.
+template <int N>
+SADMM_DEV void scales16(const float (&top)[N], Q8Scale (&k)[N])
+{
+    static_assert(N == 2 || N == 4, "rows of a group");
+    const bool a = threadIdx.x & 8, b = threadIdx.x & 4;
+    float v[N / 2];
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j)
+        v[j] = fmaxf(a ? top[2 * j + 1] : top[2 * j], __shfl_xor_sync(0xffffffffu, a ? top[2 * j] : top[2 * j + 1], 8));
+    float t = v[0];
+    if (N == 4)
+        t = fmaxf(b ? v[N / 2 - 1] : v[0], __shfl_xor_sync(0xffffffffu, b ? v[0] : v[N / 2 - 1], 4));
+    else
+        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+#pragma unroll
+    for (int o = 2; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+    const Q8Scale own = q8_scale(t);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int from = (j & 1) * 8 + (j >> 1) * 4;
+        k[j].s = __shfl_sync(0xffffffffu, own.s, from, 16);
+        k[j].r = __shfl_sync(0xffffffffu, own.r, from, 16);
+    }
 }
 
 // A matrix as bytes: it starts at lo and ends at hi.

@@ -85,7 +85,7 @@ SADMM_DEV void put4(const Args& a, long long r, long long c, float (&v)[4])
     const Q8Scale k = q8_scale(top);
     if (c >= a.n || !dbg_in(c, a.n, a.status) || !dbg_in(r, a.m, a.status)) return;
     if ((threadIdx.x & 31) == 0) a.y8.s[r * a.y8.s_row + c / kQBlock * a.y8.s_block] = k.s;
-    const uint32_t q = q8_four(q8_quotient(v[0], k), q8_quotient(v[1], k), q8_quotient(v[2], k), q8_quotient(v[3], k));
+    const uint32_t q = q8_four(v[0], v[1], v[2], v[3], k);
     uint8_t* p = static_cast<uint8_t*>(a.y8.q) + r * a.y8.ld + c;
     if (c + 4 <= a.n && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
         *reinterpret_cast<uint32_t*>(p) = q;

@@ -722,8 +722,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float* v = acc + c * 16 + j * 4;
-                            w[j] = q8_four(q8_quotient(v[0], k), q8_quotient(v[1], k), q8_quotient(v[2], k),
-                                           q8_quotient(v[3], k));
+                            w[j] = q8_four(v[0], v[1], v[2], v[3], k);
                         }
                         if ((WHOLE || wide) && live >= c * 16 + 16) {
                             reinterpret_cast<uint4*>(out)[c] = make_uint4(w[0], w[1], w[2], w[3]);

@@ -131,16 +131,19 @@ __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
     for (int i = 0; i < kRowSteps; ++i)
         take8(static_cast<const uint8_t*>(a.x) + (r * a.ldx + at(i)) * ES, (int)min(8ll, a.cols - at(i)), a.x_aligned, s.x,
               raw[i], v[i]);
+    float top[kRowSteps];
+    Q8Scale scale[kRowSteps];
+#pragma unroll
+    for (int i = 0; i < kRowSteps; ++i) top[i] = q8_top(v[i]);
+    scales16(top, scale);
 #pragma unroll
     for (int i = 0; i < kRowSteps; ++i) {
         const long long b = cg * kRowSteps + i, c = b * kQBlock + lane * 8;
-        const Q8Scale k = q8_scale(max16(q8_top(v[i])));
+        const Q8Scale k = scale[i];
         if (r >= a.rows || c >= a.cols || !dbg_in(r, a.rows, a.status) || !dbg_in(c, a.cols, a.status)) continue;
         if (lane == 0) store_scale(a.out[0], r, b, k.s);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = q8_quotient(v[i][j], k);
         store_bytes8(static_cast<uint8_t*>(a.out[0].q) + r * a.out[0].ld + c, (int)min(8ll, a.cols - c),
-                     q8_four(v[i][0], v[i][1], v[i][2], v[i][3]), q8_four(v[i][4], v[i][5], v[i][6], v[i][7]));
+                     q8_four(v[i][0], v[i][1], v[i][2], v[i][3], k), q8_four(v[i][4], v[i][5], v[i][6], v[i][7], k));
     }
 }
 
@@ -158,7 +161,8 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
     pdl_wait();
     pdl_trigger();
     const int hw = threadIdx.x >> 4, lane = threadIdx.x & 15, col = lane * 8;
-    const int late = lane >> 2 & 1;  // every other four lanes their second 16 bytes first: eight of them meet no bank twice
+    // every other four lanes' two 16 bytes change places: eight of them meet no bank twice
+    const int late = lane >> 2 & 1;
     const long long rt = blockIdx.x / a.col_tiles, ct = blockIdx.x - rt * a.col_tiles;
     const long long r0 = rt * kQBlock, c0 = ct * kQBlock;
     const Spans s = spans_of<PRO>(a);
@@ -167,11 +171,8 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
         const long long r = r0 + row;
         if (r >= a.rows || live == 0 || !dbg_in(r, a.rows, a.status) || !dbg_run(c0 + col, live, a.cols, a.status)) return;
         if (!a.tile && lane == 0) store_scale(o, r, ct, k.s);
-        float q[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = q8_quotient(v[j], k);
-        store_bytes8(static_cast<uint8_t*>(o.q) + r * o.ld + c0 + col, live, q8_four(q[0], q[1], q[2], q[3]),
-                     q8_four(q[4], q[5], q[6], q[7]));
+        store_bytes8(static_cast<uint8_t*>(o.q) + r * o.ld + c0 + col, live, q8_four(v[0], v[1], v[2], v[3], k),
+                     q8_four(v[4], v[5], v[6], v[7], k));
     };
     for (int which = 0; which < (PRO == kGate ? 2 : 1); ++which) {
         const sadmm_q8_out &o = a.out[which], &ot = a.out_t[which];
@@ -183,6 +184,7 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
         for (int i = 0; i < 8; i += U) {
             float v[U][8];
             load_source<PRO, ACT, ES, U, AL>(a, s, which, r0 + i * 16 + hw, 16, c0 + col, v);
+            float row_top[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int row = (i + u) * 16 + hw;
@@ -190,17 +192,20 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
                 }
-                const float t = q8_top(v[u]);
+                row_top[u] = q8_top(v[u]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) top[j] = fmaxf(top[j], fabsf(v[u][j]));
-                if (!a.tile && o.q) put_row(o, row, q8_scale(max16(t)), v[u]);
                 if (keep) {
                     float4* to = reinterpret_cast<float4*>(vals + row * kQBlock + col);
-                    const float4 x = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
-                    const float4 y = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
-                    to[late] = late ? y : x;
-                    to[late ^ 1] = late ? x : y;
+                    to[late] = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
+                    to[late ^ 1] = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
                 }
+            }
+            if (!a.tile && o.q) {
+                Q8Scale k[U];
+                scales16(row_top, k);
+#pragma unroll
+                for (int u = 0; u < U; ++u) put_row(o, (i + u) * 16 + hw, k[u], v[u]);
             }
         }
 #pragma unroll
@@ -242,8 +247,7 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
 #pragma unroll 2
                     for (int row = hw; row < kQBlock; row += 16) {
                         const float4* from = reinterpret_cast<const float4*>(vals + row * kQBlock + col);
-                        const float4 p = from[late], q = from[late ^ 1];
-                        const float4 x = late ? q : p, y = late ? p : q;
+                        const float4 x = from[late], y = from[late ^ 1];
                         const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                         put_row(o, row, tile, v);
                     }
@@ -260,9 +264,8 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float* f = vals + (row + 4 * i) * kQBlock + c;
-                        w[i] = q8_four(q8_quotient(f[0], k), q8_quotient(f[kQBlock], k), q8_quotient(f[2 * kQBlock], k),
-                                       q8_quotient(f[3 * kQBlock], k));
+                        const float* f = vals + (row + 4 * i) * kQBlock + (c ^ (c >> 5 & 1) << 2);
+                        w[i] = q8_four(f[0], f[kQBlock], f[2 * kQBlock], f[3 * kQBlock], k);
                     }
                     const int n = (int)min(16ll, a.rows - r0 - row);
                     if (!in || n <= 0 || !dbg_run(r0 + row, n, a.rows, a.status)) continue;

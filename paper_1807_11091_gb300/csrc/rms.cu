@@ -146,10 +146,8 @@ SADMM_DEV void finish8(const FwdArgs& a, long long r, int c, float rstd, float (
     const Q8Scale k = q8_scale(max16(q8_top(v)));
     if (c >= a.cols || !dbg_in(c, a.cols, a.status) || !dbg_in(r, a.rows, a.status)) return;
     if ((threadIdx.x & 15) == 0) a.y8.s[r * a.y8.s_row + c / kQBlock * a.y8.s_block] = k.s;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = q8_quotient(v[j], k);
-    store_bytes8(static_cast<uint8_t*>(a.y8.q) + r * a.y8.ld + c, a.cols - c, q8_four(v[0], v[1], v[2], v[3]),
-                 q8_four(v[4], v[5], v[6], v[7]));
+    store_bytes8(static_cast<uint8_t*>(a.y8.q) + r * a.y8.ld + c, a.cols - c, q8_four(v[0], v[1], v[2], v[3], k),
+                 q8_four(v[4], v[5], v[6], v[7], k));
 }
 
 // A row over a group of threads, a warp or a block, E times 8 neighbours each, kept in
