@@ -227,7 +227,7 @@ SADMM_DEV void ask8(const uint8_t* p, bool in, bool aligned, const Span& m, Raw8
 {
     aligned = AL || aligned;
     const uint8_t* b = AL ? p : p - (reinterpret_cast<uintptr_t>(p) & 15);
-    const bool ok = in && b >= m.lo && b + (ES / 2 + !aligned) * 16 <= m.hi;
+    const bool ok = in && (AL || b >= m.lo) && b + (ES / 2 + !aligned) * 16 <= m.hi;
     r.apart = in && !ok;
 #pragma unroll
     for (int k = 0; k < r.n; ++k) {
@@ -267,7 +267,12 @@ SADMM_DEV void take8(const uint8_t* p, int n, bool aligned, const Span& m, const
     for (int j = 0; j < 8; ++j) {
         const float x = ES == 4 ? __uint_as_float(w[ES == 4 ? j : 0])
                                 : __uint_as_float((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
-        v[j] = j < n ? x : 0.0f;
+        v[j] = x;
+    }
+    if (n < 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j >= n) v[j] = 0.0f;
     }
 }
 

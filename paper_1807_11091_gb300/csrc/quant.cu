@@ -98,8 +98,11 @@ SADMM_DEV void load_source(const Args& a, const Spans& s, int which, long long r
                 v[i][j] = which ? v[i][j] * f : v[i][j] * uv[j] * slope;
             else
                 v[i][j] *= slope;
-            if (c + j >= a.cols) v[i][j] = 0.0f;  // (the slope there may be 0 times an infinity)
         }
+        if (c + 8 <= a.cols) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j >= a.cols) v[i][j] = 0.0f;  // (the slope there may be 0 times an infinity)
     }
 }
 
@@ -167,9 +170,10 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
     const long long r0 = rt * kQBlock, c0 = ct * kQBlock;
     const Spans s = spans_of<PRO>(a);
     const int live = (int)max(0ll, min(8ll, a.cols - c0 - col));  // the lane's columns inside the matrix
+    const int rows = (int)min((long long)kQBlock, a.rows - r0);    // the tile's
     auto put_row = [&](const sadmm_q8_out& o, int row, const Q8Scale& k, const float (&v)[8]) {
         const long long r = r0 + row;
-        if (r >= a.rows || live == 0 || !dbg_in(r, a.rows, a.status) || !dbg_run(c0 + col, live, a.cols, a.status)) return;
+        if (row >= rows || live == 0 || !dbg_in(r, a.rows, a.status) || !dbg_run(c0 + col, live, a.cols, a.status)) return;
         if (!a.tile && lane == 0) store_scale(o, r, ct, k.s);
         store_bytes8(static_cast<uint8_t*>(o.q) + r * o.ld + c0 + col, live, q8_four(v[0], v[1], v[2], v[3], k),
                      q8_four(v[4], v[5], v[6], v[7], k));
