@@ -90,14 +90,19 @@ SADMM_DEV void load_source(const Args& a, const Spans& s, int which, long long r
         float zv[8], uv[8];
         z.take(a.z, a.ldz, a.z_aligned, s.z, a, r, step, c, Z ? i : 0, zv);
         if (PRO == kGate && which == 0) u.take(a.u, a.ldu, a.u_aligned, s.u, a, r, step, c, PRO == kGate ? i : 0, uv);
+        float f[8], slope[8];
+        if (PRO == kGate && which) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float f, slope;
-            act_slope_f32<ACT>(zv[j], f, slope);
-            if (PRO == kGate)
-                v[i][j] = which ? v[i][j] * f : v[i][j] * uv[j] * slope;
-            else
-                v[i][j] *= slope;
+            for (int j = 0; j < 8; ++j) {
+                act_slope_f32<ACT>(zv[j], f[j], slope[j]);
+                v[i][j] *= f[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                act_slope_f32<ACT>(zv[j], f[j], slope[j]);
+                v[i][j] = PRO == kGate ? v[i][j] * uv[j] * slope[j] : v[i][j] * slope[j];
+            }
         }
         if (c + 8 <= a.cols) continue;
 #pragma unroll
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(256) k_q8_rows(const Args a)
 template <int PRO, int ACT, int ES, bool AL>
 __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
 {
-    constexpr int U = PRO == kGate ? 2 : 4;  // rows whose loads are in flight together
+    constexpr int U = PRO == kGate || (PRO == kSlope && ACT != SADMM_ACT_NONE) ? 2 : 4;  // rows whose loads are in flight together
     extern __shared__ __align__(16) float vals[];  // [128][128]
     __shared__ float red[8][kQBlock], sums[PRO == kPlain ? 1 : 8][PRO == kPlain ? 1 : kQBlock], top_s[kQBlock];
     pdl_wait();
@@ -166,7 +171,9 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
     const int hw = threadIdx.x >> 4, lane = threadIdx.x & 15, col = lane * 8;
     // every other four lanes' two 16 bytes change places: eight of them meet no bank twice
     const int late = lane >> 2 & 1;
-    const long long rt = blockIdx.x / a.col_tiles, ct = blockIdx.x - rt * a.col_tiles;
+    const int which = PRO == kGate ? blockIdx.x & 1 : 0;  // (the CTAs of dg and du of a tile run side by side)
+    const long long at = PRO == kGate ? blockIdx.x >> 1 : blockIdx.x;
+    const long long rt = at / a.col_tiles, ct = at - rt * a.col_tiles;
     const long long r0 = rt * kQBlock, c0 = ct * kQBlock;
     const Spans s = spans_of<PRO>(a);
     const int live = (int)max(0ll, min(8ll, a.cols - c0 - col));  // the lane's columns inside the matrix
@@ -178,111 +185,108 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
         store_bytes8(static_cast<uint8_t*>(o.q) + r * o.ld + c0 + col, live, q8_four(v[0], v[1], v[2], v[3], k),
                      q8_four(v[4], v[5], v[6], v[7], k));
     };
-    for (int which = 0; which < (PRO == kGate ? 2 : 1); ++which) {
-        const sadmm_q8_out &o = a.out[which], &ot = a.out_t[which];
-        const bool keep = ot.q || a.tile;
-        float top[8], sum[8];
+    const sadmm_q8_out &o = a.out[which], &ot = a.out_t[which];
+    const bool keep = ot.q || a.tile;
+    float top[8], sum[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top[j] = sum[j] = 0.0f;
+    for (int j = 0; j < 8; ++j) top[j] = sum[j] = 0.0f;
 #pragma unroll 1
-        for (int i = 0; i < 8; i += U) {
-            float v[U][8];
-            load_source<PRO, ACT, ES, U, AL>(a, s, which, r0 + i * 16 + hw, 16, c0 + col, v);
-            float row_top[U];
+    for (int i = 0; i < 8; i += U) {
+        float v[U][8];
+        load_source<PRO, ACT, ES, U, AL>(a, s, which, r0 + i * 16 + hw, 16, c0 + col, v);
+        float row_top[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int row = (i + u) * 16 + hw;
-                if (PRO != kPlain) {
+        for (int u = 0; u < U; ++u) {
+            const int row = (i + u) * 16 + hw;
+            if (PRO != kPlain) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
-                }
-                row_top[u] = q8_top(v[u]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top[j] = fmaxf(top[j], fabsf(v[u][j]));
-                if (keep) {
-                    float4* to = reinterpret_cast<float4*>(vals + row * kQBlock + col);
-                    to[late] = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
-                    to[late ^ 1] = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
-                }
+                for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
             }
-            if (!a.tile && o.q) {
-                Q8Scale k[U];
-                scales16(row_top, k);
+            row_top[u] = q8_top(v[u]);
 #pragma unroll
-                for (int u = 0; u < U; ++u) put_row(o, (i + u) * 16 + hw, k[u], v[u]);
+            for (int j = 0; j < 8; ++j) top[j] = fmaxf(top[j], fabsf(v[u][j]));
+            if (keep) {
+                float4* to = reinterpret_cast<float4*>(vals + row * kQBlock + col);
+                to[late] = make_float4(v[u][0], v[u][1], v[u][2], v[u][3]);
+                to[late ^ 1] = make_float4(v[u][4], v[u][5], v[u][6], v[u][7]);
             }
         }
+        if (!a.tile && o.q) {
+            Q8Scale k[U];
+            scales16(row_top, k);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
-            if (PRO != kPlain) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
-            if (hw & 1) continue;
-            red[hw >> 1][col + j] = top[j];
-            if (PRO != kPlain) sums[PRO == kPlain ? 0 : hw >> 1][PRO == kPlain ? 0 : col + j] = sum[j];
+            for (int u = 0; u < U; ++u) put_row(o, (i + u) * 16 + hw, k[u], v[u]);
         }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
+        if (PRO != kPlain) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+        if (hw & 1) continue;
+        red[hw >> 1][col + j] = top[j];
+        if (PRO != kPlain) sums[PRO == kPlain ? 0 : hw >> 1][PRO == kPlain ? 0 : col + j] = sum[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < kQBlock) {
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t = fmaxf(t, red[w][threadIdx.x]);
+        top_s[threadIdx.x] = t;
+        if (PRO != kPlain && a.part[which] && c0 + threadIdx.x < a.cols) {
+            float p = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) p += sums[PRO == kPlain ? 0 : w][PRO == kPlain ? 0 : threadIdx.x];
+            a.part[which][rt * a.cols + c0 + threadIdx.x] = p;
+        }
+    }
+    if (keep) {
         __syncthreads();
-        if (threadIdx.x < kQBlock) {
+        Q8Scale tile = {1.0f, 1.0f};
+        if (a.tile) {
             float t = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) t = fmaxf(t, red[w][threadIdx.x]);
-            top_s[threadIdx.x] = t;
-            if (PRO != kPlain && a.part[which] && c0 + threadIdx.x < a.cols) {
-                float p = 0.0f;
+            for (int j = 0; j < 4; ++j) t = fmaxf(t, top_s[(threadIdx.x & 31) * 4 + j]);
 #pragma unroll
-                for (int w = 0; w < 8; ++w) p += sums[PRO == kPlain ? 0 : w][PRO == kPlain ? 0 : threadIdx.x];
-                a.part[which][rt * a.cols + c0 + threadIdx.x] = p;
+            for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            tile = q8_scale(t);
+            if (threadIdx.x == 0) {
+                if (o.q) store_scale(o, rt, ct, tile.s);
+                if (ot.q) store_scale(ot, ct, rt, tile.s);
             }
-        }
-        if (keep) {
-            __syncthreads();
-            Q8Scale tile = {1.0f, 1.0f};
-            if (a.tile) {
-                float t = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) t = fmaxf(t, top_s[(threadIdx.x & 31) * 4 + j]);
-#pragma unroll
-                for (int d = 16; d; d >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-                tile = q8_scale(t);
-                if (threadIdx.x == 0) {
-                    if (o.q) store_scale(o, rt, ct, tile.s);
-                    if (ot.q) store_scale(ot, ct, rt, tile.s);
-                }
-                if (o.q) {
+            if (o.q) {
 #pragma unroll 2
-                    for (int row = hw; row < kQBlock; row += 16) {
-                        const float4* from = reinterpret_cast<const float4*>(vals + row * kQBlock + col);
-                        const float4 x = from[late], y = from[late ^ 1];
-                        const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                        put_row(o, row, tile, v);
-                    }
-                }
-            }
-            if (ot.q) {
-                const int c = threadIdx.x & 127;
-                const Q8Scale k = a.tile ? tile : q8_scale(top_s[c]);
-                const bool in = c0 + c < a.cols && dbg_in(c0 + c, a.cols, a.status);
-                if (!a.tile && in && threadIdx.x < kQBlock) store_scale(ot, c0 + c, rt, k.s);
-                uint8_t* to = static_cast<uint8_t*>(ot.q) + (in ? (c0 + c) * ot.ld : 0) + r0;
-#pragma unroll 1
-                for (int row = (threadIdx.x >> 7) * 16; row < kQBlock; row += 32) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float* f = vals + (row + 4 * i) * kQBlock + (c ^ (c >> 5 & 1) << 2);
-                        w[i] = q8_four(f[0], f[kQBlock], f[2 * kQBlock], f[3 * kQBlock], k);
-                    }
-                    const int n = (int)min(16ll, a.rows - r0 - row);
-                    if (!in || n <= 0 || !dbg_run(r0 + row, n, a.rows, a.status)) continue;
-                    if (n == 16 && (reinterpret_cast<uintptr_t>(to + row) & 15) == 0) {
-                        *reinterpret_cast<uint4*>(to + row) = make_uint4(w[0], w[1], w[2], w[3]);
-                    } else {
-                        store_bytes8(to + row, n, w[0], w[1]);
-                        store_bytes8(to + row + 8, n - 8, w[2], w[3]);
-                    }
+                for (int row = hw; row < kQBlock; row += 16) {
+                    const float4* from = reinterpret_cast<const float4*>(vals + row * kQBlock + col);
+                    const float4 x = from[late], y = from[late ^ 1];
+                    const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                    put_row(o, row, tile, v);
                 }
             }
         }
-        if (PRO == kGate) __syncthreads();  // shared memory is written again
+        if (ot.q) {
+            const int c = threadIdx.x & 127;
+            const Q8Scale k = a.tile ? tile : q8_scale(top_s[c]);
+            const bool in = c0 + c < a.cols && dbg_in(c0 + c, a.cols, a.status);
+            if (!a.tile && in && threadIdx.x < kQBlock) store_scale(ot, c0 + c, rt, k.s);
+            uint8_t* to = static_cast<uint8_t*>(ot.q) + (in ? (c0 + c) * ot.ld : 0) + r0;
+#pragma unroll 1
+            for (int row = (threadIdx.x >> 7) * 16; row < kQBlock; row += 32) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float* f = vals + (row + 4 * i) * kQBlock + (c ^ (c >> 5 & 1) << 2);
+                    w[i] = q8_four(f[0], f[kQBlock], f[2 * kQBlock], f[3 * kQBlock], k);
+                }
+                const int n = (int)min(16ll, a.rows - r0 - row);
+                if (!in || n <= 0 || !dbg_run(r0 + row, n, a.rows, a.status)) continue;
+                if (n == 16 && (reinterpret_cast<uintptr_t>(to + row) & 15) == 0) {
+                    *reinterpret_cast<uint4*>(to + row) = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+                    store_bytes8(to + row, n, w[0], w[1]);
+                    store_bytes8(to + row + 8, n - 8, w[2], w[3]);
+                }
+            }
+        }
     }
 }
 
@@ -386,7 +390,7 @@ sadmm_status launch_q8_source(const Q8Source& q, void* ws, cudaStream_t s)
         if (grid > 0x7fffffffll) return SADMM_EUNSUPPORTED;
         err = launch_pdl(fp32 ? k_q8_rows<4> : k_q8_rows<2>, dim3((unsigned)grid), dim3(256), 0, s, a);
     } else {
-        const long long grid = a.row_tiles * a.col_tiles;
+        const long long grid = a.row_tiles * a.col_tiles * (q.u ? 2 : 1);
         if (grid > 0x7fffffffll) return SADMM_EUNSUPPORTED;
         const int act = a.z ? a.act : SADMM_ACT_NONE;
         if (q.u)
