@@ -143,6 +143,46 @@ bool by_pairs(const Q8Problem& t)
     return !(t.mode == kTgGated && row_scales(t)) && time_q8_pair(t) < time_q8_product(t);
 }
 
+// Rows r .. r+m-1 and columns c .. c+n-1 of a product (no gated pair); r and c are multiples of 128.
+Q8Problem part_of(const Q8Problem& t, long long r, long long m, long long c, long long n)
+{
+    Q8Problem p = t;
+    p.m = m, p.n = n;
+    for (int j = 0; j < (t.mode == kTgSum ? 2 : 1); ++j) {
+        auto rows = [](Q8Operand& o, long long first, long long count) {
+            o.p = static_cast<const uint8_t*>(o.p) + first * o.ld;
+            o.s += (first >> o.shift) * o.s_row;
+            o.rows = count;
+        };
+        rows(p.a[j], r, m);
+        rows(p.b[j], c, n);
+    }
+    if (p.bias) p.bias += c;
+    for (TgMatrix* o : {&p.y, &p.residual, &p.z})
+        if (o->p) o->p = static_cast<uint8_t*>(o->p) + (r * o->ld + c) * (o->dt == SADMM_BF16 ? 2 : 4);
+    return p;
+}
+
+// A product by CTA pairs: all of it, or whole rounds of their tiles and the remaining rows
+// or columns by single tiles, which share a long contraction among more CTAs (weights' gradient of
+// 8192 x 5120 -> 2048, 160 tiles on 76 pairs: the backward pass 280 us, so 252).
+sadmm_status launch_pairs(const Q8Problem& t, cudaStream_t s)
+{
+    if (t.mode == kTgGated) return launch_q8_pair(&t, 1, s);
+    long long rows, cols, best = time_q8_pair(t);
+    q8_pair_less(t, rows, cols);
+    Q8Problem most = t, rest = t;
+    rest.m = 0;
+    auto weigh = [&](const Q8Problem& a, const Q8Problem& b) {
+        const long long time = time_q8_pair(a) + time_q8_product(b);
+        if (time < best) best = time, most = a, rest = b;
+    };
+    if (rows > 0 && rows < t.m) weigh(part_of(t, 0, rows, 0, t.n), part_of(t, rows, t.m - rows, 0, t.n));
+    if (cols > 0 && cols < t.n) weigh(part_of(t, 0, t.m, 0, cols), part_of(t, 0, t.m, cols, t.n - cols));
+    const sadmm_status st = launch_q8_pair(&most, 1, s);
+    return st == SADMM_OK && rest.m ? launch_q8_product(rest, s) : st;
+}
+
 // Products of one call: by CTA pairs, neighbours of one kind in one launch, or by
 // single tiles.
 sadmm_status launch_q8_products(const Q8Problem* t, int n, cudaStream_t s)
@@ -152,7 +192,7 @@ sadmm_status launch_q8_products(const Q8Problem* t, int n, cudaStream_t s)
         int m = i;
         while (m < n && by_pairs(t[m]) && row_scales(t[m]) == row_scales(t[i])) ++m;
         if (m > i) {
-            st = launch_q8_pair(t + i, m - i, s);
+            st = m - i == 1 ? launch_pairs(t[i], s) : launch_q8_pair(t + i, m - i, s);
             i = m;
         } else {
             st = launch_q8_product(t[i++], s);

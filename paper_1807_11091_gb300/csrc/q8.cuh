@@ -48,6 +48,9 @@ sadmm_status launch_q8_product(const Q8Problem& t, cudaStream_t s);
 long long time_q8_product(const Q8Problem& t);
 sadmm_status launch_q8_pair(const Q8Problem* t, int count, cudaStream_t s);
 long long time_q8_pair(const Q8Problem& t);
+// The most rows (of all columns), and the most columns (of all rows), that the pairs have done one round of
+// tiles earlier, in whole tiles; 0: there is but one round.
+void q8_pair_less(const Q8Problem& t, long long& rows, long long& cols);
 
 // Matrices in 8 bits (quant.cu).  What is made 8-bit: x; dy act'(z) (z given); or
 // the gated pair's dg and du (u given), whose outputs are [0] and [1].  sums: column

@@ -900,16 +900,40 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     return vec ? run<false, true, false>(maps, a, ctas, s) : run<false, false, false>(maps, a, ctas, s);
 }
 
+namespace {
+
+// The tiles of a product by itself, a pair's one after the other.
+struct Rounds {
+    bool rows;  // the columns have scales of single rows
+    long long tall, wide, down, across, pairs, rounds;
+    explicit Rounds(const Q8Problem& t)
+    {
+        rows = t.b[0].shift == 0 || (t.mode != kTgSingle && t.b[1].shift == 0);
+        tall = rows ? 512 : 256, wide = rows || t.mode == kTgGated ? 128 : 256;
+        down = (t.m + tall - 1) / tall, across = (t.n + wide - 1) / wide;
+        pairs = device_sm_count() / 2;
+        rounds = (down * across + pairs - 1) / pairs;
+    }
+};
+
+}  // namespace
+
+void q8_pair_less(const Q8Problem& t, long long& rows, long long& cols)
+{
+    const Rounds r(t);
+    rows = (r.rounds - 1) * r.pairs / r.across * r.tall;
+    cols = (r.rounds - 1) * r.pairs / r.down * r.wide;
+}
+
 // Expected time of a product by itself, ns.  Measured: a block takes 0.41 us, 0.75 where the
 // columns have scales of single rows; a round of tiles 3.5 beside its blocks (where
 // an output's rows do not start on 16-byte boundaries 25 more: its elements are stored one by one,
 // 32 rows a store), a launch 4.
 long long time_q8_pair(const Q8Problem& t)
 {
-    const bool rows = t.b[0].shift == 0 || (t.mode != kTgSingle && t.b[1].shift == 0);
-    const int tall = rows ? 512 : 256, wide = rows || t.mode == kTgGated ? 128 : 256;
-    const long long tiles = (t.m + tall - 1) / tall * ((t.n + wide - 1) / wide);
-    const long long pairs = device_sm_count() / 2, rounds = (tiles + pairs - 1) / pairs;
+    const Rounds r(t);
+    const bool rows = r.rows;
+    const long long rounds = r.rounds;
     bool apart = false;
     // (not z and u: what is kept beside y must not change y's bits)
     for (const TgMatrix* m : {&t.y, &t.residual}) apart = apart || (m->p && !make_out(*m, t.m, t.n).vec);

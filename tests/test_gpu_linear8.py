@@ -147,6 +147,26 @@ def test_large_outputs_leave_the_rest_of_their_buffers(tokens, n_out):
             check(y, v, rounded(v, e, out), "y")
 
 
+@pytest.mark.parametrize("tokens,n_out", [(19622, 256), (19712, 250), (256, 19622), (250, 19712)])
+def test_a_few_tiles_more_than_rounds(tokens, n_out):
+    """Tiles of 256 x 256 on 76 pairs of CTAs: the last ones may be computed apart."""
+    forward(gen(tokens), tokens, 4096, n_out, "gelu", True, True, BF16, save=True)
+    forward(gen(tokens), tokens, 4096, n_out, "none", True, True, FP32, "odd", "rows", True)
+    forward(gen(tokens), tokens, 4096, n_out, "silu", True, False, FP32, scales="apart", tiles=False)
+
+
+@pytest.mark.parametrize("n_out,n_in,tokens", [(512, 9856, 2048), (500, 9850, 2050), (39000, 120, 2100), (2048, 5120, 4096)])
+def test_weight_gradients_of_a_few_tiles_more_than_rounds(n_out, n_in, tokens):
+    """Tiles of 512 x 128."""
+    g = gen(n_out)
+    dy = matrix(g, tokens, n_out, BF16, "padded", 0.01)
+    xT = operand(g, n_in, tokens, False)
+    _, dW, _ = sadmm.linear8_backward(dy, *xT, None, None, want_dx=False, dw_dtype=FP32)
+    v, e = product(quantized(dy.double().t().float()), xT)
+    check(dW, v, rounded(v, e, FP32), "dW")
+    assert sadmm.device_status() == 0
+
+
 def test_what_is_kept_does_not_change_the_result():
     g = gen(21)
     for tokens in (4, 60, 900):
