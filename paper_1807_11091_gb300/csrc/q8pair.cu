@@ -17,7 +17,7 @@
 //
 // Measured (us, of the operations at twice the 1859 TFLOP/s of bf16): 8192 x 4096 -> 4096 with
 // GELU 160 (74), the gated pair 8192 x 4096 -> 2 x 10240 with g and u kept 667 (370), gradients of
-// 8192 x 5120 -> 2048 with the quantiser 285 (92).  Bound by the accumulators' way to the sums and
+// 8192 x 5120 -> 2048 with the quantiser 252 (92).  Bound by the accumulators' way to the sums and
 // back: a block takes 0.41 us where its MMAs take 0.27, with single rows' scales 0.75; beside it
 // a tile's output is not hidden, some 4 us and with GELU 8.
 #include <string.h>
