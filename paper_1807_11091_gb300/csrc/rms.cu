@@ -47,6 +47,10 @@ SADMM_DEV void clear(RowSums& red)
     for (int i = threadIdx.x; i < 64; i += blockDim.x) (&red.v[0][0])[i] = 0.0f;
 }
 
+// The rounded root and quotient: rsqrtf may be two units off, once a row for every value of it
+// (4 x 4096 and 16384 x 4096 take the same time with either).
+SADMM_DEV float rstd_of(float sum, float n, float eps) { return 1.0f / sqrtf(sum / n + eps); }
+
 SADMM_DEV float round_to(float v, int dt) { return dt == SADMM_BF16 ? __bfloat162float(__float2bfloat16_rn(v)) : v; }
 
 // Row r of a matrix of bf16 or fp32 elements.
@@ -204,7 +208,7 @@ __global__ void __launch_bounds__(!BLOCK ? 256 : E == 4 ? 1024 : 512, !BLOCK ? 3
             for (int j = 0; j < 8; ++j) p += v[k][j] * v[k][j];
             sum += p;
         }
-        const float rstd = rsqrtf(row_sum<BLOCK>(sum, red, slot) / a.n + a.eps);
+        const float rstd = rstd_of(row_sum<BLOCK>(sum, red, slot), a.n, a.eps);
         slot ^= 1;
         if (t == 0 && a.rstd) a.rstd[r] = rstd;
 #pragma unroll
@@ -233,7 +237,7 @@ __global__ void __launch_bounds__(1024) k_rms_fwd_long(const FwdArgs a)
         for (int j = 0; j < 8; ++j) p += v[j] * v[j];
         sum += p;
     }
-    const float rstd = rsqrtf(row_sum<true>(sum, red, 0) / a.n + a.eps);
+    const float rstd = rstd_of(row_sum<true>(sum, red, 0), a.n, a.eps);
     if (threadIdx.x == 0 && a.rstd) a.rstd[r] = rstd;
     const int end = (a.cols + 255) & ~255;  // a whole warp's columns
     for (int c = threadIdx.x * 8; c < end; c += 8192) {
