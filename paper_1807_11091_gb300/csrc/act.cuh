@@ -31,13 +31,15 @@ SADMM_DEV float exp2_fast(float x)
 // error, 1.3e-7; with its rounding 4.4e-7).  The exponent c z^2, c = -log2(e) / 2, is
 // taken in two parts, because the power would enlarge its rounding.  4096^3 in fp32
 // takes 134 us so and with erf, 205 with CUDA's normcdff, which is as exact.
-SADMM_DEV float gelu_f32(float z)
+// e: exp(-z^2 / 2); returns Phi(z).
+SADMM_DEV float phi_f32(float z, float& e)
 {
     const float w = fminf(fabsf(z), 15.0f);  // past which the smaller side is 0
     constexpr float c = -0.721347511f, c_low = -9.62981517e-09f;
     const float s = w * w, h = s * c;
     const float low = fmaf(s, c, -h) + fmaf(s, c_low, fmaf(w, w, -s) * c);
-    const float p = exp2_fast(h), e = fmaf(p, low * 0.693147181f, p);
+    const float p = exp2_fast(h);
+    e = fmaf(p, low * 0.693147181f, p);
     const float t = __fdividef(1.0f, 1.0f + 0.3f * w);
     float g = 0.0359317213f;
     g = fmaf(g, t, -0.158275947f);
@@ -48,7 +50,12 @@ SADMM_DEV float gelu_f32(float z)
     g = fmaf(g, t, 0.120798357f);
     g = fmaf(g, t, 0.119626388f);
     const float q = e * (t * g);
-    return z * (z > 0.0f ? 1.0f - q : q);
+    return z > 0.0f ? 1.0f - q : q;
+}
+SADMM_DEV float gelu_f32(float z)
+{
+    float e;
+    return z * phi_f32(z, e);
 }
 
 // act(z): max(z, 0) (NaN kept); gelu_f32; z sigmoid(z).
@@ -68,7 +75,7 @@ SADMM_DEV float act_f32(float z)
 
 // act(z) and the slope act'(z) ([z > 0]; Phi(z) + z phi(z); s + z s (1 - s) with
 // s = 1 / (1 + exp(-z)), where an infinite exp gives 0) together, for results that
-// are rounded to bf16, an error of 2^-9 to 2^-8.  Chosen for speed, far below that:
+// are rounded to bf16, an error of 2^-9 to 2^-8 (and the column sums of those of a bf16 block).  Chosen for speed, far below that:
 // exp by its fast form (2^-21 and |z| 2^-23 of the value; with z^2 / 2 for |z|
 // below 2e-5), and Phi's smaller side as exp(-z^2 / 2) t P(t), t = 1 / (1 + 0.29 |z|),
 // with P of degree 5 fitted to that quotient for |z| up to 13.5 (least weighted
@@ -93,6 +100,23 @@ SADMM_DEV void act_slope_f32(float z, float& a, float& s)
     } else {
         a = act_f32<ACT>(z);
         s = ACT == SADMM_ACT_RELU ? (z > 0.0f ? 1.0f : 0.0f) : 1.0f;
+    }
+}
+
+// The same for what becomes fp32 sums or 8-bit values (a backward pass of 8-bit operands), at fp32's
+// precision: GELU by phi_f32 (the gated pair's backward of 4096 x 2048 -> 5461 361 us, 353 with the form above,
+// 3 times the error where GELU is small); SiLU's form above is that of 12 units already, and takes 337 where
+// expf takes 343.
+template <int ACT>
+SADMM_DEV void act_slope_exact(float z, float& a, float& s)
+{
+    if (ACT == SADMM_ACT_GELU) {
+        float e;
+        const float p = phi_f32(z, e);
+        a = z * p;
+        s = p + z * 0.39894228040143268f * e;
+    } else {
+        act_slope_f32<ACT>(z, a, s);
     }
 }
 

@@ -95,13 +95,13 @@ SADMM_DEV void load_source(const Args& a, const Spans& s, int which, long long r
         if (PRO == kGate && which) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                act_slope_f32<ACT>(zv[j], f[j], slope[j]);
+                act_slope_exact<ACT>(zv[j], f[j], slope[j]);
                 v[i][j] *= f[j];
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                act_slope_f32<ACT>(zv[j], f[j], slope[j]);
+                act_slope_exact<ACT>(zv[j], f[j], slope[j]);
                 v[i][j] = PRO == kGate ? v[i][j] * uv[j] * slope[j] : v[i][j] * slope[j];
             }
         }
