@@ -76,42 +76,50 @@ sadmm_status launch_q8_source(const Q8Source& a, void* ws, cudaStream_t s);
 
 #ifdef __CUDACC__
 
-// A block's scale from its largest magnitude, and the quotients x / s of the
-// block as fp32 divisions round them: q = x r with r = 1 / s and one correction,
-// q + r (x - q s), which gives the nearest number where r is the nearest to 1 / s
-// (Markstein, 1990, theorem 8); an infinite x gives NaN.  A tenth of a division's
-// time a value (1 / s is taken once a block).
+// A block's scale s from its largest magnitude, and the quotients x / s of the block
+// as fp32 divisions round them, zeros with their signs.  With s = d 2^e, 1 <= d < 2, and
+// y = -x 2^-e: q = y (-r) with r = 1 / d and one correction, q + (q d + y)(-r), which gives the
+// nearest number where r is the nearest to 1 / d (Markstein, 1990, theorem 8) and the rest
+// q d + y is exact, as it is here for every q from 2^-80 on (without 2^-e its last digits are lost
+// below s = 2^-92).  A zero's rest is +0, whatever its sign, and (+0)(-r) leaves either
+// zero as it is.  An infinite x gives NaN.  A tenth of a division's time a value (1 / d is
+// taken once a block).
 struct Q8Scale {
-    float s, r;
+    float s, d, m, r;  // the scale; d, -2^-e and -1 / d
 };
 constexpr float kE4m3Max = 448.0f;
-SADMM_DEV float q8_quotient(float x, const Q8Scale& k)
+SADMM_DEV Q8Scale q8_scale_of(float s, float r)
 {
-    const float q = __fmul_rn(x, k.r);
-    return __fmaf_rn(__fmaf_rn(-q, k.s, x), k.r, q);
+    const uint32_t bits = __float_as_uint(s);
+    return {s, __uint_as_float((bits & 0x007fffffu) | 0x3f800000u),
+            __uint_as_float((0x7f000000u - (bits & 0x7f800000u)) | 0x80000000u), r};
 }
 SADMM_DEV Q8Scale q8_scale(float top)
 {
-    Q8Scale q;
-    q.s = q8_quotient(fmaxf(top, 1.2621774483536189e-29f /* 2^-96 */), {kE4m3Max, 1.0f / kE4m3Max});
-    q.r = __frcp_rn(q.s);
-    return q;
+    constexpr float r = 1.0f / kE4m3Max;
+    top = fmaxf(top, 1.2621774483536189e-29f /* 2^-96 */);
+    const float q = __fmul_rn(top, r), s = __fmaf_rn(__fmaf_rn(-q, kE4m3Max, top), r, q);
+    Q8Scale k = q8_scale_of(s, 0.0f);
+    k.r = -__frcp_rn(k.d);
+    return k;
 }
 // Two at a time, in half the instructions.
 SADMM_DEV void q8_quotients(float& a, float& b, const Q8Scale& k)
 {
     asm("{\n\t"
-        ".reg .b64 x, q, e, s, r;\n\t"
-        "mov.b64 x, {%0, %1};\n\t"
-        "mov.b64 s, {%2, %2};\n\t"
-        "mov.b64 r, {%3, %3};\n\t"
-        "mul.rn.f32x2 q, x, r;\n\t"
-        "fma.rn.f32x2 e, q, s, x;\n\t"
+        ".reg .b64 y, q, e, d, m, r;\n\t"
+        "mov.b64 y, {%0, %1};\n\t"
+        "mov.b64 d, {%2, %2};\n\t"
+        "mov.b64 m, {%3, %3};\n\t"
+        "mov.b64 r, {%4, %4};\n\t"
+        "mul.rn.f32x2 y, y, m;\n\t"
+        "mul.rn.f32x2 q, y, r;\n\t"
+        "fma.rn.f32x2 e, q, d, y;\n\t"
         "fma.rn.f32x2 q, e, r, q;\n\t"
         "mov.b64 {%0, %1}, q;\n\t"
         "}"
         : "+f"(a), "+f"(b)
-        : "f"(-k.s), "f"(k.r));
+        : "f"(k.d), "f"(k.m), "f"(k.r));
 }
 // The largest finite magnitude of N values (0: none), of which infinities become NaN, as
 // which they end anyway: the largest passes over a NaN by itself.
@@ -174,8 +182,7 @@ SADMM_DEV void scales16(const float (&top)[N], Q8Scale (&k)[N])
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const int from = (j & 1) * 8 + (j >> 1) * 4;
-        k[j].s = __shfl_sync(0xffffffffu, own.s, from, 16);
-        k[j].r = __shfl_sync(0xffffffffu, own.r, from, 16);
+        k[j] = q8_scale_of(__shfl_sync(0xffffffffu, own.s, from, 16), __shfl_sync(0xffffffffu, own.r, from, 16));
     }
 }
 

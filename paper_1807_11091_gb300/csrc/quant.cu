@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(256, AL ? 3 : 2) k_q8_tile(const Args a)
     }
     if (keep) {
         __syncthreads();
-        Q8Scale tile = {1.0f, 1.0f};
+        Q8Scale tile = {};
         if (a.tile) {
             float t = 0.0f;
 #pragma unroll
