@@ -165,6 +165,13 @@ PyObject* wrap_there(const Output* o, int n)
     return t;
 }
 
+// An out of its own type cannot hold what out_dtype e4m3 asks for, q and scales.
+void no_bits_in(PyObject* out, PyObject* out_dtype)
+{
+    if (out != Py_None && dtype_arg(out_dtype, at::kFloat) == at::kFloat8_e4m3fn)
+        fail(PyExc_TypeError, "out_dtype float8_e4m3fn with an out: 8-bit results are the call's own tensors");
+}
+
 // x, gamma, residual, eps, out_dtype, stats, out, sum_out, stream
 PyObject* rms_norm(PyObject* const* v)
 {
@@ -172,6 +179,7 @@ PyObject* rms_norm(PyObject* const* v)
     const Matrix m = matrix(x, "x");
     const double eps = PyFloat_AsDouble(v[3]);
     if (eps == -1.0 && PyErr_Occurred()) throw PythonError();
+    no_bits_in(v[6], v[4]);
     const ScalarType want = dtype_arg(v[4], m.type);
     const bool stats = flag(v[5]), bits = v[6] == Py_None && want == at::kFloat8_e4m3fn;
     Matrix r;
@@ -292,6 +300,7 @@ PyObject* linear8(PyObject* const* v)
     const Eight w = eight(v[2], v[3], "W", -1, m.cols);
     const Tensor* residual = tensor_or_none(v[5], "residual");
     const bool save = flag(v[8]);
+    no_bits_in(v[9], v[7]);
     Call call(x, v[10]);
     Output o[2];
     o[0] = v[9] != Py_None

@@ -922,6 +922,7 @@ def gated_backward(dh, x, Wg, Wu, g, u, act: int = SADMM_ACT_SILU, want_dx: bool
 # of any strides; the two follow each other as arguments and results.  Scales that a call
 # makes have those of a block of columns next to each other.  The transposes that the
 # backward passes read are quantize's (a weight's with tiles, so that both have its scales).
+# An `out` together with out_dtype float8_e4m3fn is refused (TypeError): it could hold neither.
 
 
 def rms_norm(x, gamma=None, residual=None, eps: float = 1e-5, out_dtype=None, stats: bool = False, out=None, sum_out=None,
