@@ -183,22 +183,14 @@ sadmm_status launch_pairs(const Q8Problem& t, cudaStream_t s)
     return st == SADMM_OK && rest.m ? launch_q8_product(rest, s) : st;
 }
 
-// Products of one call: by CTA pairs, neighbours of one kind in one launch, or by
-// single tiles.
-sadmm_status launch_q8_products(const Q8Problem* t, int n, cudaStream_t s)
+sadmm_status launch_one(const Q8Problem& t, cudaStream_t s) { return by_pairs(t) ? launch_pairs(t, s) : launch_q8_product(t, s); }
+
+// Two products of one shape that no call has one of alone: by CTA pairs in one launch, or by single tiles.
+sadmm_status launch_two(const Q8Problem* t, cudaStream_t s)
 {
-    sadmm_status st = SADMM_OK;
-    for (int i = 0; i < n && st == SADMM_OK;) {
-        int m = i;
-        while (m < n && by_pairs(t[m]) && row_scales(t[m]) == row_scales(t[i])) ++m;
-        if (m > i) {
-            st = m - i == 1 ? launch_pairs(t[i], s) : launch_q8_pair(t + i, m - i, s);
-            i = m;
-        } else {
-            st = launch_q8_product(t[i++], s);
-        }
-    }
-    return st;
+    if (by_pairs(t[0]) && by_pairs(t[1])) return launch_q8_pair(t, 2, s);
+    const sadmm_status st = launch_one(t[0], s);
+    return st == SADMM_OK ? launch_one(t[1], s) : st;
 }
 
 // What a call runs, with its places in the workspace.
@@ -258,7 +250,7 @@ sadmm_status run(Forward f, cudaStream_t s)
 {
     if (!f.t.m) return SADMM_OK;
     const sadmm_status st = run_copies(f.c, f.copies, s);
-    return st != SADMM_OK ? st : launch_q8_products(&f.t, 1, s);
+    return st != SADMM_OK ? st : launch_one(f.t, s);
 }
 
 // The gradients: a source made 8-bit by rows (for dx) and by columns (for the
@@ -347,11 +339,10 @@ sadmm_status run(Backward b, cudaStream_t s)
 {
     sadmm_status st = run_copies(b.c, b.copies, s);
     if (st == SADMM_OK) st = launch_q8_source(b.src, b.src_ws, s);
-    Q8Problem t[3];
-    int n = 0;
-    if (b.want_dx) t[n++] = b.dx;
-    for (int i = 0; i < b.dws; ++i) t[n++] = b.dw[i];
-    return st == SADMM_OK && n ? launch_q8_products(t, n, s) : st;
+    // (dx by itself: a launch that it shared with the weights' gradients gave it other bits than it has alone)
+    if (st == SADMM_OK && b.want_dx) st = launch_one(b.dx, s);
+    if (st == SADMM_OK && b.dws) st = b.dws == 2 ? launch_two(b.dw, s) : launch_one(b.dw[0], s);
+    return st;
 }
 
 }  // namespace

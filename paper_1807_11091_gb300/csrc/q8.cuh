@@ -42,7 +42,7 @@ inline bool q8_aligned(const void* p, long long ld)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 15) == 0;
 }
 
-// One tile a CTA (q8gemm.cu), or up to three products by CTA pairs (q8pair.cu), and the times
+// One tile a CTA (q8gemm.cu), or one or two products by CTA pairs (q8pair.cu), and the times
 // they are expected to take.
 sadmm_status launch_q8_product(const Q8Problem& t, cudaStream_t s);
 long long time_q8_product(const Q8Problem& t);

@@ -50,7 +50,7 @@ struct Tile {
     // the ring of scales: [block][row of the CTA], then [block][column], or where 128 columns have one [half][block]
     static constexpr int own = VEC ? 256 : 128, columns = 4 * own;
 };
-constexpr int kProducts = 3;
+constexpr int kProducts = 2, kOperands = 4;            // of a launch, and maps of its operands
 constexpr int kBoxBytes = 4096;                       // 32 output rows of 128 bytes on their way out
 constexpr int kSlots = 3;                             // places of the ring of scales, four blocks each
 constexpr int kSlotFloats = 4 * 384;
@@ -70,7 +70,7 @@ struct Product {
 };
 
 struct Maps {
-    CUtensorMap map[8 + kProducts + 2];
+    CUtensorMap map[kOperands + kProducts + 2];
 };
 
 struct Args {
@@ -858,11 +858,11 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
         const int na = p.sum ? 2 : 1, nb = p.sum || gated ? 2 : 1;
         p.pm = next;
         for (int j = 0; j < na; ++j)
-            if (next >= 8 || !encode8(&maps.map[next++], q.a[j], 128)) return SADMM_ECUDA;
+            if (next >= kOperands || !encode8(&maps.map[next++], q.a[j], 128)) return SADMM_ECUDA;
         p.qm = next;
         for (int j = 0; j < nb; ++j)
-            if (next >= 8 || !encode8(&maps.map[next++], q.b[j], vec ? 64 : 128)) return SADMM_ECUDA;
-        p.ym = encode_out(&maps.map[8 + i], q.y, q.m, q.n) ? 8 + i : -1;
+            if (next >= kOperands || !encode8(&maps.map[next++], q.b[j], vec ? 64 : 128)) return SADMM_ECUDA;
+        p.ym = encode_out(&maps.map[kOperands + i], q.y, q.m, q.n) ? kOperands + i : -1;
         for (int j = 0; j < 2; ++j) {
             p.ps[j] = scales_of(q.a[na == 2 ? j : 0]);
             p.qs[j] = scales_of(q.b[nb == 2 ? j : 0]);
@@ -877,8 +877,9 @@ sadmm_status launch_q8_pair(const Q8Problem* problems, int count, cudaStream_t s
     if (f.residual.p) a.t.res = make_out(f.residual, f.m, f.n);
     if (f.z.p) a.t.z = make_out(f.z, f.m, f.n);
     if (f.u.p) a.t.u = make_out(f.u, f.m, f.n);
-    a.zm = !vec && encode_out(&maps.map[8 + kProducts], f.z, f.m, f.n) ? 8 + kProducts : -1;
-    a.um = encode_out(&maps.map[9 + kProducts], f.u, f.m, f.n) ? 9 + kProducts : -1;
+    constexpr int zm = kOperands + kProducts, um = zm + 1;
+    a.zm = !vec && encode_out(&maps.map[zm], f.z, f.m, f.n) ? zm : -1;
+    a.um = encode_out(&maps.map[um], f.u, f.m, f.n) ? um : -1;
     a.t.status = device_status_ptr();
     a.y8 = f.y8;
     a.idesc = (1u << 4) | (vec ? 128u >> 3 : 256u >> 3) << 17 | (256u >> 4) << 24;  // e4m3 operands, fp32 sums
