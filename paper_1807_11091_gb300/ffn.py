@@ -99,6 +99,11 @@ class FeedForward8:
     updates, and in 8 bits with a scale for each 128 x 128 tile, as they are and
     transposed.  Whoever changes the bf16 weights calls ``quantize()`` afterwards.
     ``saved`` is as in FeedForward: what a backward pass reads of its forward(train=True).
+
+    A training pass does not give the bits of a plain one: n and h are rounded to bf16 before
+    they are made 8-bit (their transposes, which the gradients read, are made from bf16), where the
+    plain pass makes them 8-bit from fp32.  The rounding is off by up to 2^-8, the 8-bit
+    form by 2^-4 in either.
     """
 
     def __init__(self, gamma, Wg, Wu, Wd, bias=None, act: int = sadmm.SADMM_ACT_SILU, eps: float = 1e-5):
@@ -122,7 +127,7 @@ class FeedForward8:
 
     def forward(self, x, delta=None, train: bool = False):
         """x [tokens][D] (bf16 or fp32, the residual stream) -> y of the same type.  With `delta`, the
-        output of the layer before that is still to be added to it, x + delta in x's place."""
+        output of the layer before that is still to be added to it, that of x + delta (x itself stays as it is)."""
         import torch
         if not train:
             if delta is None:
