@@ -5,8 +5,8 @@
 // du = dh act(g), whose column sums (the bias's gradient) are taken on the way.
 //
 // Measured: 10240 x 4096 bf16 in tiles, both ways, 51 us (25 of its 168 MB at 6.79 TB/s), bound by
-// issuing (56 % of the cycles) and shared memory; the gated pair's dg and du of 4096 x 5461, both
-// ways, 105 us cold (33 of its 224 MB), bound by issuing (67 %): act, its slope and two quotients a value;
+// issuing (58 % of the cycles) and shared memory; the gated pair's dg and du of 4096 x 5461, both
+// ways, 100 us cold (33 of its 224 MB), bound by issuing (67 %): act, its slope and two quotients a value;
 // 131 with both in one CTA, a quotient and a row's scale at a time.
 #include "act.cuh"
 #include "q8.cuh"

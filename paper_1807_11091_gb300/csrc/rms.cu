@@ -7,8 +7,9 @@
 // Bound by memory.  A group of threads (a warp, or a block for long rows) takes a row at a
 // time and keeps it in registers; sixteen lanes hold a block of 128 columns, so that its
 // scale is a matter of four shuffles.  Measured: 16384 x 4096 bf16 with an fp32 residual into e4m3,
-// sum and 1/rms kept, 119 us (109 of its 740 MB at the copy's 6.79 TB/s); 4 x 4096 6.9 us, a launch,
-// a row's loads and its sum one after the other.
+// sum and 1/rms kept, 116 us (109 of its 740 MB at the copy's 6.79 TB/s); 4 x 4096 6.9 us, a launch,
+// a row's loads and its sum one after the other.  Both from fp32 into bf16, 161 us (138); 4096 x 16384
+// of them 179: past 8192 columns a thread's 32 values of two fp32 matrices do not fit 64 registers (260 bytes spilled).
 #include "q8.cuh"
 
 namespace sadmm {
